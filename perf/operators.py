@@ -234,7 +234,8 @@ def _run_own(st, case):
     cache = st["cache"]
     if kind == "arrive":
         cas.cascade_pages_free(cache, st["all"])
-        cas.cascade_paged_extend(cache, st["q_start"], st["slots"], st["visible"], st["accepted"], row_shard=st["shard"])
+        cas.cascade_paged_extend(cache, st["q_start"], st["slots"], st["visible"], st["accepted"],
+                                 row_shard=st["shard"] if case["shards"] > 1 else None)
         cas.cascade_paged_append(cache, 0, st["slots"], st["k"], st["v"], positions=st["positions"], rope=st["rope"], q=st["q0"], q_out=st["q"])
     elif kind == "branch":
         cas.cascade_pages_free(cache, st["dst"])
