@@ -467,6 +467,159 @@ CASCADE_API int32_t cascade_layer_kv_to_cache(const cascade_plan *plan, const ca
                                   const void *workspace, void *k_cache, void *v_cache,
                                   int32_t shard_capacity, int32_t *shard_len_dev, void *stream);
 
+/* ------------------------------------------------------------------ rotary positions
+ * The rotation of EPI_ROPE as an operator of its own (queries and keys of a paged cache, whose
+ * positions differ from row to row), with the variants that models use.  The first rot_dim
+ * columns of every head are turned in rot_dim / 2 pairs (a, b), the rest is passed on:
+ *   (a, b) -> amplitude * (a cos - b sin, a sin + b cos),  angle = position * f_i
+ *   f_i = theta^(-2i / rot_dim), i < rot_dim / 2
+ *   ROPE_LINEAR: f_i / factor
+ *   ROPE_RAMP:   f_i ((1 - g) / factor + g), g = clamp((r - low) / (high - low), 0, 1),
+ *                r = original_len * f_i / (2 pi): turns that pair i makes over original_len
+ * Angles are formed in 64 bits, so that they hold at every int32 position; a negative
+ * position turns back.                                                            */
+#define CASCADE_ROPE_HALF        0 /* pairs (i, i + rot_dim / 2)                       */
+#define CASCADE_ROPE_INTERLEAVED 1 /* pairs (2i, 2i + 1)                               */
+#define CASCADE_ROPE_UNSCALED 0
+#define CASCADE_ROPE_LINEAR   1
+#define CASCADE_ROPE_RAMP     2
+
+typedef struct cascade_rope_desc {
+    int32_t layout;       /* CASCADE_ROPE_HALF | CASCADE_ROPE_INTERLEAVED             */
+    int32_t rot_dim;      /* even, 2 .. 512, at most the head dimension               */
+    int32_t scaling;      /* CASCADE_ROPE_UNSCALED | _LINEAR | _RAMP                  */
+    int32_t original_len; /* ROPE_RAMP: above 0                                       */
+    double  theta;        /* above 0                                                  */
+    double  factor;       /* ROPE_LINEAR, ROPE_RAMP: above 0                          */
+    double  low, high;    /* ROPE_RAMP: low < high                                    */
+    double  amplitude;    /* of the rotated columns (1: a rotation)                   */
+} cascade_rope_desc;
+
+/* x, y: rows of n_heads * head_dim elements, x_stride / y_stride elements apart (0:
+ * dense); positions_dev [rows] int32.  y may be x (with the same stride); otherwise
+ * they must not overlap.  Errors: EINVAL, ESHAPE (strides below a row, rot_dim above
+ * head_dim, y == x with another stride), EUNSUPPORTED (dtype, rot_dim), EHIP.       */
+CASCADE_API int32_t cascade_rope(const cascade_rope_desc *desc, int32_t dtype, int32_t rows, int32_t n_heads,
+                     int32_t head_dim, const int32_t *positions_dev, const void *x, int64_t x_stride, void *y,
+                     int64_t y_stride, void *stream);
+
+/* ------------------------------------------------------------------ paged cache
+ * The token-sharded cache of cascade_decode_partial_attn in pages instead of slabs:
+ * sequences grow by any number of tokens at a time, share what they have in common,
+ * and hold no memory that they do not use.  Every (sequence, key/value shard) pair has
+ * a list of pages; row r of shard s (ascending token index inside the shard) lies in
+ * page page_table[sequence][s][r / page_size] at row r % page_size.  A page is free if
+ * its page_refs is 0.  Only pages whose rows are all in use are ever shared
+ * (page_refs above 1): rows are only written behind the end of a list, in a page that
+ * list holds alone.  One set of lists serves the pools of all layers.
+ * The descriptor is read during the call; what it points to belongs to the caller.
+ * Page ids and lengths are read on the device: an id outside [0, n_pages) holds no
+ * keys (they are skipped like masked ones), lengths count up to max_pages * page_size. */
+typedef struct cascade_paged_cache {
+    int32_t dtype;
+    int32_t n_layers, n_pages;
+    int32_t n_kv_heads, head_dim;     /* head_dim: a multiple of 8 (bf16) or 4 (f32), at most 256 */
+    int32_t page_size;                /* rows: a power of two, 16 .. 65536             */
+    int32_t n_seqs, n_shards;         /* n_shards: at most 1024                        */
+    int32_t max_pages;                /* of a list                                     */
+    void *k_pages, *v_pages;          /* [n_layers, n_pages, H_KV, page_size, d], 16-byte aligned */
+    int32_t *page_table;              /* [n_seqs, n_shards, max_pages]; unused entries -1 */
+    int32_t *kv_len;                  /* [n_seqs, n_shards] rows                       */
+    int32_t *page_refs;               /* [n_pages]                                     */
+} cascade_paged_cache;
+
+/* Room for new rows, once per step and before the layers' cascade_paged_append.  The
+ * rows of all sequences lie back to back: those of sequence b are q_start_dev[b] ..
+ * q_start_dev[b + 1] (q_start_dev [n_seqs + 1], ascending; a sequence may have none).
+ * row_shard_dev [rows]: key/value shard of each row (NULL: one shard only).  Pages are
+ * taken lowest id first, list by list.  Outputs (device, int32):
+ *   slots [rows]              page * page_size + row of the page; -1: row not stored
+ *   visible [rows, n_shards]  rows of shard s at or before this row, itself included:
+ *                             the causal limit of cascade_paged_attn
+ *   accepted [n_seqs]         0: the sequence did not fit (no free page, list full) and
+ *                             is as it was, its rows have slot -1 and see nothing
+ * and kv_len, page_table, page_refs are brought up to date.  Once a sequence finds no
+ * free page, later ones that need one are refused too.  Rows behind the last sequence
+ * (a padded batch) have slot -1 and see nothing; so does a row whose shard id is outside
+ * [0, n_shards), but it sees what its neighbours see.
+ * Errors: EINVAL, EUNSUPPORTED (sizes above), EHIP.                                 */
+CASCADE_API int32_t cascade_paged_extend(const cascade_paged_cache *cache, int32_t rows, const int32_t *q_start_dev,
+                             const int32_t *row_shard_dev, int32_t *slots, int32_t *visible, int32_t *accepted,
+                             void *stream);
+
+/* Writes the keys and values of `rows` new rows into their slots in layer `layer`'s
+ * pages.  k, v: rows of H_KV * d elements, kv_stride apart (0: dense).  With `rope` the
+ * keys are rotated on the way (positions_dev [rows]), and so are n_heads queries per row
+ * from q to q_out if q is given (rows of n_heads * d elements; q_out may be q with the
+ * same stride).  Without `rope`, positions_dev and q are NULL.  A row whose slot is
+ * outside [0, n_pages * page_size) is not stored (its queries are rotated all the same);
+ * no slot may be named twice.
+ * Errors: EINVAL, ESHAPE (strides, rot_dim above head_dim, layer), EUNSUPPORTED, EHIP. */
+CASCADE_API int32_t cascade_paged_append(const cascade_paged_cache *cache, int32_t layer, int32_t rows,
+                             const int32_t *slots_dev, const void *k, const void *v, int64_t kv_stride,
+                             const cascade_rope_desc *rope, const int32_t *positions_dev, int32_t n_heads,
+                             const void *q, int64_t q_stride, void *q_out, int64_t q_out_stride, void *stream);
+
+/* Attention of the new rows over the cached keys of their sequence, the partials of all
+ * key/value shards merged (Algorithms 3 and 4 on the rows at hand): one token per
+ * sequence, a chunk of a prompt, or both at once.  Row t of sequence b, which are the
+ * rows q_start_dev[b] .. q_start_dev[b + 1], sees the rows j < visible_dev[t][s] of
+ * shard s (at most kv_len of them); visible_dev [rows, n_shards], as
+ * cascade_paged_extend writes it.  NULL: all kv_len rows, without a mask (a bidirectional
+ * chunk, or cross attention to cached states).  Query head h reads kv head
+ * h / (n_heads / H_KV).
+ *   o [rows, n_heads * d] in o_dtype; lse [n_heads, rows] fp32 = log sum exp(a) (NULL:
+ *   not wanted).  A row that sees nothing: o = 0, lse = -inf.  Rows behind the last
+ *   sequence are left as they were.  What a row does not see never reaches it, be it
+ *   NaN.  With o in fp32, (lse, 1, o) is a partial that cascade_lse_merge takes
+ *   (CASCADE_U_NORMALISED), where other parties hold more shards.
+ * q, o 16-byte aligned, strides in elements (0: dense) and multiples of 16 bytes.  Calls
+ * that may overlap in time need a workspace each (16-byte aligned); its contents need
+ * not be kept between calls.
+ * Errors: EINVAL, ESHAPE (n_heads % H_KV, strides, layer), EUNSUPPORTED (alignment,
+ * sizes), EWORKSPACE, EHIP.                                                         */
+typedef struct cascade_paged_attn_desc {
+    int32_t rows, n_heads;
+    float   scale;
+    int32_t o_dtype;      /* the cache's, or CASCADE_F32                              */
+    int64_t q_stride, o_stride;
+} cascade_paged_attn_desc;
+
+CASCADE_API size_t cascade_paged_attn_workspace_bytes(const cascade_paged_cache *cache, const cascade_paged_attn_desc *desc);
+CASCADE_API int32_t cascade_paged_attn(const cascade_paged_cache *cache, int32_t layer, const cascade_paged_attn_desc *desc,
+                           const int32_t *q_start_dev, const int32_t *visible_dev, const void *q, void *o, float *lse,
+                           void *workspace, size_t workspace_bytes, void *stream);
+
+/* Pages of finished or dropped sequences: every list of the n sequences seqs_dev [n]
+ * becomes empty and its pages lose one reference each.  Ids outside [0, n_seqs) are
+ * skipped, one named twice is freed once.  Errors: EINVAL, EUNSUPPORTED, EHIP.      */
+CASCADE_API int32_t cascade_pages_free(const cascade_paged_cache *cache, int32_t n, const int32_t *seqs_dev, void *stream);
+
+/* Branches: sequence dst_dev[i] becomes a copy of src_dev[i], i < n.  Full pages are
+ * shared; a last page that is partly filled is copied, its used rows in every layer, into
+ * the lowest free page.  accepted [n] (device): 0 where a pair was refused and changed
+ * nothing: an id out of range, a destination that is not empty or that an earlier pair
+ * names too, or no free page (for every later pair that needs one as well).  Sources are
+ * taken as they were before the call.  n * n_shards at most 8192.
+ * Errors: EINVAL, EUNSUPPORTED, EWORKSPACE, EHIP.                                   */
+CASCADE_API size_t cascade_pages_workspace_bytes(const cascade_paged_cache *cache);
+CASCADE_API int32_t cascade_pages_fork(const cascade_paged_cache *cache, int32_t n, const int32_t *src_dev,
+                           const int32_t *dst_dev, int32_t *accepted, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Moves the pages in use to the front of the pools: afterwards they are 0 .. n_live - 1
+ * (n_live: device int32, may be NULL).  Pages behind that move, in ascending order, to
+ * the free ones before it; the lists follow.
+ * Errors: EINVAL, EUNSUPPORTED, EWORKSPACE, EHIP.                                   */
+CASCADE_API int32_t cascade_pages_compact(const cascade_paged_cache *cache, int32_t *n_live, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/* Copies page src_dev[i] onto page dst_dev[i] in every layer, i < n; pairs with an id
+ * outside [0, n_pages) are skipped.  No page may be a destination twice, nor a source
+ * and another pair's destination.  Lists and references stay.
+ * Errors: EINVAL, EUNSUPPORTED, EHIP.                                               */
+CASCADE_API int32_t cascade_pages_copy(const cascade_paged_cache *cache, int32_t n, const int32_t *src_dev,
+                           const int32_t *dst_dev, void *stream);
+
 /* ------------------------------------------------------------------ measured ceiling
  * Not a step of the method: the rate (TFLOP/s) this device sustains on back-to-back
  * bf16 16x16x32 MFMAs with random operands, for the roofline figures quoted next

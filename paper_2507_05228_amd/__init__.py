@@ -23,6 +23,8 @@ NORM_NONE, NORM_LAYERNORM, NORM_RMSNORM = 0, 1, 2
 ACT_GELU_ERF, ACT_GELU_TANH, ACT_SWIGLU = 0, 1, 2
 ATTN_FUSED, ATTN_MATERIALISED = 0, 1
 NORM_PRE, NORM_POST = 0, 1
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_UNSCALED, ROPE_LINEAR, ROPE_RAMP = 0, 1, 2
 EPI_BIAS, EPI_GELU_ERF, EPI_GELU_TANH, EPI_SWIGLU, EPI_ROPE, EPI_RESIDUAL = 1, 2, 4, 8, 16, 32
 
 EXPORTS = ["cascade_plan_create", "cascade_plan_create_rs", "cascade_plan_maps", "cascade_plan_maps_host",
@@ -33,7 +35,9 @@ EXPORTS = ["cascade_plan_create", "cascade_plan_create_rs", "cascade_plan_maps",
            "cascade_layer_forward", "cascade_layer_forward_staged", "cascade_layer_partials",
            "cascade_layer_stack_workspace_bytes", "cascade_layer_stack_forward",
            "cascade_lm_head_workspace_bytes", "cascade_lm_head", "cascade_greedy_token", "cascade_layer_kv_to_cache", "cascade_norm",
-           "cascade_decode_partial_attn", "cascade_mfma_ceiling"]
+           "cascade_decode_partial_attn", "cascade_mfma_ceiling", "cascade_rope", "cascade_paged_extend", "cascade_paged_append",
+           "cascade_paged_attn_workspace_bytes", "cascade_paged_attn", "cascade_pages_free", "cascade_pages_workspace_bytes",
+           "cascade_pages_fork", "cascade_pages_compact", "cascade_pages_copy"]
 N_STAGE_EVENTS = 10
 STAGE_NAMES = ["gather_norm1", "qkv_gemm", "rope", "attention", "lse_merge", "o_proj", "norm2", "ffn_up", "ffn_down"]
 
@@ -71,6 +75,23 @@ class LmHeadDesc(C.Structure):
 
 
 LM_ALL_ROWS, LM_LAST_ROW = 0, 1
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [("layout", C.c_int32), ("rot_dim", C.c_int32), ("scaling", C.c_int32), ("original_len", C.c_int32),
+                ("theta", C.c_double), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double), ("amplitude", C.c_double)]
+
+
+class PagedCache(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_layers", C.c_int32), ("n_pages", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("page_size", C.c_int32), ("n_seqs", C.c_int32), ("n_shards", C.c_int32),
+                ("max_pages", C.c_int32), ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_table", C.c_void_p),
+                ("kv_len", C.c_void_p), ("page_refs", C.c_void_p)]
+
+
+class PagedAttnDesc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("n_heads", C.c_int32), ("scale", C.c_float), ("o_dtype", C.c_int32),
+                ("q_stride", C.c_int64), ("o_stride", C.c_int64)]
 
 _WEIGHT_FIELDS = ["wq", "wk", "wv", "wo", "w_gate", "w_up", "w_down", "bq", "bk", "bv", "bo", "b_up", "b_down",
                   "norm1_g", "norm1_b", "norm2_g", "norm2_b"]
@@ -161,6 +182,19 @@ def load_library():
     lib.cascade_decode_partial_attn.restype = I32
     lib.cascade_mfma_ceiling.argtypes = [I32, I32, P(C.c_float), VP]
     lib.cascade_mfma_ceiling.restype = I32
+    I64, PC = C.c_int64, P(PagedCache)
+    for name, args in {
+            "cascade_rope": [P(RopeDesc), I32, I32, I32, I32, VP, VP, I64, VP, I64, VP],
+            "cascade_paged_extend": [PC, I32, VP, VP, VP, VP, VP, VP],
+            "cascade_paged_append": [PC, I32, I32, VP, VP, VP, I64, P(RopeDesc), VP, I32, VP, I64, VP, I64, VP],
+            "cascade_paged_attn": [PC, I32, P(PagedAttnDesc), VP, VP, VP, VP, VP, VP, C.c_size_t, VP],
+            "cascade_pages_free": [PC, I32, VP, VP],
+            "cascade_pages_fork": [PC, I32, VP, VP, VP, VP, C.c_size_t, VP],
+            "cascade_pages_compact": [PC, VP, VP, C.c_size_t, VP],
+            "cascade_pages_copy": [PC, I32, VP, VP, VP]}.items():
+        getattr(lib, name).argtypes, getattr(lib, name).restype = args, I32
+    lib.cascade_paged_attn_workspace_bytes.argtypes, lib.cascade_paged_attn_workspace_bytes.restype = [PC, P(PagedAttnDesc)], C.c_size_t
+    lib.cascade_pages_workspace_bytes.argtypes, lib.cascade_pages_workspace_bytes.restype = [PC], C.c_size_t
     _lib = lib
     return lib
 
@@ -534,6 +568,163 @@ def cascade_decode_partial_attn(q, k_cache, v_cache, shard_len, m, e, u, scale, 
     st = lib.cascade_decode_partial_attn(C.byref(desc), B, S, cap, _ptr(shard_len), _ptr(q), _ptr(k_cache), _ptr(v_cache),
                                          _ptr(m), _ptr(e), _ptr(u), _stream(stream))
     _check(st, "cascade_decode_partial_attn")
+
+
+# ------------------------------------------------------------------ rotary positions and the paged cache
+def make_rope_desc(rot_dim, theta, layout=ROPE_HALF, scaling=ROPE_UNSCALED, factor=1.0, low=1.0, high=4.0, original_len=0,
+                   amplitude=1.0):
+    return RopeDesc(layout, rot_dim, scaling, original_len, theta, factor, low, high, amplitude)
+
+
+def _head_rows(t, where):
+    """Row stride of a [rows, heads, d] tensor whose heads lie back to back."""
+    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise CascadeError(ESHAPE, f"{where}: [rows, heads, d] with dense heads")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _checked(where, dtype, **tensors):
+    """Tensors of a call that are contiguous, on the GPU, and of the given type (None passes)."""
+    for name, t in tensors.items():
+        if t is not None and (t.dtype != dtype or not t.is_contiguous() or not t.is_cuda):
+            raise CascadeError(ESHAPE, f"{where}: {name} must be a contiguous {dtype} tensor on the GPU")
+
+
+def _counted(where, *checks):
+    for ok, what in checks:
+        if not ok:
+            raise CascadeError(ESHAPE, f"{where}: {what}")
+
+
+def cascade_rope(desc, x, positions, y=None, stream=None):
+    """x [rows, heads, d] (heads dense, rows at any stride), positions int32 [rows]; y like x (None: in place)."""
+    import torch
+    lib = load_library()
+    y = x if y is None else y
+    _checked("cascade_rope", torch.int32, positions=positions)
+    _counted("cascade_rope", (x.dim() == 3 and y.shape == x.shape and y.dtype == x.dtype, "y like x"),
+             (positions is None or positions.numel() == x.shape[0], "a position per row"))
+    st = lib.cascade_rope(C.byref(desc), _dtype_code(x), x.shape[0], x.shape[1], x.shape[2], _ptr(positions), _ptr(x),
+                          _head_rows(x, "cascade_rope"), _ptr(y), _head_rows(y, "cascade_rope"), _stream(stream))
+    _check(st, "cascade_rope")
+
+
+def make_paged_cache(k_pages, v_pages, page_table, kv_len, page_refs):
+    """PagedCache of k_pages, v_pages [layers, pages, Hkv, page_size, d], page_table int32 [seqs, shards, max_pages], kv_len
+    int32 [seqs, shards] and page_refs int32 [pages].  The cache keeps the tensors alive."""
+    import torch
+    _checked("make_paged_cache", k_pages.dtype, k_pages=k_pages, v_pages=v_pages)
+    _checked("make_paged_cache", torch.int32, page_table=page_table, kv_len=kv_len, page_refs=page_refs)
+    _counted("make_paged_cache", (k_pages.dim() == 5 and v_pages.shape == k_pages.shape, "k_pages, v_pages [layers, pages, Hkv, page_size, d]"),
+             (page_table.dim() == 3 and kv_len.shape == page_table.shape[:2], "page_table [seqs, shards, max_pages], kv_len [seqs, shards]"),
+             (page_refs.shape == k_pages.shape[1:2], "page_refs [pages]"))
+    L, n_pages, Hkv, page, d = k_pages.shape
+    cache = PagedCache(_dtype_code(k_pages), L, n_pages, Hkv, d, page, *page_table.shape, k_pages.data_ptr(), v_pages.data_ptr(),
+                       page_table.data_ptr(), kv_len.data_ptr(), page_refs.data_ptr())
+    cache.tensors = (k_pages, v_pages, page_table, kv_len, page_refs)
+    return cache
+
+
+def cascade_paged_extend(cache, q_start, slots, visible, accepted, row_shard=None, stream=None):
+    """q_start int32 [seqs + 1]; slots int32 [rows], visible int32 [rows, shards], accepted int32 [seqs] are written."""
+    import torch
+    lib = load_library()
+    _checked("cascade_paged_extend", torch.int32, q_start=q_start, slots=slots, visible=visible, accepted=accepted, row_shard=row_shard)
+    rows = slots.numel()
+    _counted("cascade_paged_extend", (q_start.numel() == cache.n_seqs + 1, "q_start [seqs + 1]"),
+             (visible.numel() == rows * cache.n_shards, "visible [rows, shards]"), (accepted.numel() == cache.n_seqs, "accepted [seqs]"),
+             (row_shard is None or row_shard.numel() == rows, "row_shard [rows]"))
+    _check(lib.cascade_paged_extend(C.byref(cache), rows, _ptr(q_start), _ptr(row_shard), _ptr(slots), _ptr(visible), _ptr(accepted),
+                                    _stream(stream)), "cascade_paged_extend")
+
+
+def cascade_paged_append(cache, layer, slots, k, v, positions=None, rope=None, q=None, q_out=None, stream=None):
+    """k, v [rows, Hkv, d] and q [rows, H, d] with dense heads (views of a fused projection serve); q_out None: q in place."""
+    import torch
+    lib = load_library()
+    where = "cascade_paged_append"
+    _checked(where, torch.int32, slots=slots, positions=positions)
+    rows = slots.numel()
+    _counted(where, (k.dim() == 3 and k.shape == v.shape == (rows, cache.n_kv_heads, cache.head_dim), "k, v [rows, Hkv, d]"),
+             (_dtype_code(k) == _dtype_code(v) == cache.dtype, "k, v of the cache's type"),
+             (rows < 2 or k.stride(0) == v.stride(0), "k and v of one row stride"),
+             (positions is None or positions.numel() == rows, "a position per row"))
+    _head_rows(v, where)
+    q_out = q if q_out is None else q_out
+    qs = qos = heads = 0
+    if q is not None:
+        _counted(where, (q.dim() == 3 and q.shape[0] == rows and q.shape[2] == cache.head_dim and q_out.shape == q.shape, "q, q_out [rows, H, d]"),
+                 (_dtype_code(q) == _dtype_code(q_out) == cache.dtype, "q, q_out of the cache's type"))
+        heads, qs, qos = q.shape[1], _head_rows(q, where), _head_rows(q_out, where)
+    st = lib.cascade_paged_append(C.byref(cache), layer, rows, _ptr(slots), _ptr(k), _ptr(v), _head_rows(k, where),
+                                  None if rope is None else C.byref(rope), _ptr(positions), heads, _ptr(q), qs, _ptr(q_out), qos,
+                                  _stream(stream))
+    _check(st, where)
+
+
+def cascade_paged_attn_workspace_bytes(cache, rows, n_heads):
+    desc = PagedAttnDesc(rows, n_heads, 1.0, cache.dtype, 0, 0)
+    return load_library().cascade_paged_attn_workspace_bytes(C.byref(cache), C.byref(desc))
+
+
+def cascade_paged_attn(cache, layer, q, o, q_start, scale, visible=None, lse=None, workspace=None, stream=None):
+    """q, o [rows, H, d] with dense heads (o in the cache's type or fp32); q_start int32 [seqs + 1]; visible int32 [rows, shards]
+    (None: no mask); lse fp32 [H, rows] or None."""
+    import torch
+    lib = load_library()
+    where = "cascade_paged_attn"
+    _checked(where, torch.int32, q_start=q_start, visible=visible)
+    _checked(where, torch.float32, lse=lse)
+    _counted(where, (q.dim() == 3 and q.shape[2] == cache.head_dim and o.shape == q.shape, "q, o [rows, H, d]"),
+             (_dtype_code(q) == cache.dtype, "q of the cache's type"), (q_start.numel() == cache.n_seqs + 1, "q_start [seqs + 1]"),
+             (visible is None or visible.numel() == q.shape[0] * cache.n_shards, "visible [rows, shards]"),
+             (lse is None or lse.numel() == q.shape[0] * q.shape[1], "lse [H, rows]"))
+    desc = PagedAttnDesc(q.shape[0], q.shape[1], scale, _dtype_code(o), _head_rows(q, where), _head_rows(o, where))
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    st = lib.cascade_paged_attn(C.byref(cache), layer, C.byref(desc), _ptr(q_start), _ptr(visible), _ptr(q), _ptr(o), _ptr(lse),
+                                _ptr(workspace), ws_bytes, _stream(stream))
+    _check(st, where)
+
+
+def cascade_pages_free(cache, seqs, stream=None):
+    """seqs int32 [n]."""
+    import torch
+    lib = load_library()
+    _checked("cascade_pages_free", torch.int32, seqs=seqs)
+    _check(lib.cascade_pages_free(C.byref(cache), seqs.numel(), _ptr(seqs), _stream(stream)), "cascade_pages_free")
+
+
+def cascade_pages_workspace_bytes(cache):
+    return load_library().cascade_pages_workspace_bytes(C.byref(cache))
+
+
+def cascade_pages_fork(cache, src, dst, accepted, workspace, stream=None):
+    """src, dst, accepted int32 [n]."""
+    import torch
+    lib = load_library()
+    _checked("cascade_pages_fork", torch.int32, src=src, dst=dst, accepted=accepted)
+    _counted("cascade_pages_fork", (src.numel() == dst.numel() == accepted.numel(), "src, dst, accepted [n]"))
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib.cascade_pages_fork(C.byref(cache), src.numel(), _ptr(src), _ptr(dst), _ptr(accepted), _ptr(workspace), ws_bytes,
+                                  _stream(stream)), "cascade_pages_fork")
+
+
+def cascade_pages_compact(cache, n_live, workspace, stream=None):
+    """n_live int32 [1] or None."""
+    import torch
+    lib = load_library()
+    _checked("cascade_pages_compact", torch.int32, n_live=n_live)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib.cascade_pages_compact(C.byref(cache), _ptr(n_live), _ptr(workspace), ws_bytes, _stream(stream)), "cascade_pages_compact")
+
+
+def cascade_pages_copy(cache, src, dst, stream=None):
+    """src, dst int32 [n]."""
+    import torch
+    lib = load_library()
+    _checked("cascade_pages_copy", torch.int32, src=src, dst=dst)
+    _counted("cascade_pages_copy", (src.numel() == dst.numel(), "src, dst [n]"))
+    _check(lib.cascade_pages_copy(C.byref(cache), src.numel(), _ptr(src), _ptr(dst), _stream(stream)), "cascade_pages_copy")
 
 
 def cascade_mfma_ceiling(lds_operands, iters=200000, stream=None):
