@@ -27,6 +27,8 @@ struct PagedAttnParams {
 };
 
 constexpr int PAGED_TARGET = 1024;                         // pieces of a launch, all kv heads together
+constexpr int PAGED_TILE = 256, PAGED_TILE_TARGET = 256;   // paged_attn_tile.hip: rows of a tile; pieces
+constexpr int PAGED_FEW = 32;                              // flattened rows of a sequence up to which it goes to paged_attn_rows.hip
 
 struct PagedWork {
     int b, first_row, n_rows;                              // sequence, its first row in q, its flattened rows
@@ -116,4 +118,38 @@ static inline PagedGrid paged_grid(const PagedAttnParams &p, int tile) {
     return g;
 }
 
+int32_t launch_paged_tile(PagedAttnParams p, float *workspace, hipStream_t s);
+
+constexpr float LN2F = 0.6931471805599453f;
+
+// Tiles whose walk was cut: their partials, weighted by exp2(m - largest m)
+template <typename T, int TILE, int KEYS>
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnParams p) {
+    PagedWork wk;
+    if (!paged_find_work<TILE, KEYS, true>(p, blockIdx.x, wk)) return;
+    const int g = blockIdx.y, per_row = p.d / 4;
+    const int64_t step = (int64_t)p.Hkv * TILE;
+    for (int e = threadIdx.x + 256 * blockIdx.z; e < TILE * per_row; e += 256 * gridDim.z) {
+        const int row = e / per_row, c = (e - row * per_row) * 4, r = wk.tile * TILE + row;
+        if (r >= wk.n_rows) break;
+        const int64_t at = ((int64_t)wk.first_piece * p.Hkv + g) * TILE + row;
+        float top = -INFINITY;
+        for (int i = 0; i < wk.n_pieces; ++i) top = fmaxf(top, p.part_ml[(at + i * step) * 2]);
+        const float off = top == -INFINITY ? 0.f : top;
+        float sum = 0.f;
+        f32x4 u = {0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < wk.n_pieces; ++i) {
+            const float f = __builtin_amdgcn_exp2f(p.part_ml[(at + i * step) * 2] - off);
+            sum += p.part_ml[(at + i * step) * 2 + 1] * f;
+            u += *(const f32x4 *)(p.part_u + (at + i * step) * p.d + c) * f;
+        }
+        const int t = r / p.rep, h = g * p.rep + r - t * p.rep;
+        const int64_t out = (int64_t)(wk.first_row + t) * p.o_stride + (int64_t)h * p.d + c;
+        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+        u *= inv;
+        if (sizeof(T) == 4 || p.o_f32) *(f32x4 *)((float *)p.o + out) = u;
+        else *(bf16x4 *)((bf16_t *)p.o + out) = bf16x4{(bf16_t)u[0], (bf16_t)u[1], (bf16_t)u[2], (bf16_t)u[3]};
+        if (c == 0 && p.lse) p.lse[(int64_t)h * p.rows + wk.first_row + t] = (top + __builtin_log2f(sum)) * LN2F;
+    }
+}
 

@@ -19,7 +19,6 @@
 namespace {
 
 constexpr float RAISE = 8.0f;
-constexpr float LN2F = 0.6931471805599453f;
 
 template <typename T> struct Kind;
 template <> struct Kind<bf16_t> {
@@ -385,37 +384,6 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedAttnParams p) {
     }
 }
 
-// Tiles whose walk was cut: their partials, weighted by exp2(m - largest m)
-template <typename T, int TILE, int KEYS>
-__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnParams p) {
-    PagedWork wk;
-    if (!paged_find_work<TILE, KEYS, true>(p, blockIdx.x, wk)) return;
-    const int g = blockIdx.y, per_row = p.d / 4;
-    const int64_t step = (int64_t)p.Hkv * TILE;
-    for (int e = threadIdx.x + 256 * blockIdx.z; e < TILE * per_row; e += 256 * gridDim.z) {
-        const int row = e / per_row, c = (e - row * per_row) * 4, r = wk.tile * TILE + row;
-        if (r >= wk.n_rows) break;
-        const int64_t at = ((int64_t)wk.first_piece * p.Hkv + g) * TILE + row;
-        float top = -INFINITY;
-        for (int i = 0; i < wk.n_pieces; ++i) top = fmaxf(top, p.part_ml[(at + i * step) * 2]);
-        const float off = top == -INFINITY ? 0.f : top;
-        float sum = 0.f;
-        f32x4 u = {0.f, 0.f, 0.f, 0.f};
-        for (int i = 0; i < wk.n_pieces; ++i) {
-            const float f = __builtin_amdgcn_exp2f(p.part_ml[(at + i * step) * 2] - off);
-            sum += p.part_ml[(at + i * step) * 2 + 1] * f;
-            u += *(const f32x4 *)(p.part_u + (at + i * step) * p.d + c) * f;
-        }
-        const int t = r / p.rep, h = g * p.rep + r - t * p.rep;
-        const int64_t out = (int64_t)(wk.first_row + t) * p.o_stride + (int64_t)h * p.d + c;
-        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-        u *= inv;
-        if (sizeof(T) == 4 || p.o_f32) *(f32x4 *)((float *)p.o + out) = u;
-        else *(bf16x4 *)((bf16_t *)p.o + out) = bf16x4{(bf16_t)u[0], (bf16_t)u[1], (bf16_t)u[2], (bf16_t)u[3]};
-        if (c == 0 && p.lse) p.lse[(int64_t)h * p.rows + wk.first_row + t] = (top + __builtin_log2f(sum)) * LN2F;
-    }
-}
-
 template <typename T, int DM, int RB>
 int32_t launch_rows(PagedAttnParams p, float *workspace, hipStream_t s) {
     constexpr int TILE = 16 * RB;
@@ -444,6 +412,9 @@ int32_t launch_type(const PagedAttnParams &p, float *workspace, hipStream_t s) {
     return p.d <= 64 ? launch_dim<T, 64>(p, workspace, s) : p.d <= 128 ? launch_dim<T, 128>(p, workspace, s) : launch_dim<T, 256>(p, workspace, s);
 }
 
+// bf16, head dimensions of 64 and 128: paged_attn_tile.hip takes the sequences of many rows
+bool tiled(const cascade_paged_cache *c) { return c->dtype == CASCADE_BF16 && (c->head_dim == 64 || c->head_dim == 128); }
+
 int32_t check_attn(const cascade_paged_cache *c, const cascade_paged_attn_desc *d) {
     const int32_t st = check_paged_cache(c);
     if (st != CASCADE_OK) return st;
@@ -468,6 +439,11 @@ extern "C" size_t cascade_paged_attn_workspace_bytes(const cascade_paged_cache *
     size_t most = 0;
     for (int tile : {16, 32}) {
         const size_t floats = (size_t)paged_grid(p, tile).parts * cache->n_kv_heads * tile * (cache->head_dim + 2);
+        most = floats > most ? floats : most;
+    }
+    if (tiled(cache) && (int64_t)p.rows * p.rep > PAGED_FEW) {
+        p.target = max(1, PAGED_TILE_TARGET / cache->n_kv_heads);
+        const size_t floats = (size_t)paged_grid(p, PAGED_TILE).parts * cache->n_kv_heads * PAGED_TILE * (cache->head_dim + 2);
         most = floats > most ? floats : most;
     }
     return align_up(most * sizeof(float), 256);
@@ -496,6 +472,18 @@ extern "C" int32_t cascade_paged_attn(const cascade_paged_cache *cache, int32_t 
     p.scale_log2 = desc->scale * 1.4426950408889634f;
     p.o_f32 = desc->o_dtype == CASCADE_F32;
     p.above = 0; p.upto = INT32_MAX;
+    if (tiled(cache)) {
+        // sequences of many rows, if the rows at hand can make one; then those of few, if there can be any (the launches follow
+        // one another and may share the workspace)
+        if ((int64_t)p.rows * p.rep > PAGED_FEW) {
+            PagedAttnParams many = p;
+            many.above = p.B == 1 ? 0 : PAGED_FEW;          // (a single one goes there with however many it has)
+            const int32_t st = launch_paged_tile(many, (float *)workspace, (hipStream_t)stream);
+            if (st != CASCADE_OK) return st;
+            if (p.B == 1) return CASCADE_OK;
+        }
+        p.upto = PAGED_FEW;
+    }
     return cache->dtype == CASCADE_BF16 ? launch_type<bf16_t>(p, (float *)workspace, (hipStream_t)stream)
                                         : launch_type<float>(p, (float *)workspace, (hipStream_t)stream);
 }
