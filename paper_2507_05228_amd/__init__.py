@@ -210,8 +210,9 @@ def _ptr(t):
 
 def _stream(stream):
     import torch
-    s = torch.cuda.current_stream() if stream is None else stream
-    return C.c_void_p(s.cuda_stream)
+    if stream is None:                                     # the handle itself: 0.3 us instead of 3 for a stream object
+        return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+    return C.c_void_p(stream.cuda_stream)
 
 
 def _dtype_code(t):
@@ -578,9 +579,11 @@ def make_rope_desc(rot_dim, theta, layout=ROPE_HALF, scaling=ROPE_UNSCALED, fact
 
 def _head_rows(t, where):
     """Row stride of a [rows, heads, d] tensor whose heads lie back to back."""
-    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
-        raise CascadeError(ESHAPE, f"{where}: [rows, heads, d] with dense heads")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    if t.dim() == 3:
+        (rows, heads, d), (sr, sh, sd) = t.shape, t.stride()
+        if sd == 1 and (heads < 2 or sh == d):
+            return sr if rows > 1 else heads * d
+    raise CascadeError(ESHAPE, f"{where}: [rows, heads, d] with dense heads")
 
 
 def _checked(where, dtype, **tensors):

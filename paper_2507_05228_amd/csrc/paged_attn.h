@@ -11,23 +11,27 @@
 #include "device_utils.h"
 #include "paged.h"
 
+struct PagedSet {                                          // the sequences of one kernel
+    int32_t above, upto;                                   // those of more than `above` and at most `upto` flattened rows
+    int32_t min_steps, target;
+    float inv_target;
+    int32_t max_parts;                                     // partials that the workspace holds, per kv head
+    float *part_u, *part_ml;                               // [piece][kv head][tile_rows][d]; [piece][kv head][tile_rows][2]: m (log2 units), l
+};
 struct PagedAttnParams {
     const void *q, *k_pages, *v_pages;                     // the layer's pools
     void *o;
     float *lse;
     const int32_t *q_start, *visible, *table, *len;
-    float *part_u, *part_ml;                               // [piece][kv head][tile_rows][d]; [piece][kv head][tile_rows][2]: m (log2 units), l
     int64_t q_stride, o_stride;
     int32_t rows, H, Hkv, rep, d, S, B, max_pages, page_shift, n_pages;
     float scale_log2;
     int32_t o_f32;
-    int32_t above, upto;                                   // sequences of more than `above` and at most `upto` flattened rows
-    int32_t min_steps, target;
-    int32_t max_parts;                                     // partials that the workspace holds, per kv head
+    PagedSet few, many;                                    // paged_attn_rows.hip, paged_attn_tile.hip
 };
 
-constexpr int PAGED_TARGET = 1024;                         // pieces of a launch, all kv heads together
-constexpr int PAGED_TILE = 256, PAGED_TILE_TARGET = 256;   // paged_attn_tile.hip: rows of a tile; pieces
+constexpr int PAGED_FEW_TARGET = 512;                      // pieces of a launch, all kv heads together
+constexpr int PAGED_TILE = 256, PAGED_TILE_KEYS = 64, PAGED_TILE_TARGET = 256;      // paged_attn_tile.hip: rows of a tile, keys of a step; pieces
 constexpr int PAGED_FEW = 32;                              // flattened rows of a sequence up to which it goes to paged_attn_rows.hip
 
 struct PagedWork {
@@ -37,13 +41,18 @@ struct PagedWork {
     int k0, k1;                                            // steps of this piece
 };
 
-template <typename T> __device__ __forceinline__ T wave_inclusive(T v) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const T t = __shfl_up(v, o, WAVE);
-        if ((int)(threadIdx.x & 63) >= o) v += t;
-    }
-    return v;
+// Sum over the lanes up to this one.  Inside rows of 16 lanes by shifts, then the last lane of a row is handed to the rows
+// behind it: data-parallel-primitive moves, no LDS traffic.
+template <int CTRL, int ROWS> __device__ __forceinline__ int dpp_or_zero(int v) {
+    return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int wave_inclusive(int v) {
+    v += dpp_or_zero<0x111, 0xf>(v);                       // row_shr 1, 2, 4, 8
+    v += dpp_or_zero<0x112, 0xf>(v);
+    v += dpp_or_zero<0x114, 0xf>(v);
+    v += dpp_or_zero<0x118, 0xf>(v);
+    v += dpp_or_zero<0x142, 0xa>(v);                       // row_bcast 15 into rows 1 and 3
+    return v + dpp_or_zero<0x143, 0xc>(v);                 // row_bcast 31 into rows 2 and 3
 }
 
 // Keys of a list that count
@@ -51,9 +60,16 @@ __device__ __forceinline__ int paged_len(const PagedAttnParams &p, int64_t list)
     return min(max(p.len[list], 0), p.max_pages << p.page_shift);
 }
 
+// Part i of n nearly equal parts of [0, steps)
+__device__ __forceinline__ void paged_cut(int steps, int i, int n, int &k0, int &k1) {
+    const int each = n == 1 ? steps : (int)((uint32_t)steps / (uint32_t)n), more = n == 1 ? 0 : steps - each * n;
+    k0 = i * each + min(i, more);
+    k1 = k0 + each + (i < more);
+}
+
 // Piece number w of the launch (whole wavefronts call this, with the same w).  MERGE: tile number w among those with partials.
 template <int TILE, int KEYS, bool MERGE>
-__device__ __forceinline__ bool paged_find_work(const PagedAttnParams &p, int w, PagedWork &out) {
+__device__ __forceinline__ bool paged_find_work(const PagedAttnParams &p, const PagedSet &set, int w, PagedWork &out) {
     const int lane = threadIdx.x & 63;
     int tiles = 0, steps = 0, lo = 0, n = 0;
     auto load = [&](int b) {
@@ -61,23 +77,30 @@ __device__ __forceinline__ bool paged_find_work(const PagedAttnParams &p, int w,
         if (b >= p.B) return;
         lo = min(max(p.q_start[b], 0), p.rows);
         const int64_t flat = (int64_t)max(min(p.q_start[b + 1], p.rows) - lo, 0) * p.rep;
-        if (flat <= p.above || flat > p.upto) return;
+        if (flat <= set.above || flat > set.upto) return;
         n = (int)flat;
         tiles = (n + TILE - 1) / TILE;
-        for (int s = 0; s < p.S; ++s) steps += (paged_len(p, (int64_t)b * p.S + s) + KEYS - 1) / KEYS;
+        const int64_t list0 = (int64_t)b * p.S;
+        for (int s0 = 0; s0 < p.S; s0 += 8) {              // eight loads in flight
+            int n_s[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) n_s[i] = paged_len(p, list0 + min(s0 + i, p.S - 1));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) steps += s0 + i < p.S ? (n_s[i] + KEYS - 1) / KEYS : 0;
+        }
     };
-    unsigned long long total = 0;
+    // (in fp32: every workgroup forms the same sum in the same order; the margin keeps the number of pieces inside its bound)
+    float total = 0.f;
     for (int b0 = 0; b0 < p.B; b0 += 64) {
         load(b0 + lane);
-        total += (unsigned long long)tiles * steps;
+        total += (float)tiles * (float)steps;
     }
-#pragma unroll
-    for (int o = 32; o; o >>= 1) total += __shfl_xor(total, o, WAVE);
-    const int per_piece = (int)max((unsigned long long)p.min_steps, (total + p.target - 1) / p.target);
+    total = wave_sum(total);
+    const int per_piece = __builtin_amdgcn_readfirstlane(max(set.min_steps, (int)fminf(total * set.inv_target * 1.0001f + 1.f, 1e9f)));
     int before = 0, parts_before = 0;
     for (int b0 = 0; b0 < p.B; b0 += 64) {
         if (p.B > 64) load(b0 + lane);                     // (else they are those of the loop above)
-        const int pieces = max(1, (int)(((int64_t)steps + per_piece - 1) / per_piece));
+        const int pieces = steps <= per_piece ? 1 : (int)(((uint32_t)steps + (uint32_t)per_piece - 1) / (uint32_t)per_piece);
         const int parts = pieces > 1 ? tiles * pieces : 0;
         const int items = MERGE ? (pieces > 1 ? tiles : 0) : tiles * pieces;
         const int incl = wave_inclusive(items), parts_incl = wave_inclusive(parts);
@@ -88,7 +111,7 @@ __device__ __forceinline__ bool paged_find_work(const PagedAttnParams &p, int w,
             const int i = w - before - of(incl - items);
             out.n_pieces = of(pieces);
             // late tiles first: with a causal limit they are the long ones
-            const int tile = MERGE ? i : i / out.n_pieces;
+            const int tile = MERGE || out.n_pieces == 1 ? i : (int)((uint32_t)i / (uint32_t)out.n_pieces);
             out.b = b0 + at;
             out.first_row = of(lo);
             out.n_rows = of(n);
@@ -96,10 +119,9 @@ __device__ __forceinline__ bool paged_find_work(const PagedAttnParams &p, int w,
             out.piece = MERGE ? 0 : i - tile * out.n_pieces;
             out.first_piece = parts_before + of(parts_incl - parts) + tile * out.n_pieces;
             out.tile = of(tiles) - 1 - tile;
-            out.k0 = (int)((int64_t)out.steps * out.piece / out.n_pieces);
-            out.k1 = (int)((int64_t)out.steps * (out.piece + 1) / out.n_pieces);
+            paged_cut(out.steps, out.piece, out.n_pieces, out.k0, out.k1);
             // (more partials than the launch has room for: only where sequences overlap, which they must not)
-            return out.n_pieces == 1 || out.first_piece + out.n_pieces <= p.max_parts;
+            return out.n_pieces == 1 || out.first_piece + out.n_pieces <= set.max_parts;
         }
         before += __builtin_amdgcn_readlane(incl, 63);
         parts_before += __builtin_amdgcn_readlane(parts_incl, 63);
@@ -107,49 +129,21 @@ __device__ __forceinline__ bool paged_find_work(const PagedAttnParams &p, int w,
     return false;
 }
 
-// What a launch of tiles of `tile` rows may need: workgroups per kv head, and tiles with partials and partials among them
+// What a set of tiles of `tile` rows may need: workgroups per kv head, and tiles with partials and partials among them
 struct PagedGrid { int64_t pieces, split_tiles, parts; };
-static inline PagedGrid paged_grid(const PagedAttnParams &p, int tile) {
-    const int64_t tiles = (int64_t)p.rows * p.rep / tile + (p.B < p.rows ? p.B : p.rows);
+static inline PagedGrid paged_grid(const PagedAttnParams &p, const PagedSet &set, int tile) {
+    const int64_t flat = (int64_t)p.rows * p.rep, seqs = flat / (set.above + 1);
+    const int64_t tiles = flat / tile + (p.B < seqs ? p.B : seqs);
     PagedGrid g;
-    g.pieces = tiles + p.target;                           // sum of ceil(steps / per_piece) <= tiles + sum of steps / per_piece
-    g.split_tiles = tiles < p.target ? tiles : p.target;   // a cut walk is longer than per_piece
-    g.parts = g.pieces < 2 * p.target ? g.pieces : 2 * (int64_t)p.target;      // ceil(x) < 2 x above 1
+    g.pieces = tiles + set.target;                         // sum of ceil(steps / per_piece) <= tiles + sum of steps / per_piece
+    g.split_tiles = tiles < set.target ? tiles : set.target;       // a cut walk is longer than per_piece
+    g.parts = g.pieces < 2 * set.target ? g.pieces : 2 * (int64_t)set.target;     // ceil(x) < 2 x above 1
     return g;
 }
-
-int32_t launch_paged_tile(PagedAttnParams p, float *workspace, hipStream_t s);
-
-constexpr float LN2F = 0.6931471805599453f;
-
-// Tiles whose walk was cut: their partials, weighted by exp2(m - largest m)
-template <typename T, int TILE, int KEYS>
-__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnParams p) {
-    PagedWork wk;
-    if (!paged_find_work<TILE, KEYS, true>(p, blockIdx.x, wk)) return;
-    const int g = blockIdx.y, per_row = p.d / 4;
-    const int64_t step = (int64_t)p.Hkv * TILE;
-    for (int e = threadIdx.x + 256 * blockIdx.z; e < TILE * per_row; e += 256 * gridDim.z) {
-        const int row = e / per_row, c = (e - row * per_row) * 4, r = wk.tile * TILE + row;
-        if (r >= wk.n_rows) break;
-        const int64_t at = ((int64_t)wk.first_piece * p.Hkv + g) * TILE + row;
-        float top = -INFINITY;
-        for (int i = 0; i < wk.n_pieces; ++i) top = fmaxf(top, p.part_ml[(at + i * step) * 2]);
-        const float off = top == -INFINITY ? 0.f : top;
-        float sum = 0.f;
-        f32x4 u = {0.f, 0.f, 0.f, 0.f};
-        for (int i = 0; i < wk.n_pieces; ++i) {
-            const float f = __builtin_amdgcn_exp2f(p.part_ml[(at + i * step) * 2] - off);
-            sum += p.part_ml[(at + i * step) * 2 + 1] * f;
-            u += *(const f32x4 *)(p.part_u + (at + i * step) * p.d + c) * f;
-        }
-        const int t = r / p.rep, h = g * p.rep + r - t * p.rep;
-        const int64_t out = (int64_t)(wk.first_row + t) * p.o_stride + (int64_t)h * p.d + c;
-        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-        u *= inv;
-        if (sizeof(T) == 4 || p.o_f32) *(f32x4 *)((float *)p.o + out) = u;
-        else *(bf16x4 *)((bf16_t *)p.o + out) = bf16x4{(bf16_t)u[0], (bf16_t)u[1], (bf16_t)u[2], (bf16_t)u[3]};
-        if (c == 0 && p.lse) p.lse[(int64_t)h * p.rows + wk.first_row + t] = (top + __builtin_log2f(sum)) * LN2F;
-    }
+static inline size_t paged_part_floats(const PagedAttnParams &p, const PagedSet &set, int tile) {
+    return (size_t)paged_grid(p, set, tile).parts * p.Hkv * tile * (p.d + 2);
 }
 
+int32_t launch_paged_tile(const PagedAttnParams &p, hipStream_t s);
+
+constexpr float LN2F = 0.6931471805599453f;

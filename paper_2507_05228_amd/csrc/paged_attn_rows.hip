@@ -54,23 +54,28 @@ __device__ __forceinline__ bool word_not_finite(float x, bool is_bf16_pair) {
     return is_bf16_pair ? (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u : (w & 0x7f800000u) == 0x7f800000u;
 }
 
+// Wavefronts per SIMD that the registers allow: keys and values of a step, queries and accumulators, and some 70 more
+constexpr int rows_occupancy(int size, int DM, int RB) {
+    const int regs = DM / 4 * size + (DM / 16 * size + DM / 4) * RB + 70;
+    return regs <= 168 ? 3 : regs <= 256 ? 2 : 1;
+}
+
 template <typename T, int DM, int RB>
-__global__ __launch_bounds__(256) void paged_rows_kernel(PagedAttnParams p) {
+__global__ __launch_bounds__(256, rows_occupancy(sizeof(T), DM, RB)) void paged_rows_kernel(PagedAttnParams p) {
     typedef typename Kind<T>::frag frag;
     constexpr bool BF = sizeof(T) == 2;
     constexpr int KD = Kind<T>::KD, KS = DM / KD, TILE = 16 * RB, KEYS = 32;
     constexpr int VW = DM / 16 * sizeof(T) / 4;            // 32-bit words of a V row in a lane
     constexpr int RUN = BF ? (DM / 16 < 8 ? DM / 16 : 8) : 4;      // neighbouring columns in a lane
     constexpr int NB = DM / 16;                            // products of 16 columns
-    constexpr int BUFS = (BF ? DM : 2 * DM) <= 256 ? 2 : 1;        // steps loaded ahead, where registers allow
-    typedef __attribute__((ext_vector_type(RUN * sizeof(T) / 4))) uint32_t vload;
+    constexpr int RW = RUN * sizeof(T) / 4;
 
     extern __shared__ __attribute__((aligned(16))) float smem[];   // [4][TILE][DM] u, then [4][TILE][2]; before that the shards' steps
     const int lane = threadIdx.x & 63, c16 = lane & 15, g4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = blockIdx.y;
     PagedWork wk;
-    if (!paged_find_work<TILE, KEYS, false>(p, blockIdx.x, wk)) return;
+    if (!paged_find_work<TILE, KEYS, false>(p, p.few, blockIdx.x, wk)) return;
 
     // first step of every shard, and its length (several shards only)
     int32_t *cum = (int32_t *)smem, *lens = cum + p.S + 1;
@@ -95,7 +100,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedAttnParams p) {
     int token[RB];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        const int r = min(wk.tile * TILE + rb * 16 + c16, wk.n_rows - 1), t = r / p.rep;
+        const int r = min(wk.tile * TILE + rb * 16 + c16, wk.n_rows - 1), t = (int)((uint32_t)r / (uint32_t)p.rep);
         token[rb] = wk.first_row + t;
         const T *src = qp + (int64_t)token[rb] * p.q_stride + (int64_t)(g * p.rep + r - t * p.rep) * p.d;
 #pragma unroll
@@ -117,75 +122,86 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedAttnParams p) {
     }
 
     struct Step {
-        frag k[2][KS];
-        float v[8][VW];                                    // rows 4 g4 + j of the first, then of the second 16 keys
         int seen[RB];                                      // keys of the step that a row sees
-        int64_t page[2];                                   // offset of the 16 keys' first row in the pools
+        int j0, shard, bad;                                // first key; bit kb: 16 keys whose list entry is no page
     };
-    Step st[BUFS];
+    frag kf[2][KS];                                        // keys of a step; refilled as soon as its scores are formed
+    float vf[8][VW];                                       // values, rows 4 g4 + j of the first, then of the second 16 keys; refilled behind the output product
 
+    // Where step k lies: read a step before its loads are requested
+    struct Place { int j0, shard, len, id[2]; };
     int shard = 0;
     const int only_len = p.S > 1 ? 0 : __builtin_amdgcn_readfirstlane(paged_len(p, list0));
-    auto load = [&](int k, Step &x) {
-        int j0 = k * KEYS, len;
+    auto locate = [&](int k) {
+        Place x;
+        int j0 = k * KEYS, len = only_len;
         if (p.S > 1) {
             while (k >= cum[shard + 1]) ++shard;           // (ends: k is below cum[S])
             j0 = (k - cum[shard]) * KEYS;
             len = lens[shard];
-        } else len = only_len;
-        j0 = __builtin_amdgcn_readfirstlane(j0);
-        len = __builtin_amdgcn_readfirstlane(len);
-        const int s = __builtin_amdgcn_readfirstlane(shard);
-        const int32_t *ids = p.table + (list0 + s) * p.max_pages;
-        // the second 16 keys may begin behind the end: then the first ones stand in (and are not seen)
-        int bad = 0;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const int j = j0 + (kb == 1 && j0 + 16 < len ? 16 : 0);
-            int id = ids[j >> p.page_shift];
-            if ((uint32_t)id >= (uint32_t)p.n_pages) { bad |= 1 << kb; id = 0; }
-            x.page[kb] = ((((int64_t)id * p.Hkv + g) << p.page_shift) + (j & ((1 << p.page_shift) - 1))) * p.d;
         }
-        const int rows = len - j0;                         // keys of the step that exist: at least 1
+        x.j0 = __builtin_amdgcn_readfirstlane(j0);
+        x.len = __builtin_amdgcn_readfirstlane(len);
+        x.shard = __builtin_amdgcn_readfirstlane(shard);
+        const int32_t *ids = p.table + (list0 + x.shard) * p.max_pages;
+        x.id[0] = ids[x.j0 >> p.page_shift];
+        x.id[1] = ids[min(x.j0 + 16, x.len - 1) >> p.page_shift];      // (a second 16 that does not exist: any entry that does)
+        return x;
+    };
+    const uint32_t row_bytes = p.d * sizeof(T);
+    const uint32_t k_off = c16 * row_bytes + g4 * 16, v_off = 4 * g4 * row_bytes + c16 * (RUN * sizeof(T));
+    // (columns behind the head: outside every descriptor, which returns zeros)
+    const auto k_at = [&](int ks) { return ks * KD + g4 * (KD / 4) < p.d ? k_off + ks * 64 : 0x40000000u; };
+    // The rows of 16 keys that exist: what lies behind them is outside the descriptor and arrives as zeros
+    auto rows_of = [&](const void *pages, const Place &at, int kb) {
+        const bool page = (uint32_t)at.id[kb] < (uint32_t)p.n_pages;
+        const int exist = page ? min(max(at.len - at.j0 - 16 * kb, 0), 16) : 0;
+        const int64_t first = exist ? ((((int64_t)at.id[kb] * p.Hkv + g) << p.page_shift) + ((at.j0 + 16 * kb) & ((1 << p.page_shift) - 1))) * p.d : 0;
+        return __builtin_amdgcn_make_buffer_rsrc((T *)pages + first, 0, exist * row_bytes, 0x00020000);
+    };
+    auto load_keys = [&](const Place &at, Step &x) {
+        const int rows = at.len - at.j0;                   // keys of the step that exist: at least 1
+        x.j0 = at.j0;
+        x.shard = at.shard;
+        x.bad = ((uint32_t)at.id[0] >= (uint32_t)p.n_pages) | ((uint32_t)at.id[1] >= (uint32_t)p.n_pages && rows > 16) << 1;
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
             int n = rows;
-            if (p.visible) n = min(n, p.visible[(int64_t)token[rb] * p.S + s] - j0);
-            // keys of a list entry that is no page do not exist: bit 30 for the first 16, 31 for the second
-            x.seen[rb] = (min(max(n, 0), KEYS)) | bad << 30;
+            if (p.visible) n = min(n, p.visible[(int64_t)token[rb] * p.S + at.shard] - at.j0);
+            x.seen[rb] = min(max(n, 0), KEYS);
         }
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-            const int exist = min(rows - 16 * kb, 16) < 1 ? 16 : min(rows - 16 * kb, 16);    // (stand-in: the first 16, all there)
-            const T *kr = (const T *)p.k_pages + x.page[kb] + (int64_t)min(c16, exist - 1) * p.d;
+            const __amdgpu_buffer_rsrc_t r = rows_of(p.k_pages, at, kb);
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const int c = ks * KD + g4 * (KD / 4);
-                x.k[kb][ks] = *(const frag *)(kr + (c < p.d ? c : 0));
-            }
+            for (int ks = 0; ks < KS; ++ks)
+                kf[kb][ks] = __builtin_bit_cast(frag, __builtin_amdgcn_raw_buffer_load_b128(r, p.d == DM ? k_off + ks * 64 : k_at(ks), 0, 0));
+        }
+    };
+    auto load_values = [&](const Place &at) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const T *vr = (const T *)p.v_pages + x.page[kb] + (int64_t)min(4 * g4 + j, exist - 1) * p.d;
+        for (int kb = 0; kb < 2; ++kb) {
+            const __amdgpu_buffer_rsrc_t r = rows_of(p.v_pages, at, kb);
 #pragma unroll
-                for (int h = 0; h < VW * 4 / (int)(RUN * sizeof(T)); ++h) {
-                    const int c = h * 16 * RUN + RUN * c16;
-                    const vload t = *(const vload *)(vr + (c < p.d ? c : 0));
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-                    for (int w = 0; w < (int)(RUN * sizeof(T) / 4); ++w)
-                        x.v[kb * 4 + j][h * (RUN * sizeof(T) / 4) + w] = __builtin_bit_cast(float, (uint32_t)t[w]);
+                for (int h = 0; h < VW / RW; ++h) {
+                    const uint32_t off = v_off + j * row_bytes + h * 16 * (RUN * sizeof(T));
+                    if constexpr (RW == 4) {
+                        const u32x4 t = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) vf[kb * 4 + j][h * 4 + w] = __uint_as_float(t[w]);
+                    } else {
+                        const u32x2 t = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0));
+                        vf[kb * 4 + j][0] = __uint_as_float(t[0]);
+                        vf[kb * 4 + j][1] = __uint_as_float(t[1]);
+                    }
                 }
-            }
         }
     };
 
-    auto step = [&](Step &x) {
-        if (p.d < DM) {                                    // columns behind the head: zero on both sides
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks)
-                    if (ks * KD + g4 * (KD / 4) >= p.d) x.k[kb][ks] = frag{};
-        }
+    // One step: scores, then the request of the next keys; exponentials and output product, then that of the next values
+    auto step = [&](Step &x, const Place &next) {
         f32x4 s[RB][2];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb)
@@ -193,16 +209,14 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedAttnParams p) {
             for (int kb = 0; kb < 2; ++kb) {
                 s[rb][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) s[rb][kb] = score_mfma(x.k[kb][ks], Q[rb][ks], s[rb][kb]);
+                for (int ks = 0; ks < KS; ++ks) s[rb][kb] = score_mfma(kf[kb][ks], Q[rb][ks], s[rb][kb]);
             }
+        Step ahead;
+        load_keys(next, ahead);
         bool masked = false;
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) masked |= x.seen[rb] != KEYS;
-        masked = __any(masked);
-        auto sees = [&](int rb, int kb, int r) {
-            const int seen = x.seen[rb];
-            return 16 * kb + 4 * g4 + r < (seen & 63) && !((uint32_t)seen >> (30 + kb) & 1);
-        };
+        masked = __any(masked) || x.bad;
         if (masked) {
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb)
@@ -210,7 +224,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedAttnParams p) {
                 for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        if (!sees(rb, kb, r)) s[rb][kb][r] = -INFINITY;
+                        if (16 * kb + 4 * g4 + r >= x.seen[rb] || (x.bad >> kb & 1)) s[rb][kb][r] = -INFINITY;
         }
         bool raise = false;
         float top[RB];
@@ -248,18 +262,18 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedAttnParams p) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
-                for (int w = 0; w < VW; ++w) odd |= word_not_finite(x.v[j][w], BF);
+                for (int w = 0; w < VW; ++w) odd |= word_not_finite(vf[j][w], BF);
             if (__any(odd)) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
 #pragma unroll
                     for (int w = 0; w < VW; ++w) {
-                        uint32_t u = __builtin_bit_cast(uint32_t, x.v[j][w]);
+                        uint32_t u = __builtin_bit_cast(uint32_t, vf[j][w]);
                         if (BF) {
                             if ((u & 0x7f80u) == 0x7f80u) u &= 0xffff0000u;
                             if ((u & 0x7f800000u) == 0x7f800000u) u &= 0xffffu;
                         } else if ((u & 0x7f800000u) == 0x7f800000u) u = 0;
-                        x.v[j][w] = __builtin_bit_cast(float, u);
+                        vf[j][w] = __builtin_bit_cast(float, u);
                     }
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb)
@@ -270,16 +284,19 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedAttnParams p) {
                         for (int i = 1; i < 8; ++i)
                             if ((key >> 4) * 4 + (key & 3) == i) w = s[rb][i / 4][i % 4];
                         w = __shfl(w, (key >> 2 & 3) * 16 + c16, WAVE);
-                        if (key >= (x.seen[rb] & 63) || ((uint32_t)x.seen[rb] >> (30 + (key >> 4)) & 1)) continue;
-                        const T *vr = (const T *)p.v_pages + (key < 16 ? x.page[0] : x.page[1]) + (int64_t)(key & 15) * p.d;
+                        if (key >= x.seen[rb] || (x.bad >> (key >> 4) & 1)) continue;
+                        const int j = x.j0 + key, id = p.table[(list0 + x.shard) * p.max_pages + (j >> p.page_shift)];
+                        const T *vr = (const T *)p.v_pages + ((((int64_t)id * p.Hkv + g) << p.page_shift) + (j & ((1 << p.page_shift) - 1))) * p.d;
 #pragma unroll
-                        for (int i = 0; i < NB; ++i)
+                        for (int i = 0; i < NB; ++i) {
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {
                                 const int c = i / RUN * 16 * RUN + RUN * (4 * g4 + r) + i % RUN;
                                 const float v = (float)vr[c < p.d ? c : 0];
                                 if (word_not_finite(v, false)) O[rb][i][r] += w * v;
                             }
+                            __builtin_amdgcn_sched_barrier(0);     // (rare: few registers matter more than its time)
+                        }
                     }
             }
         }
@@ -294,7 +311,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedAttnParams p) {
                 u32x4 even, odd;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const uint32_t a = __builtin_bit_cast(uint32_t, x.v[2 * j][w]), b = __builtin_bit_cast(uint32_t, x.v[2 * j + 1][w]);
+                    const uint32_t a = __builtin_bit_cast(uint32_t, vf[2 * j][w]), b = __builtin_bit_cast(uint32_t, vf[2 * j + 1][w]);
                     even[j] = __builtin_amdgcn_perm(b, a, 0x05040100);
                     odd[j] = __builtin_amdgcn_perm(b, a, 0x07060302);
                 }
@@ -311,27 +328,27 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedAttnParams p) {
                 for (int i = 0; i < NB; ++i)
 #pragma unroll
                     for (int rb = 0; rb < RB; ++rb)
-                        O[rb][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(x.v[j][i], s[rb][j / 4][j % 4], O[rb][i], 0, 0, 0);
+                        O[rb][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[j][i], s[rb][j / 4][j % 4], O[rb][i], 0, 0, 0);
         }
+        load_values(next);
+        x = ahead;
     };
 
     // this wavefront's quarter of the piece
-    const int n = wk.k1 - wk.k0, a = wk.k0 + (int)((int64_t)n * wave / 4), b = wk.k0 + (int)((int64_t)n * (wave + 1) / 4);
+    int a, b;
+    paged_cut(wk.k1 - wk.k0, wave, 4, a, b);
+    a += wk.k0;
+    b += wk.k0;
     if (a < b) {
-        if constexpr (BUFS == 2) {
-            load(a, st[0]);
-            // the request ahead is not conditional (behind the end it repeats the last step): with a branch around it the
-            // compiler cannot count the loads in flight and waits for all of them
-            for (int k = a;; k += 2) {
-                load(min(k + 1, b - 1), st[1]);
-                step(st[0]);
-                if (k + 1 >= b) break;
-                load(min(k + 2, b - 1), st[0]);
-                step(st[1]);
-                if (k + 2 >= b) break;
-            }
-        } else {
-            for (int k = a; k < b; ++k) { load(k, st[0]); step(st[0]); }
+        // (the requests ahead are not conditional, behind the end they repeat the last step: with a branch around them the compiler
+        // cannot count the loads in flight and waits for all of them)
+        Step x;
+        Place at = locate(a);
+        load_keys(at, x);
+        load_values(at);
+        for (int k = a; k < b; ++k) {
+            at = locate(min(k + 1, b - 1));
+            step(x, at);
         }
     }
 
@@ -352,10 +369,9 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedAttnParams p) {
             for (int r = 0; r < 4; ++r) u[i / RUN * 16 * RUN + RUN * (4 * g4 + r) + i % RUN] = O[rb][i][r];
     }
     __syncthreads();
-    const int per_row = p.d / 4;
-    for (int e = threadIdx.x; e < TILE * per_row; e += 256) {
-        const int row = e / per_row, c = (e - row * per_row) * 4, r = wk.tile * TILE + row;
-        if (r >= wk.n_rows) break;
+    for (int e = threadIdx.x; e < TILE * (DM / 4); e += 256) {
+        const int row = e / (DM / 4), c = e % (DM / 4) * 4, r = wk.tile * TILE + row;
+        if (r >= wk.n_rows || c >= p.d) continue;
         float top = -INFINITY;
 #pragma unroll
         for (int w = 0; w < 4; ++w) top = fmaxf(top, sm[(w * TILE + row) * 2]);
@@ -370,11 +386,11 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedAttnParams p) {
         }
         if (wk.n_pieces > 1) {
             const int64_t at = ((int64_t)(wk.first_piece + wk.piece) * p.Hkv + g) * TILE + row;
-            *(f32x4 *)(p.part_u + at * p.d + c) = u;
-            if (c == 0) { p.part_ml[at * 2] = top; p.part_ml[at * 2 + 1] = sum; }
+            *(f32x4 *)(p.few.part_u + at * p.d + c) = u;
+            if (c == 0) { p.few.part_ml[at * 2] = top; p.few.part_ml[at * 2 + 1] = sum; }
             continue;
         }
-        const int t = r / p.rep, h = g * p.rep + r - t * p.rep;
+        const int t = (int)((uint32_t)r / (uint32_t)p.rep), h = g * p.rep + r - t * p.rep;
         const int64_t out = (int64_t)(wk.first_row + t) * p.o_stride + (int64_t)h * p.d + c;
         const float inv = sum == 0.f ? 0.f : 1.0f / sum;
         u *= inv;
@@ -384,36 +400,127 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedAttnParams p) {
     }
 }
 
+// Tiles whose walk was cut, of either kernel: their partials, weighted by exp2(m - largest m).  DM / 4 lanes to a row (a power of
+// two); the lanes of a row share the search for the largest m, then every thread adds its four columns, eight partials requested
+// at a time.
+template <typename T, int TILE, int KEYS, int DM>
+__device__ __forceinline__ void merge_tile(const PagedAttnParams &p, const PagedSet &set, int w) {
+    constexpr int LPR = DM / 4;
+    PagedWork wk;
+    if (!paged_find_work<TILE, KEYS, true>(p, set, w, wk)) return;
+    const int g = blockIdx.y;
+    const int64_t step = (int64_t)p.Hkv * TILE;
+    for (int e = threadIdx.x + 256 * blockIdx.z; e < TILE * LPR; e += 256 * gridDim.z) {
+        const int row = e / LPR, sub = e % LPR, c = sub * 4, r = wk.tile * TILE + row;
+        if (r >= wk.n_rows) return;                        // (all lanes of the row)
+        const int64_t at = ((int64_t)wk.first_piece * p.Hkv + g) * TILE + row;
+        const float2 *ml = (const float2 *)set.part_ml + at;
+        float top = -INFINITY;
+        for (int i = sub; i < wk.n_pieces; i += LPR) top = fmaxf(top, ml[i * step].x);
+#pragma unroll
+        for (int o = 1; o < LPR; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, WAVE));
+        const float off = top == -INFINITY ? 0.f : top;
+        float sum = 0.f;
+        f32x4 u = {0.f, 0.f, 0.f, 0.f};
+        const float *pu = set.part_u + at * p.d + (c < p.d ? c : 0);
+        for (int i0 = 0; i0 < wk.n_pieces; i0 += 8) {
+            float2 w[8];
+            f32x4 x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int64_t i = min(i0 + j, wk.n_pieces - 1) * step;
+                w[j] = ml[i];
+                x[j] = *(const f32x4 *)(pu + i * p.d);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (i0 + j >= wk.n_pieces) break;
+                const float f = __builtin_amdgcn_exp2f(w[j].x - off);
+                sum += w[j].y * f;
+                u += x[j] * f;
+            }
+        }
+        if (c >= p.d) continue;
+        const int t = (int)((uint32_t)r / (uint32_t)p.rep), h = g * p.rep + r - t * p.rep;
+        const int64_t out = (int64_t)(wk.first_row + t) * p.o_stride + (int64_t)h * p.d + c;
+        u *= sum == 0.f ? 0.f : 1.0f / sum;
+        if (sizeof(T) == 4 || p.o_f32) *(f32x4 *)((float *)p.o + out) = u;
+        else *(bf16x4 *)((bf16_t *)p.o + out) = bf16x4{(bf16_t)u[0], (bf16_t)u[1], (bf16_t)u[2], (bf16_t)u[3]};
+        if (c == 0 && p.lse) p.lse[(int64_t)h * p.rows + wk.first_row + t] = (top + __builtin_log2f(sum)) * LN2F;
+    }
+}
+template <typename T, int TILE, int DM>
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnParams p, int many_tiles) {
+    if constexpr (sizeof(T) == 2 && DM <= 128) {
+        if ((int)blockIdx.x < many_tiles) return merge_tile<T, PAGED_TILE, PAGED_TILE_KEYS, DM>(p, p.many, blockIdx.x);
+    }
+    merge_tile<T, TILE, 32, DM>(p, p.few, blockIdx.x - many_tiles);
+}
+
 template <typename T, int DM, int RB>
-int32_t launch_rows(PagedAttnParams p, float *workspace, hipStream_t s) {
+int32_t launch_rows(const PagedAttnParams &p, hipStream_t s) {
     constexpr int TILE = 16 * RB;
-    p.target = max(1, PAGED_TARGET / p.Hkv);
-    p.min_steps = 4;                                       // a step for each wavefront
-    const PagedGrid g = paged_grid(p, TILE);
-    p.max_parts = (int32_t)g.parts;
-    p.part_ml = workspace;
-    p.part_u = workspace + g.parts * p.Hkv * TILE * 2;
-    const int lds = max((int)sizeof(float) * 4 * TILE * (DM + 2), 4 * (2 * p.S + 1));
-    auto kern = paged_rows_kernel<T, DM, RB>;
-    static std::atomic<uint64_t> lds_ready{0};
-    CASCADE_HIP_TRY(ensure_dynamic_lds((const void *)kern, sizeof(float) * 4 * TILE * (DM + 2), lds_ready));
-    hipLaunchKernelGGL(kern, dim3((unsigned)g.pieces, p.Hkv), dim3(256), lds, s, p);
-    hipLaunchKernelGGL((paged_merge_kernel<T, TILE, 32>), dim3((unsigned)g.split_tiles, p.Hkv, RB), dim3(256), 0, s, p);
+    unsigned many_tiles = 0, few_tiles = 0;
+    if (p.many.target) {
+        const int32_t st = launch_paged_tile(p, s);
+        if (st != CASCADE_OK) return st;
+        many_tiles = (unsigned)paged_grid(p, p.many, PAGED_TILE).split_tiles;
+    }
+    if (p.few.target) {
+        const PagedGrid g = paged_grid(p, p.few, TILE);
+        const int lds = max((int)sizeof(float) * 4 * TILE * (DM + 2), 4 * (2 * p.S + 1));
+        auto kern = paged_rows_kernel<T, DM, RB>;
+        static std::atomic<uint64_t> lds_ready{0};
+        CASCADE_HIP_TRY(ensure_dynamic_lds((const void *)kern, sizeof(float) * 4 * TILE * (DM + 2), lds_ready));
+        hipLaunchKernelGGL(kern, dim3((unsigned)g.pieces, p.Hkv), dim3(256), lds, s, p);
+        few_tiles = (unsigned)g.split_tiles;
+    }
+    hipLaunchKernelGGL((paged_merge_kernel<T, TILE, DM>), dim3(many_tiles + few_tiles, p.Hkv, max(2, TILE * DM / 2048)), dim3(256), 0, s, p, (int)many_tiles);
     CASCADE_HIP_TRY(hipGetLastError());
     return CASCADE_OK;
 }
+// 32 rows a tile where sequences have more than 16 on average, else 16; heads of more than 128 have no registers for 32
+int rows_tile(const PagedAttnParams &p) { return (int64_t)p.rows * p.rep > (int64_t)16 * p.B && p.d <= 128 ? 32 : 16; }
 template <typename T, int DM>
-int32_t launch_dim(const PagedAttnParams &p, float *workspace, hipStream_t s) {
-    // 32 rows a tile where sequences have more than 16 on average, else 16
-    return (int64_t)p.rows * p.rep > (int64_t)16 * p.B ? launch_rows<T, DM, 2>(p, workspace, s) : launch_rows<T, DM, 1>(p, workspace, s);
+int32_t launch_dim(const PagedAttnParams &p, hipStream_t s) {
+    if constexpr (DM <= 128)
+        if (rows_tile(p) == 32) return launch_rows<T, DM, 2>(p, s);
+    return launch_rows<T, DM, 1>(p, s);
 }
 template <typename T>
-int32_t launch_type(const PagedAttnParams &p, float *workspace, hipStream_t s) {
-    return p.d <= 64 ? launch_dim<T, 64>(p, workspace, s) : p.d <= 128 ? launch_dim<T, 128>(p, workspace, s) : launch_dim<T, 256>(p, workspace, s);
+int32_t launch_type(const PagedAttnParams &p, hipStream_t s) {
+    return p.d <= 64 ? launch_dim<T, 64>(p, s) : p.d <= 128 ? launch_dim<T, 128>(p, s) : launch_dim<T, 256>(p, s);
 }
 
-// bf16, head dimensions of 64 and 128: paged_attn_tile.hip takes the sequences of many rows
-bool tiled(const cascade_paged_cache *c) { return c->dtype == CASCADE_BF16 && (c->head_dim == 64 || c->head_dim == 128); }
+// Sizes, and which sequences go to which kernel: bf16 with head dimensions of 64 and 128 has paged_attn_tile.hip for the
+// sequences of many rows, if the rows at hand can make one; with a single sequence it takes that with however many rows it has.
+void set_sizes(PagedAttnParams &p, const cascade_paged_cache *c, const cascade_paged_attn_desc *d) {
+    p.rows = d->rows; p.H = d->n_heads; p.Hkv = c->n_kv_heads; p.rep = p.H / p.Hkv; p.d = c->head_dim;
+    p.S = c->n_shards; p.B = c->n_seqs; p.max_pages = c->max_pages; p.page_shift = page_shift(c); p.n_pages = c->n_pages;
+    auto set = [&](PagedSet &x, int32_t above, int32_t upto, int target) {
+        x.above = above; x.upto = upto;
+        x.target = max(1, target / p.Hkv);
+        x.inv_target = 1.0f / x.target;
+        x.min_steps = 4;
+    };
+    const bool tiles = c->dtype == CASCADE_BF16 && (p.d == 64 || p.d == 128) && (int64_t)p.rows * p.rep > PAGED_FEW;
+    if (tiles) set(p.many, p.B == 1 ? 0 : PAGED_FEW, INT32_MAX, PAGED_TILE_TARGET);
+    if (!tiles || p.B > 1) set(p.few, 0, tiles ? PAGED_FEW : INT32_MAX, PAGED_FEW_TARGET);
+}
+size_t set_parts(PagedAttnParams &p, float *workspace) {
+    size_t floats = 0;
+    auto set = [&](PagedSet &x, int tile) {
+        if (!x.target) return;
+        const size_t parts = (size_t)paged_grid(p, x, tile).parts;
+        x.max_parts = (int32_t)parts;
+        x.part_u = workspace + floats;
+        x.part_ml = x.part_u + parts * p.Hkv * tile * p.d;
+        floats += align_up(parts * p.Hkv * tile * (p.d + 2), 4);
+    };
+    set(p.many, PAGED_TILE);
+    set(p.few, rows_tile(p));
+    return floats;
+}
 
 int32_t check_attn(const cascade_paged_cache *c, const cascade_paged_attn_desc *d) {
     const int32_t st = check_paged_cache(c);
@@ -434,19 +541,8 @@ int32_t check_attn(const cascade_paged_cache *c, const cascade_paged_attn_desc *
 extern "C" size_t cascade_paged_attn_workspace_bytes(const cascade_paged_cache *cache, const cascade_paged_attn_desc *desc) {
     if (check_attn(cache, desc) != CASCADE_OK) return 0;
     PagedAttnParams p = {};
-    p.rows = desc->rows; p.rep = desc->n_heads / cache->n_kv_heads; p.B = cache->n_seqs;
-    p.target = max(1, PAGED_TARGET / cache->n_kv_heads);
-    size_t most = 0;
-    for (int tile : {16, 32}) {
-        const size_t floats = (size_t)paged_grid(p, tile).parts * cache->n_kv_heads * tile * (cache->head_dim + 2);
-        most = floats > most ? floats : most;
-    }
-    if (tiled(cache) && (int64_t)p.rows * p.rep > PAGED_FEW) {
-        p.target = max(1, PAGED_TILE_TARGET / cache->n_kv_heads);
-        const size_t floats = (size_t)paged_grid(p, PAGED_TILE).parts * cache->n_kv_heads * PAGED_TILE * (cache->head_dim + 2);
-        most = floats > most ? floats : most;
-    }
-    return align_up(most * sizeof(float), 256);
+    set_sizes(p, cache, desc);
+    return align_up(set_parts(p, nullptr) * sizeof(float), 256);
 }
 
 extern "C" int32_t cascade_paged_attn(const cascade_paged_cache *cache, int32_t layer, const cascade_paged_attn_desc *desc,
@@ -467,23 +563,9 @@ extern "C" int32_t cascade_paged_attn(const cascade_paged_cache *cache, int32_t 
     p.q_start = q_start_dev; p.visible = visible_dev; p.table = cache->page_table; p.len = cache->kv_len;
     p.q_stride = desc->q_stride ? desc->q_stride : row;
     p.o_stride = desc->o_stride ? desc->o_stride : row;
-    p.rows = desc->rows; p.H = desc->n_heads; p.Hkv = cache->n_kv_heads; p.rep = p.H / p.Hkv; p.d = cache->head_dim;
-    p.S = cache->n_shards; p.B = cache->n_seqs; p.max_pages = cache->max_pages; p.page_shift = page_shift(cache); p.n_pages = cache->n_pages;
+    set_sizes(p, cache, desc);
+    set_parts(p, (float *)workspace);
     p.scale_log2 = desc->scale * 1.4426950408889634f;
     p.o_f32 = desc->o_dtype == CASCADE_F32;
-    p.above = 0; p.upto = INT32_MAX;
-    if (tiled(cache)) {
-        // sequences of many rows, if the rows at hand can make one; then those of few, if there can be any (the launches follow
-        // one another and may share the workspace)
-        if ((int64_t)p.rows * p.rep > PAGED_FEW) {
-            PagedAttnParams many = p;
-            many.above = p.B == 1 ? 0 : PAGED_FEW;          // (a single one goes there with however many it has)
-            const int32_t st = launch_paged_tile(many, (float *)workspace, (hipStream_t)stream);
-            if (st != CASCADE_OK) return st;
-            if (p.B == 1) return CASCADE_OK;
-        }
-        p.upto = PAGED_FEW;
-    }
-    return cache->dtype == CASCADE_BF16 ? launch_type<bf16_t>(p, (float *)workspace, (hipStream_t)stream)
-                                        : launch_type<float>(p, (float *)workspace, (hipStream_t)stream);
+    return cache->dtype == CASCADE_BF16 ? launch_type<bf16_t>(p, (hipStream_t)stream) : launch_type<float>(p, (hipStream_t)stream);
 }

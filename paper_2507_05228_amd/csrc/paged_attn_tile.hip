@@ -19,7 +19,7 @@
 namespace {
 
 constexpr float RAISE = 8.0f;
-constexpr int KEYS = 64;
+constexpr int KEYS = PAGED_TILE_KEYS;
 
 __device__ __forceinline__ f32x16 mfma32(const bf16x8 &a, const bf16x8 &b, const f32x16 &c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -57,7 +57,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g = blockIdx.y;
     PagedWork wk;
-    if (!paged_find_work<TILE, KEYS, false>(p, blockIdx.x, wk)) return;
+    if (!paged_find_work<TILE, KEYS, false>(p, p.many, blockIdx.x, wk)) return;
     const int64_t list0 = (int64_t)wk.b * p.S;
 
     // ---- keys of every shard that some row of the tile sees, and those that all of them see
@@ -93,7 +93,8 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
         __syncthreads();
     }
     const int steps = __builtin_amdgcn_readfirstlane(cum[p.S]);
-    const int k0 = (int)((int64_t)steps * wk.piece / wk.n_pieces), k1 = (int)((int64_t)steps * (wk.piece + 1) / wk.n_pieces);
+    int k0, k1;
+    paged_cut(steps, wk.piece, wk.n_pieces, k0, k1);
 
     // ---- this lane's query row
     const int row = wk.tile * TILE + wave * 32 + l32, r = min(row, wk.n_rows - 1), tok = r / p.rep;
@@ -320,8 +321,8 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
         for (int db = 0; db < DB; ++db)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                *(f32x4 *)(p.part_u + at * D + 32 * db + 8 * i + 4 * h) = f32x4{O[db][4 * i], O[db][4 * i + 1], O[db][4 * i + 2], O[db][4 * i + 3]};
-        if (h == 0) { p.part_ml[at * 2] = m; p.part_ml[at * 2 + 1] = l; }
+                *(f32x4 *)(p.many.part_u + at * D + 32 * db + 8 * i + 4 * h) = f32x4{O[db][4 * i], O[db][4 * i + 1], O[db][4 * i + 2], O[db][4 * i + 3]};
+        if (h == 0) { p.many.part_ml[at * 2] = m; p.many.part_ml[at * 2 + 1] = l; }
         return;
     }
     const float inv = l == 0.f ? 0.f : 1.0f / l;
@@ -341,25 +342,15 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
 template <int D>
 int32_t launch_dim(const PagedAttnParams &p, hipStream_t s) {
     constexpr int NW = PAGED_TILE / 32;
-    const PagedGrid g = paged_grid(p, PAGED_TILE);
     auto kern = paged_tile_kernel<D, NW>;
     const int lds = 4 * KEYS * 2 * D + 4 * (3 * p.S + 2);
     static std::atomic<uint64_t> lds_ready{0};
     CASCADE_HIP_TRY(ensure_dynamic_lds((const void *)kern, 4 * KEYS * 2 * D + 4 * (3 * 1024 + 2), lds_ready));
-    hipLaunchKernelGGL(kern, dim3((unsigned)g.pieces, p.Hkv), dim3(64 * NW), lds, s, p);
-    hipLaunchKernelGGL((paged_merge_kernel<bf16_t, PAGED_TILE, KEYS>), dim3((unsigned)g.split_tiles, p.Hkv, PAGED_TILE / 16), dim3(256), 0, s, p);
+    hipLaunchKernelGGL(kern, dim3((unsigned)paged_grid(p, p.many, PAGED_TILE).pieces, p.Hkv), dim3(64 * NW), lds, s, p);
     CASCADE_HIP_TRY(hipGetLastError());
     return CASCADE_OK;
 }
 
 }   // namespace
 
-int32_t launch_paged_tile(PagedAttnParams p, float *workspace, hipStream_t s) {
-    p.target = max(1, PAGED_TILE_TARGET / p.Hkv);
-    p.min_steps = 4;
-    const PagedGrid g = paged_grid(p, PAGED_TILE);
-    p.max_parts = (int32_t)g.parts;
-    p.part_ml = workspace;
-    p.part_u = workspace + g.parts * p.Hkv * PAGED_TILE * 2;
-    return p.d == 64 ? launch_dim<64>(p, s) : launch_dim<128>(p, s);
-}
+int32_t launch_paged_tile(const PagedAttnParams &p, hipStream_t s) { return p.d == 64 ? launch_dim<64>(p, s) : launch_dim<128>(p, s); }
