@@ -49,8 +49,8 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
     constexpr int BUF = KEYS * ROW;                        // bytes of a tile of keys (or values)
     constexpr int RPI = 1024 / ROW;                        // rows that one instruction of a wavefront loads
     constexpr int NI = KEYS / RPI / NW;                    // instructions of a wavefront for a tile
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];   // K, K, V, V, then the shards' words
-    int32_t *const cum = (int32_t *)(smem + 4 * BUF), *const limit = cum + p.S + 1, *const least = limit + p.S;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];   // three tiles of K, three of V, the shards' words
+    int32_t *const cum = (int32_t *)(smem + 6 * BUF), *const limit = cum + p.S + 1, *const least = limit + p.S;
     int32_t *const odd_flag = least + p.S;
 
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, h = lane >> 5;
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
 #pragma unroll
         for (int i = 0; i < NI; ++i) load16_to_lds(rs, buf + (wave * ROWS_W + i * RPI) * ROW, off[i]);
     };
-    unsigned char *const kbuf = smem, *const vbuf = smem + 2 * BUF;
+    unsigned char *const kbuf = smem, *const vbuf = smem + 3 * BUF;
 
     // ---- pieces of a step
     const int k_swz = D == 128 ? l32 & 15 : (l32 >> 1) & 7, k_row = l32 * ROW;
@@ -209,19 +209,29 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
         int shard_ahead = 0;
         Tile cur = tile_at(k0, shard_ahead), next, after;
         request(cur, p.k_pages, kbuf, k_off);
+        // (behind the last step: nothing is requested, and scores of what the buffer holds are formed and not used)
+        auto tile_or_none = [&](int t, const Tile &last) {
+            if (t < k1) return tile_at(t, shard_ahead);
+            Tile x = last;
+            x.here = 0;
+            return x;
+        };
+        next = tile_or_none(k0 + 1, cur);
         request(cur, p.v_pages, vbuf, v_off);
-        next = k0 + 1 < k1 ? tile_at(k0 + 1, shard_ahead) : cur;
         request(next, p.k_pages, kbuf + BUF, k_off);
-        after = k0 + 2 < k1 ? tile_at(k0 + 2, shard_ahead) : next;
+        after = tile_or_none(k0 + 2, next);
+        request(next, p.v_pages, vbuf + BUF, v_off);
+        request(after, p.k_pages, kbuf + 2 * BUF, k_off);
         phase_barrier<0, false>();
         scores(kbuf, S);
         float top = masked_top(cur, S, top_of(S));
+        int b0 = 0, b1 = BUF, b2 = 2 * BUF;                // buffers of steps t, t + 1, t + 2 (mod 3)
         for (int t = k0; t < k1; ++t) {
-            const int odd = (t - k0) & 1;
-            phase_barrier<0, false>();                     // K of step t + 1 and V of step t are there; K of t and V of t - 1 are free
-            request(after, p.k_pages, kbuf + odd * BUF, k_off);
-            request(next, p.v_pages, vbuf + (1 - odd) * BUF, v_off);
-            const unsigned char *vb = vbuf + odd * BUF;
+            // K of step t + 1 and V of step t are there (each wavefront waited for its own in the step before); everyone is done
+            // with K of t and V of t - 1
+            phase_barrier<-1, false>();
+            const Tile later = tile_or_none(t + 3, after); // (requested at the end of the step: its page numbers arrive meanwhile)
+            const unsigned char *vb = vbuf + b0;
             const bool care = cur.j0 + KEYS > __builtin_amdgcn_readfirstlane(least[cur.shard]);
             bool not_finite = false;
             if (care) {                                    // (the same for all wavefronts)
@@ -260,7 +270,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
             }
             const float off = m == -INFINITY ? 0.f : m;
             f32x16 S_next[2];
-            scores(kbuf + (1 - odd) * BUF, S_next);        // (behind the last step: the last tile again, unused)
+            scores(kbuf + b1, S_next);                     // (behind the last step: unused)
             bf16x8 P[4];
             float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -272,11 +282,17 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
                     P[kk][j] = (bf16_t)e;
                 }
             l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0): K of step t + 2 and V of t + 1, requested a step ago
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
                 for (int db = 0; db < DB; ++db) O[db] = mfma32(v_frag(vb, kk, db), P[kk], O[db]);
             float top_next = top_of(S_next);
+            // The requests stand behind the reads of V: in front of a transposing read the compiler waits for every load into
+            // LDS that is under way.
+            __builtin_amdgcn_sched_barrier(0);
+            request(later, p.k_pages, kbuf + b0, k_off);
+            request(after, p.v_pages, vbuf + b2, v_off);
             if (not_finite) {
                 // values of this tile from memory: keys that this row sees, columns that this lane holds
                 const int32_t *ids = p.table + (list0 + cur.shard) * p.max_pages;
@@ -298,6 +314,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
                         for (int i = 0; i < 16; ++i) {
                             const float v = (float)vr[32 * db + 8 * (i >> 2) + 4 * h + (i & 3)];
                             if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) O[db][i] += w * v;
+                            if ((i & 3) == 3) __builtin_amdgcn_sched_barrier(0);       // (rare: few registers matter more than its time)
                         }
                 }
             }
@@ -307,7 +324,9 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
             S[1] = S_next[1];
             cur = next;
             next = after;
-            if (t + 3 < k1) after = tile_at(t + 3, shard_ahead);
+            after = later;
+            const int free = b0;
+            b0 = b1; b1 = b2; b2 = free;
         }
     }
     {
@@ -343,9 +362,9 @@ template <int D>
 int32_t launch_dim(const PagedAttnParams &p, hipStream_t s) {
     constexpr int NW = PAGED_TILE / 32;
     auto kern = paged_tile_kernel<D, NW>;
-    const int lds = 4 * KEYS * 2 * D + 4 * (3 * p.S + 2);
+    const int lds = 6 * KEYS * 2 * D + 4 * (3 * p.S + 2);
     static std::atomic<uint64_t> lds_ready{0};
-    CASCADE_HIP_TRY(ensure_dynamic_lds((const void *)kern, 4 * KEYS * 2 * D + 4 * (3 * 1024 + 2), lds_ready));
+    CASCADE_HIP_TRY(ensure_dynamic_lds((const void *)kern, 6 * KEYS * 2 * D + 4 * (3 * 1024 + 2), lds_ready));
     hipLaunchKernelGGL(kern, dim3((unsigned)paged_grid(p, p.many, PAGED_TILE).pieces, p.Hkv), dim3(64 * NW), lds, s, p);
     CASCADE_HIP_TRY(hipGetLastError());
     return CASCADE_OK;
