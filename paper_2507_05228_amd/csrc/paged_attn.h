@@ -11,6 +11,9 @@
 #include "device_utils.h"
 #include "paged.h"
 
+// Lists and lengths do not change while a kernel runs: read through the scalar cache, beside the loads of keys and values
+typedef const __attribute__((address_space(4))) int32_t *scalar_ints;
+
 struct PagedSet {                                          // the sequences of one kernel
     int32_t above, upto;                                   // those of more than `above` and at most `upto` flattened rows
     int32_t min_steps, target;

@@ -51,16 +51,19 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
     constexpr int NI = KEYS / RPI / NW;                    // instructions of a wavefront for a tile
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];   // three tiles of K, three of V, the shards' words
     int32_t *const cum = (int32_t *)(smem + 6 * BUF), *const limit = cum + p.S + 1, *const least = limit + p.S;
-    int32_t *const odd_flag = least + p.S;
+    int32_t *const any_bad = least + p.S, *const odd_flag = any_bad + 1;
 
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const bool second = wave >= NW / 2;                    // (the SIMD's other wavefront)
     const int g = blockIdx.y;
     PagedWork wk;
     if (!paged_find_work<TILE, KEYS, false>(p, p.many, blockIdx.x, wk)) return;
     const int64_t list0 = (int64_t)wk.b * p.S;
 
-    // ---- keys of every shard that some row of the tile sees, and those that all of them see
+    // ---- keys of every shard that some row of the tile sees, and whether the lists name pages for them
+    if (tid < 2) any_bad[tid] = 0;
+    __syncthreads();
     {
         const int r0 = wk.tile * TILE, r1 = min(r0 + TILE, wk.n_rows) - 1;
         const int first = wk.first_row + r0 / p.rep, last = wk.first_row + r1 / p.rep;
@@ -78,8 +81,11 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
                 fewest = wave_min_int(fewest);
             }
             if (lane == 0) { limit[s] = most; least[s] = fewest; }
+            const int pages = (most + (1 << p.page_shift) - 1) >> p.page_shift;
+            bool bad = false;
+            for (int i = lane; i < pages; i += 64) bad |= (uint32_t)p.table[(list0 + s) * p.max_pages + i] >= (uint32_t)p.n_pages;
+            if (bad) *any_bad = 1;
         }
-        if (tid == 0) *odd_flag = 0;
         __syncthreads();
         if (wave == 0) {
             int carry = 0;
@@ -93,6 +99,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
         __syncthreads();
     }
     const int steps = __builtin_amdgcn_readfirstlane(cum[p.S]);
+    const bool bad_pages = __builtin_amdgcn_readfirstlane(*any_bad) != 0;
     int k0, k1;
     paged_cut(steps, wk.piece, wk.n_pieces, k0, k1);
 
@@ -115,26 +122,38 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
         int j0, shard, end, bad;                           // first key; keys of the shard that count; blocks of 16 without a page
         int64_t at;                                        // offset of the piece of a page that this wavefront loads
         int here;                                          // its rows that count
+        bool care;                                         // some row of the workgroup does not see all of it
     };
     constexpr int ROWS_W = KEYS / NW;                      // rows that a wavefront loads: within 16
-    auto tile_at = [&](int t, int &shard) {
+    struct Walk { int shard, base, upto, end, least; };    // a shard: its first step, the next one's, its keys that count
+    auto shard_at = [&](int s) {
+        Walk w;
+        w.shard = s;
+        w.base = __builtin_amdgcn_readfirstlane(cum[s]);
+        w.upto = __builtin_amdgcn_readfirstlane(cum[s + 1]);
+        w.end = __builtin_amdgcn_readfirstlane(limit[s]);
+        w.least = __builtin_amdgcn_readfirstlane(least[s]);
+        return w;
+    };
+    auto tile_at = [&](int t, Walk &w) {
+        while (t >= w.upto) w = shard_at(w.shard + 1);     // (ends: t is below cum[S])
         Tile x;
-        if (p.S > 1)
-            while (t >= cum[shard + 1]) ++shard;           // (ends: t is below cum[S])
-        x.shard = __builtin_amdgcn_readfirstlane(shard);
-        x.j0 = __builtin_amdgcn_readfirstlane((t - cum[shard]) * KEYS);
-        x.end = __builtin_amdgcn_readfirstlane(limit[shard]);
-        const int32_t *ids = p.table + (list0 + x.shard) * p.max_pages;
+        x.shard = w.shard;
+        x.j0 = (t - w.base) * KEYS;
+        x.end = w.end;
+        x.care = x.j0 + KEYS > w.least;
+        const scalar_ints ids = (scalar_ints)p.table + (list0 + x.shard) * p.max_pages;
         x.bad = 0;
+        if (bad_pages) {
 #pragma unroll
-        for (int b = 0; b < KEYS / 16; ++b) {
-            const int j = x.j0 + 16 * b;
-            const int id = ids[min(j, x.end - 1) >> p.page_shift];
-            if (j < x.end && (uint32_t)id >= (uint32_t)p.n_pages) x.bad |= 1 << b;
+            for (int b = 0; b < KEYS / 16; ++b) {
+                const int j = x.j0 + 16 * b;
+                if (j < x.end && (uint32_t)ids[j >> p.page_shift] >= (uint32_t)p.n_pages) x.bad |= 1 << b;
+            }
         }
         const int j = x.j0 + wave * ROWS_W;
-        const int id = __builtin_amdgcn_readfirstlane(ids[min(j, x.end - 1) >> p.page_shift]);
-        x.here = (uint32_t)id < (uint32_t)p.n_pages ? min(max(x.end - j, 0), ROWS_W) : 0;
+        const int id = ids[min(j, x.end - 1) >> p.page_shift];
+        x.here = __builtin_amdgcn_readfirstlane((uint32_t)id < (uint32_t)p.n_pages ? min(max(x.end - j, 0), ROWS_W) : 0);
         x.at = x.here ? ((((int64_t)id * p.Hkv + g) << p.page_shift) + (j & ((1 << p.page_shift) - 1))) * D : 0;
         return x;
     };
@@ -157,12 +176,12 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
     const int k_swz = D == 128 ? l32 & 15 : (l32 >> 1) & 7, k_row = l32 * ROW;
     auto scores = [&](const unsigned char *kb, f32x16 (&out)[2]) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            out[b] = f32x16{};
+        for (int b = 0; b < 2; ++b) out[b] = f32x16{};
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
                 out[b] = mfma32(*(const bf16x8 *)(kb + b * 32 * ROW + k_row + (((2 * ks + h) ^ k_swz) * 16)), Q[ks], out[b]);
-        }
     };
     auto top_of = [&](const f32x16 (&s)[2]) {
         float t = fmaxf(s[0][0], s[1][0]);
@@ -179,18 +198,15 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
         if (p.visible) seen = min(seen, p.visible[(int64_t)token * p.S + shard]);
         seen_least = __builtin_amdgcn_readfirstlane(wave_min_int(seen));
     };
-    // masks what the rows do not see; the largest score that is left, in log2 units
-    auto masked_top = [&](const Tile &x, f32x16 (&s)[2], float top) {
+    // masks what the rows do not see
+    auto mask = [&](const Tile &x, f32x16 (&s)[2]) {
         limits(x.shard);
-        if (x.j0 + KEYS > seen_least || x.bad) {
+        if (x.j0 + KEYS <= seen_least && !x.bad) return;
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (x.j0 + key_of(b, i) >= seen || (x.bad >> (2 * b + (i >> 3)) & 1)) s[b][i] = -INFINITY;
-            top = top_of(s);
-        }
-        return top;
+            for (int i = 0; i < 16; ++i)
+                if (x.j0 + key_of(b, i) >= seen || (x.bad >> (2 * b + (i >> 3)) & 1)) s[b][i] = -INFINITY;
     };
     const int vr_row = (lane & 15) >> 2;                   // row of the four keys that this lane's address names
     const int v_col = 16 * (lane >> 4 & 1) + 4 * (lane & 3);       // and its first column of 32
@@ -205,61 +221,54 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
     };
 
+    // Values that are not finite must not meet the zero weight of a row that does not see them.  In a tile that some row of the
+    // workgroup does not see whole, a wavefront clears those among the rows that it loaded itself, once they have arrived; what
+    // they do to the rows that see them is made good behind the walk.
+    auto clear_odd = [&](unsigned char *vb) {
+        unsigned char *const mine = vb + wave * ROWS_W * ROW + lane * 16;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            u32x4 w = *(const u32x4 *)(mine + i * 1024);
+            bool odd = false;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if ((w[j] & 0x7f80u) == 0x7f80u) { w[j] &= 0xffff0000u; odd = true; }
+                if ((w[j] & 0x7f800000u) == 0x7f800000u) { w[j] &= 0xffffu; odd = true; }
+            }
+            if (odd) { *(u32x4 *)(mine + i * 1024) = w; *odd_flag = 1; }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // (in front of the next barrier)
+    };
     if (k0 < k1) {
-        int shard_ahead = 0;
-        Tile cur = tile_at(k0, shard_ahead), next, after;
-        request(cur, p.k_pages, kbuf, k_off);
+        int s0 = 0;
+        while (k0 >= cum[s0 + 1]) ++s0;
+        Walk ahead = shard_at(__builtin_amdgcn_readfirstlane(s0));
         // (behind the last step: nothing is requested, and scores of what the buffer holds are formed and not used)
         auto tile_or_none = [&](int t, const Tile &last) {
-            if (t < k1) return tile_at(t, shard_ahead);
+            if (t < k1) return tile_at(t, ahead);
             Tile x = last;
             x.here = 0;
+            x.care = false;
             return x;
         };
-        next = tile_or_none(k0 + 1, cur);
+        Tile cur = tile_at(k0, ahead);
+        request(cur, p.k_pages, kbuf, k_off);
         request(cur, p.v_pages, vbuf, v_off);
+        Tile next = tile_or_none(k0 + 1, cur);
         request(next, p.k_pages, kbuf + BUF, k_off);
-        after = tile_or_none(k0 + 2, next);
-        request(next, p.v_pages, vbuf + BUF, v_off);
-        request(after, p.k_pages, kbuf + 2 * BUF, k_off);
+        Tile after = tile_or_none(k0 + 2, next);
         phase_barrier<0, false>();
+        if (cur.care) clear_odd(vbuf);
         scores(kbuf, S);
-        float top = masked_top(cur, S, top_of(S));
         int b0 = 0, b1 = BUF, b2 = 2 * BUF;                // buffers of steps t, t + 1, t + 2 (mod 3)
+        if (second) phase_barrier<-1, false>();            // half a step behind the first four wavefronts
         for (int t = k0; t < k1; ++t) {
-            // K of step t + 1 and V of step t are there (each wavefront waited for its own in the step before); everyone is done
-            // with K of t and V of t - 1
-            phase_barrier<-1, false>();
-            const Tile later = tile_or_none(t + 3, after); // (requested at the end of the step: its page numbers arrive meanwhile)
-            const unsigned char *vb = vbuf + b0;
-            const bool care = cur.j0 + KEYS > __builtin_amdgcn_readfirstlane(least[cur.shard]);
-            bool not_finite = false;
-            if (care) {                                    // (the same for all wavefronts)
-                bool mine = false;
-#pragma unroll
-                for (int i = 0; i < BUF / (1024 * NW); ++i) {
-                    const u32x4 w = *(const u32x4 *)(vb + (i * NW * 64 + tid) * 16);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) mine |= (w[j] & 0x7f80u) == 0x7f80u || (w[j] & 0x7f800000u) == 0x7f800000u;
-                }
-                if (mine) *odd_flag = 1;
-                phase_barrier<-1, true>();
-                not_finite = __builtin_amdgcn_readfirstlane(*odd_flag) != 0;
-                if (not_finite) {                          // out of the product; added below, row by row
-#pragma unroll
-                    for (int i = 0; i < BUF / (1024 * NW); ++i) {
-                        u32x4 w = *(const u32x4 *)(vb + (i * NW * 64 + tid) * 16);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            if ((w[j] & 0x7f80u) == 0x7f80u) w[j] &= 0xffff0000u;
-                            if ((w[j] & 0x7f800000u) == 0x7f800000u) w[j] &= 0xffffu;
-                        }
-                        *(u32x4 *)(vb + (i * NW * 64 + tid) * 16) = w;
-                    }
-                    phase_barrier<-1, true>();
-                    if (tid == 0) *odd_flag = 0;
-                }
-            }
+            // ---- vector half
+            request(after, p.k_pages, kbuf + b2, k_off);
+            request(next, p.v_pages, vbuf + b1, v_off);
+            const Tile later = tile_or_none(t + 3, after);
+            mask(cur, S);
+            const float top = top_of(S);
             if (__any(top > m + RAISE)) {
                 const float m_new = fmaxf(m, halves_max(top));
                 const float f = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
@@ -269,43 +278,51 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
                 for (int i = 0; i < DB; ++i) O[i] *= f;
             }
             const float off = m == -INFINITY ? 0.f : m;
-            f32x16 S_next[2];
-            scores(kbuf + b1, S_next);                     // (behind the last step: unused)
-            bf16x8 P[4];
+            u32x4 P[4];
             float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float e = __builtin_amdgcn_exp2f(fmaf(S[kk >> 1][8 * (kk & 1) + j], p.scale_log2, -off));
-                    sum[j & 3] += e;
-                    P[kk][j] = (bf16_t)e;
+                for (int j = 0; j < 4; ++j) {
+                    const float e0 = __builtin_amdgcn_exp2f(fmaf(S[kk >> 1][8 * (kk & 1) + 2 * j], p.scale_log2, -off));
+                    const float e1 = __builtin_amdgcn_exp2f(fmaf(S[kk >> 1][8 * (kk & 1) + 2 * j + 1], p.scale_log2, -off));
+                    sum[j] += e0 + e1;
+                    P[kk][j] = __builtin_bit_cast(uint32_t, bf16x2{(bf16_t)e0, (bf16_t)e1});
                 }
             l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-            __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0): K of step t + 2 and V of t + 1, requested a step ago
+            asm volatile("" : "+v"(l));                    // (here, not behind the products with 32 registers in tow)
+            phase_barrier<-1, false>();
+            // ---- matrix half
+            __builtin_amdgcn_s_setprio(1);
+            const unsigned char *vb = vbuf + b0;
+            scores(kbuf + b1, S);
+            __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0): what this wavefront requested half a step ago
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
-                for (int db = 0; db < DB; ++db) O[db] = mfma32(v_frag(vb, kk, db), P[kk], O[db]);
-            float top_next = top_of(S_next);
-            // The requests stand behind the reads of V: in front of a transposing read the compiler waits for every load into
-            // LDS that is under way.
-            __builtin_amdgcn_sched_barrier(0);
-            request(later, p.k_pages, kbuf + b0, k_off);
-            request(after, p.v_pages, vbuf + b2, v_off);
-            if (not_finite) {
-                // values of this tile from memory: keys that this row sees, columns that this lane holds
-                const int32_t *ids = p.table + (list0 + cur.shard) * p.max_pages;
+                for (int db = 0; db < DB; ++db) O[db] = mfma32(v_frag(vb, kk, db), __builtin_bit_cast(bf16x8, P[kk]), O[db]);
+            __builtin_amdgcn_s_setprio(0);
+            if (next.care) clear_odd(vbuf + b1);
+            cur = next;
+            next = after;
+            after = later;
+            const int free = b0;
+            b0 = b1; b1 = b2; b2 = free;
+            phase_barrier<-1, false>();
+        }
+        if (!second) phase_barrier<-1, false>();           // (as many for every wavefront)
+        if (__builtin_amdgcn_readfirstlane(*odd_flag)) {
+            // a weight times a value that is not finite is that value, whatever the weight
+            Walk w = shard_at(__builtin_amdgcn_readfirstlane(s0));
+            for (int t = k0; t < k1; ++t) {
+                const Tile x = tile_at(t, w);
+                if (!x.care) continue;
+                limits(x.shard);
+                const scalar_ints ids = (scalar_ints)p.table + (list0 + x.shard) * p.max_pages;
 #pragma nounroll
-                for (int key = 0; key < KEYS; ++key) {
-                    float w = 0.f;
-                    const int idx = (key >> 5) * 16 + (key >> 3 & 3) * 4 + (key & 3);      // register of the lane that holds it
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (idx == i) w = (float)P[i >> 3][i & 7];
-                    w = __shfl(w, (key >> 2 & 1) * 32 + l32, WAVE);
-                    const int j = cur.j0 + key;
-                    if (j >= seen || (cur.bad >> (key >> 4) & 1)) continue;
+                for (int key = 0; key < KEYS && x.j0 + key < x.end; ++key) {
+                    const int j = x.j0 + key;
+                    if (x.bad >> (key >> 4) & 1) continue;
                     const bf16_t *vr = (const bf16_t *)p.v_pages +
                         ((((int64_t)ids[j >> p.page_shift] * p.Hkv + g) << p.page_shift) + (j & ((1 << p.page_shift) - 1))) * D;
 #pragma unroll
@@ -313,20 +330,10 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const float v = (float)vr[32 * db + 8 * (i >> 2) + 4 * h + (i & 3)];
-                            if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) O[db][i] += w * v;
-                            if ((i & 3) == 3) __builtin_amdgcn_sched_barrier(0);       // (rare: few registers matter more than its time)
+                            if (j < seen && (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) O[db][i] += v;
                         }
                 }
             }
-            if (t + 1 < k1) top_next = masked_top(next, S_next, top_next);
-            top = top_next;
-            S[0] = S_next[0];
-            S[1] = S_next[1];
-            cur = next;
-            next = after;
-            after = later;
-            const int free = b0;
-            b0 = b1; b1 = b2; b2 = free;
         }
     }
     {
@@ -362,9 +369,9 @@ template <int D>
 int32_t launch_dim(const PagedAttnParams &p, hipStream_t s) {
     constexpr int NW = PAGED_TILE / 32;
     auto kern = paged_tile_kernel<D, NW>;
-    const int lds = 6 * KEYS * 2 * D + 4 * (3 * p.S + 2);
+    const int lds = 6 * KEYS * 2 * D + 4 * (3 * p.S + 3);
     static std::atomic<uint64_t> lds_ready{0};
-    CASCADE_HIP_TRY(ensure_dynamic_lds((const void *)kern, 6 * KEYS * 2 * D + 4 * (3 * 1024 + 2), lds_ready));
+    CASCADE_HIP_TRY(ensure_dynamic_lds((const void *)kern, 6 * KEYS * 2 * D + 4 * (3 * 1024 + 3), lds_ready));
     hipLaunchKernelGGL(kern, dim3((unsigned)paged_grid(p, p.many, PAGED_TILE).pieces, p.Hkv), dim3(64 * NW), lds, s, p);
     CASCADE_HIP_TRY(hipGetLastError());
     return CASCADE_OK;
