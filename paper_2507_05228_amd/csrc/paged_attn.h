@@ -42,6 +42,7 @@ struct PagedWork {
     int tile, steps;                                       // steps: of the sequence's whole walk
     int piece, n_pieces, first_piece;                      // first_piece: number of this tile's first partial (n_pieces > 1)
     int k0, k1;                                            // steps of this piece
+    bool valid;
 };
 
 // Sum over the lanes up to this one.  Inside rows of 16 lanes by shifts, then the last lane of a row is handed to the rows
@@ -70,20 +71,18 @@ __device__ __forceinline__ void paged_cut(int steps, int i, int n, int &k0, int 
     k1 = k0 + each + (i < more);
 }
 
-// Piece number w of the launch (whole wavefronts call this, with the same w).  MERGE: tile number w among those with partials.
-template <int TILE, int KEYS, bool MERGE>
-__device__ __forceinline__ bool paged_find_work(const PagedAttnParams &p, const PagedSet &set, int w, PagedWork &out) {
-    const int lane = threadIdx.x & 63;
-    int tiles = 0, steps = 0, lo = 0, n = 0;
-    auto load = [&](int b) {
+// The division of a set's work, held by a wavefront: lane i has sequence b0 + i (of 64 at a time)
+template <int TILE, int KEYS>
+struct PagedPlan {
+    int tiles, steps, lo, n;                               // of the lane's sequence
+    int per_piece;
+
+    __device__ __forceinline__ void load(const PagedAttnParams &p, const PagedSet &set, int b) {
         tiles = steps = lo = n = 0;
         if (b >= p.B) return;
+        const int64_t list0 = (int64_t)b * p.S;
         lo = min(max(p.q_start[b], 0), p.rows);
         const int64_t flat = (int64_t)max(min(p.q_start[b + 1], p.rows) - lo, 0) * p.rep;
-        if (flat <= set.above || flat > set.upto) return;
-        n = (int)flat;
-        tiles = (n + TILE - 1) / TILE;
-        const int64_t list0 = (int64_t)b * p.S;
         for (int s0 = 0; s0 < p.S; s0 += 8) {              // eight loads in flight
             int n_s[8];
 #pragma unroll
@@ -91,52 +90,63 @@ __device__ __forceinline__ bool paged_find_work(const PagedAttnParams &p, const 
 #pragma unroll
             for (int i = 0; i < 8; ++i) steps += s0 + i < p.S ? (n_s[i] + KEYS - 1) / KEYS : 0;
         }
-    };
-    // (in fp32: every workgroup forms the same sum in the same order; the margin keeps the number of pieces inside its bound)
-    float total = 0.f;
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-        load(b0 + lane);
-        total += (float)tiles * (float)steps;
+        if (flat <= set.above || flat > set.upto) { steps = 0; return; }
+        n = (int)flat;
+        tiles = (n + TILE - 1) / TILE;
     }
-    total = wave_sum(total);
-    const int per_piece = __builtin_amdgcn_readfirstlane(max(set.min_steps, (int)fminf(total * set.inv_target * 1.0001f + 1.f, 1e9f)));
-    int before = 0, parts_before = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-        if (p.B > 64) load(b0 + lane);                     // (else they are those of the loop above)
-        const int pieces = steps <= per_piece ? 1 : (int)(((uint32_t)steps + (uint32_t)per_piece - 1) / (uint32_t)per_piece);
-        const int parts = pieces > 1 ? tiles * pieces : 0;
-        const int items = MERGE ? (pieces > 1 ? tiles : 0) : tiles * pieces;
-        const int incl = wave_inclusive(items), parts_incl = wave_inclusive(parts);
-        const uint64_t past = __ballot(before + incl > w);
-        if (past) {
-            const int at = __ffsll((unsigned long long)past) - 1;
-            auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
-            const int i = w - before - of(incl - items);
-            out.n_pieces = of(pieces);
-            // late tiles first: with a causal limit they are the long ones
-            const int tile = MERGE || out.n_pieces == 1 ? i : (int)((uint32_t)i / (uint32_t)out.n_pieces);
-            out.b = b0 + at;
-            out.first_row = of(lo);
-            out.n_rows = of(n);
-            out.steps = of(steps);
-            out.piece = MERGE ? 0 : i - tile * out.n_pieces;
-            out.first_piece = parts_before + of(parts_incl - parts) + tile * out.n_pieces;
-            out.tile = of(tiles) - 1 - tile;
-            paged_cut(out.steps, out.piece, out.n_pieces, out.k0, out.k1);
-            // (more partials than the launch has room for: only where sequences overlap, which they must not)
-            return out.n_pieces == 1 || out.first_piece + out.n_pieces <= set.max_parts;
+    __device__ __forceinline__ void make(const PagedAttnParams &p, const PagedSet &set) {
+        // (in fp32: every workgroup forms the same sum in the same order; the margin keeps the number of pieces inside its bound)
+        float total = 0.f;
+        for (int b0 = 0; b0 < p.B; b0 += 64) {
+            load(p, set, b0 + (threadIdx.x & 63));
+            total += (float)tiles * (float)steps;
         }
-        before += __builtin_amdgcn_readlane(incl, 63);
-        parts_before += __builtin_amdgcn_readlane(parts_incl, 63);
+        total = wave_sum(total);
+        per_piece = __builtin_amdgcn_readfirstlane(max(set.min_steps, (int)fminf(total * set.inv_target * 1.0001f + 1.f, 1e9f)));
     }
-    return false;
-}
+    // Piece number w; MERGE: tile number w among those with partials.  Whole wavefronts call this, with the same w.
+    template <bool MERGE>
+    __device__ __forceinline__ bool pick(const PagedAttnParams &p, const PagedSet &set, int w, PagedWork &out) {
+        int before = 0, parts_before = 0;
+        for (int b0 = 0; b0 < p.B; b0 += 64) {
+            if (p.B > 64) load(p, set, b0 + (threadIdx.x & 63));       // (else the lanes have them)
+            const int pieces = steps <= per_piece ? 1 : (int)(((uint32_t)steps + (uint32_t)per_piece - 1) / (uint32_t)per_piece);
+            const int parts = pieces > 1 ? tiles * pieces : 0;
+            const int items = MERGE ? (pieces > 1 ? tiles : 0) : tiles * pieces;
+            const int incl = wave_inclusive(items), parts_incl = wave_inclusive(parts);
+            const uint64_t past = __ballot(before + incl > w);
+            if (past) {
+                const int at = __ffsll((unsigned long long)past) - 1;
+                auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+                const int i = w - before - of(incl - items);
+                out.n_pieces = of(pieces);
+                // late tiles first: with a causal limit they are the long ones
+                const int tile = MERGE || out.n_pieces == 1 ? i : (int)((uint32_t)i / (uint32_t)out.n_pieces);
+                out.b = b0 + at;
+                out.first_row = of(lo);
+                out.n_rows = of(n);
+                out.steps = of(steps);
+                out.piece = MERGE ? 0 : i - tile * out.n_pieces;
+                out.first_piece = parts_before + of(parts_incl - parts) + tile * out.n_pieces;
+                out.tile = of(tiles) - 1 - tile;
+                paged_cut(out.steps, out.piece, out.n_pieces, out.k0, out.k1);
+                // (more partials than the launch has room for: only where sequences overlap, which they must not)
+                out.valid = out.n_pieces == 1 || out.first_piece + out.n_pieces <= set.max_parts;
+                return true;
+            }
+            before += __builtin_amdgcn_readlane(incl, 63);
+            parts_before += __builtin_amdgcn_readlane(parts_incl, 63);
+        }
+        return false;
+    }
+};
 
 // What a set of tiles of `tile` rows may need: workgroups per kv head, and tiles with partials and partials among them
 struct PagedGrid { int64_t pieces, split_tiles, parts; };
 static inline PagedGrid paged_grid(const PagedAttnParams &p, const PagedSet &set, int tile) {
     const int64_t flat = (int64_t)p.rows * p.rep, seqs = flat / (set.above + 1);
-    const int64_t tiles = flat / tile + (p.B < seqs ? p.B : seqs);
+    const int64_t n_seqs = p.B < seqs ? p.B : seqs, each = ((int64_t)set.upto + tile - 1) / tile;
+    const int64_t tiles = flat / tile < n_seqs * (each - 1) ? flat / tile + n_seqs : n_seqs * each;
     PagedGrid g;
     g.pieces = tiles + set.target;                         // sum of ceil(steps / per_piece) <= tiles + sum of steps / per_piece
     g.split_tiles = tiles < set.target ? tiles : set.target;       // a cut walk is longer than per_piece

@@ -49,11 +49,6 @@ __device__ __forceinline__ float rows_sum(float v) {
     return v + __shfl_xor(v, 32, WAVE);
 }
 
-__device__ __forceinline__ bool word_not_finite(float x, bool is_bf16_pair) {
-    const uint32_t w = __builtin_bit_cast(uint32_t, x);
-    return is_bf16_pair ? (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u : (w & 0x7f800000u) == 0x7f800000u;
-}
-
 // Wavefronts per SIMD that the registers allow: keys and values of a step, queries and accumulators, and some 70 more
 constexpr int rows_occupancy(int size, int DM, int RB) {
     const int regs = DM / 4 * size + (DM / 16 * size + DM / 4) * RB + 70;
@@ -73,9 +68,11 @@ __global__ __launch_bounds__(256, rows_occupancy(sizeof(T), DM, RB)) void paged_
     extern __shared__ __attribute__((aligned(16))) float smem[];   // [4][TILE][DM] u, then [4][TILE][2]; before that the shards' steps
     const int lane = threadIdx.x & 63, c16 = lane & 15, g4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    PagedPlan<TILE, KEYS> plan;
+    plan.make(p, p.few);
     const int g = blockIdx.y;
     PagedWork wk;
-    if (!paged_find_work<TILE, KEYS, false>(p, p.few, blockIdx.x, wk)) return;
+    if (!plan.template pick<false>(p, p.few, blockIdx.x, wk) || !wk.valid) return;
 
     // first step of every shard, and its length (several shards only)
     int32_t *cum = (int32_t *)smem, *lens = cum + p.S + 1;
@@ -122,8 +119,8 @@ __global__ __launch_bounds__(256, rows_occupancy(sizeof(T), DM, RB)) void paged_
     }
 
     struct Step {
-        int seen[RB];                                      // keys of the step that a row sees
-        int j0, shard, bad;                                // first key; bit kb: 16 keys whose list entry is no page
+        int limit[RB];                                     // keys of the shard that a row may see
+        int j0, rows, bad;                                 // first key; keys of the step that exist; bit kb: 16 keys whose list entry is no page
     };
     frag kf[2][KS];                                        // keys of a step; refilled as soon as its scores are formed
     float vf[8][VW];                                       // values, rows 4 g4 + j of the first, then of the second 16 keys; refilled behind the output product
@@ -143,7 +140,7 @@ __global__ __launch_bounds__(256, rows_occupancy(sizeof(T), DM, RB)) void paged_
         x.j0 = __builtin_amdgcn_readfirstlane(j0);
         x.len = __builtin_amdgcn_readfirstlane(len);
         x.shard = __builtin_amdgcn_readfirstlane(shard);
-        const int32_t *ids = p.table + (list0 + x.shard) * p.max_pages;
+        const scalar_ints ids = (scalar_ints)p.table + (list0 + x.shard) * p.max_pages;
         x.id[0] = ids[x.j0 >> p.page_shift];
         x.id[1] = ids[min(x.j0 + 16, x.len - 1) >> p.page_shift];      // (a second 16 that does not exist: any entry that does)
         return x;
@@ -152,6 +149,17 @@ __global__ __launch_bounds__(256, rows_occupancy(sizeof(T), DM, RB)) void paged_
     const uint32_t k_off = c16 * row_bytes + g4 * 16, v_off = 4 * g4 * row_bytes + c16 * (RUN * sizeof(T));
     // (columns behind the head: outside every descriptor, which returns zeros)
     const auto k_at = [&](int ks) { return ks * KD + g4 * (KD / 4) < p.d ? k_off + ks * 64 : 0x40000000u; };
+    // limits of the sequence's rows; without any, the descriptor is empty and its zeros are not looked at
+    const __amdgpu_buffer_rsrc_t limits = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<int32_t *>(p.visible ? p.visible + (int64_t)wk.first_row * p.S : nullptr), 0,
+        p.visible ? (p.rows - wk.first_row) * p.S * 4 : 0, 0x00020000);
+    uint32_t limit_off[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) limit_off[rb] = (uint32_t)(token[rb] - wk.first_row) * (uint32_t)(p.S * 4);
+    auto seen_of = [&](const Step &x, int rb) {            // keys of a step that a row sees
+        const int n = p.visible ? min(x.rows, x.limit[rb] - x.j0) : x.rows;
+        return min(max(n, 0), KEYS);
+    };
     // The rows of 16 keys that exist: what lies behind them is outside the descriptor and arrives as zeros
     auto rows_of = [&](const void *pages, const Place &at, int kb) {
         const bool page = (uint32_t)at.id[kb] < (uint32_t)p.n_pages;
@@ -162,14 +170,11 @@ __global__ __launch_bounds__(256, rows_occupancy(sizeof(T), DM, RB)) void paged_
     auto load_keys = [&](const Place &at, Step &x) {
         const int rows = at.len - at.j0;                   // keys of the step that exist: at least 1
         x.j0 = at.j0;
-        x.shard = at.shard;
+        x.rows = rows;
         x.bad = ((uint32_t)at.id[0] >= (uint32_t)p.n_pages) | ((uint32_t)at.id[1] >= (uint32_t)p.n_pages && rows > 16) << 1;
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            int n = rows;
-            if (p.visible) n = min(n, p.visible[(int64_t)token[rb] * p.S + at.shard] - at.j0);
-            x.seen[rb] = min(max(n, 0), KEYS);
-        }
+        for (int rb = 0; rb < RB; ++rb)                    // (looked at a step later, so that nothing waits for it here)
+            x.limit[rb] = (int)__builtin_amdgcn_raw_buffer_load_b32(limits, limit_off[rb], at.shard * 4, 0);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             const __amdgpu_buffer_rsrc_t r = rows_of(p.k_pages, at, kb);
@@ -200,6 +205,7 @@ __global__ __launch_bounds__(256, rows_occupancy(sizeof(T), DM, RB)) void paged_
         }
     };
 
+    bool odd = false;
     // One step: scores, then the request of the next keys; exponentials and output product, then that of the next values
     auto step = [&](Step &x, const Place &next) {
         f32x4 s[RB][2];
@@ -213,9 +219,13 @@ __global__ __launch_bounds__(256, rows_occupancy(sizeof(T), DM, RB)) void paged_
             }
         Step ahead;
         load_keys(next, ahead);
+        int seen[RB];
         bool masked = false;
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) masked |= x.seen[rb] != KEYS;
+        for (int rb = 0; rb < RB; ++rb) {
+            seen[rb] = seen_of(x, rb);
+            masked |= seen[rb] != KEYS;
+        }
         masked = __any(masked) || x.bad;
         if (masked) {
 #pragma unroll
@@ -224,7 +234,7 @@ __global__ __launch_bounds__(256, rows_occupancy(sizeof(T), DM, RB)) void paged_
                 for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        if (16 * kb + 4 * g4 + r >= x.seen[rb] || (x.bad >> kb & 1)) s[rb][kb][r] = -INFINITY;
+                        if (16 * kb + 4 * g4 + r >= seen[rb] || (x.bad >> kb & 1)) s[rb][kb][r] = -INFINITY;
         }
         bool raise = false;
         float top[RB];
@@ -256,49 +266,18 @@ __global__ __launch_bounds__(256, rows_occupancy(sizeof(T), DM, RB)) void paged_
             l[rb] += ((s[rb][0][0] + s[rb][0][1]) + (s[rb][0][2] + s[rb][0][3])) + ((s[rb][1][0] + s[rb][1][1]) + (s[rb][1][2] + s[rb][1][3]));
         }
         // A value that is not finite must not meet the zero weight of a row that does not see it.  Steps in which every row
-        // sees every key need no care; in the others such values leave the product and are added row by row.
+        // sees every key need no care; in the others such values leave the product, and what they do to the rows that see them
+        // is made good behind the walk.
         if (masked) {
-            bool odd = false;
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
-                for (int w = 0; w < VW; ++w) odd |= word_not_finite(vf[j][w], BF);
-            if (__any(odd)) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-#pragma unroll
-                    for (int w = 0; w < VW; ++w) {
-                        uint32_t u = __builtin_bit_cast(uint32_t, vf[j][w]);
-                        if (BF) {
-                            if ((u & 0x7f80u) == 0x7f80u) u &= 0xffff0000u;
-                            if ((u & 0x7f800000u) == 0x7f800000u) u &= 0xffffu;
-                        } else if ((u & 0x7f800000u) == 0x7f800000u) u = 0;
-                        vf[j][w] = __builtin_bit_cast(float, u);
-                    }
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb)
-#pragma nounroll
-                    for (int key = 0; key < KEYS; ++key) {
-                        float w = s[rb][0][0];
-#pragma unroll
-                        for (int i = 1; i < 8; ++i)
-                            if ((key >> 4) * 4 + (key & 3) == i) w = s[rb][i / 4][i % 4];
-                        w = __shfl(w, (key >> 2 & 3) * 16 + c16, WAVE);
-                        if (key >= x.seen[rb] || (x.bad >> (key >> 4) & 1)) continue;
-                        const int j = x.j0 + key, id = p.table[(list0 + x.shard) * p.max_pages + (j >> p.page_shift)];
-                        const T *vr = (const T *)p.v_pages + ((((int64_t)id * p.Hkv + g) << p.page_shift) + (j & ((1 << p.page_shift) - 1))) * p.d;
-#pragma unroll
-                        for (int i = 0; i < NB; ++i) {
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) {
-                                const int c = i / RUN * 16 * RUN + RUN * (4 * g4 + r) + i % RUN;
-                                const float v = (float)vr[c < p.d ? c : 0];
-                                if (word_not_finite(v, false)) O[rb][i][r] += w * v;
-                            }
-                            __builtin_amdgcn_sched_barrier(0);     // (rare: few registers matter more than its time)
-                        }
-                    }
-            }
+                for (int w = 0; w < VW; ++w) {
+                    uint32_t u = __float_as_uint(vf[j][w]);
+                    if (BF && (u & 0x7f80u) == 0x7f80u) { u &= 0xffff0000u; odd = true; }
+                    if ((u & 0x7f800000u) == 0x7f800000u) { u = BF ? u & 0xffffu : 0u; odd = true; }
+                    vf[j][w] = __uint_as_float(u);
+                }
         }
         if constexpr (BF) {
             bf16x8 P[RB];
@@ -340,15 +319,52 @@ __global__ __launch_bounds__(256, rows_occupancy(sizeof(T), DM, RB)) void paged_
     a += wk.k0;
     b += wk.k0;
     if (a < b) {
-        // (the requests ahead are not conditional, behind the end they repeat the last step: with a branch around them the compiler
+        // (the requests ahead are not conditional, behind the end they are of no rows: with a branch around them the compiler
         // cannot count the loads in flight and waits for all of them)
         Step x;
         Place at = locate(a);
         load_keys(at, x);
         load_values(at);
+        const int first_shard = shard;
         for (int k = a; k < b; ++k) {
             at = locate(min(k + 1, b - 1));
+            if (k + 1 == b) at.len = at.j0;                // (no rows: nothing is read)
             step(x, at);
+        }
+        if (__any(odd)) {
+            // a weight times a value that is not finite is that value, whatever the weight
+            shard = first_shard;
+            for (int k = a; k < b; ++k) {
+                const Place at = locate(k);
+                int seen[RB];
+                bool masked = false;
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) {
+                    x.rows = at.len - at.j0;
+                    x.j0 = at.j0;
+                    x.limit[rb] = (int)__builtin_amdgcn_raw_buffer_load_b32(limits, limit_off[rb], at.shard * 4, 0);
+                    seen[rb] = seen_of(x, rb);
+                    masked |= seen[rb] != KEYS;
+                }
+                if (!__any(masked) && (uint32_t)at.id[0] < (uint32_t)p.n_pages && (uint32_t)at.id[1] < (uint32_t)p.n_pages) continue;
+#pragma nounroll
+                for (int key = 0; key < min(x.rows, KEYS); ++key) {
+                    const int id = key < 16 ? at.id[0] : at.id[1];
+                    if ((uint32_t)id >= (uint32_t)p.n_pages) continue;
+                    const T *vr = (const T *)p.v_pages + ((((int64_t)id * p.Hkv + g) << p.page_shift) + ((at.j0 + key) & ((1 << p.page_shift) - 1))) * p.d;
+#pragma unroll
+                    for (int i = 0; i < NB; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const int c = i / RUN * 16 * RUN + RUN * (4 * g4 + r) + i % RUN;
+                            const float v = (float)vr[c < p.d ? c : 0];
+                            if ((__float_as_uint(v) & 0x7f800000u) != 0x7f800000u) continue;
+#pragma unroll
+                            for (int rb = 0; rb < RB; ++rb)
+                                if (key < seen[rb]) O[rb][i][r] += v;
+                        }
+                }
+            }
         }
     }
 
@@ -400,47 +416,62 @@ __global__ __launch_bounds__(256, rows_occupancy(sizeof(T), DM, RB)) void paged_
     }
 }
 
-// Tiles whose walk was cut, of either kernel: their partials, weighted by exp2(m - largest m).  DM / 4 lanes to a row (a power of
-// two); the lanes of a row share the search for the largest m, then every thread adds its four columns, eight partials requested
-// at a time.
+// Tiles whose walk was cut, of either kernel: their partials, weighted by exp2(m - largest m).  A wavefront takes a row at a
+// time, DM / 4 lanes its columns; the lane groups that are left take every SUB-th partial, eight requested at once, with a running
+// maximum each, and meet at the end.
 template <typename T, int TILE, int KEYS, int DM>
-__device__ __forceinline__ void merge_tile(const PagedAttnParams &p, const PagedSet &set, int w) {
-    constexpr int LPR = DM / 4;
-    PagedWork wk;
-    if (!paged_find_work<TILE, KEYS, true>(p, set, w, wk)) return;
-    const int g = blockIdx.y;
+__device__ __forceinline__ void merge_set(const PagedAttnParams &p, const PagedSet &set, int first, int stride) {
+    constexpr int LPR = DM / 4, SUB = 64 / LPR, AT_ONCE = 8;
+    PagedPlan<TILE, KEYS> plan;
+    plan.make(p, set);
+    const int lane = threadIdx.x & 63, sub = lane / LPR, c = lane % LPR * 4;
     const int64_t step = (int64_t)p.Hkv * TILE;
-    for (int e = threadIdx.x + 256 * blockIdx.z; e < TILE * LPR; e += 256 * gridDim.z) {
-        const int row = e / LPR, sub = e % LPR, c = sub * 4, r = wk.tile * TILE + row;
-        if (r >= wk.n_rows) return;                        // (all lanes of the row)
+    // units: four rows of a tile and kv head
+    for (int unit = first;; unit += stride) {
+        const int quad = unit % (TILE / 4), rest = unit / (TILE / 4), w = (int)((uint32_t)rest / (uint32_t)p.Hkv), g = rest - w * p.Hkv;
+        PagedWork wk;
+        if (!plan.template pick<true>(p, set, w, wk)) return;
+        const int row = quad * 4 + (threadIdx.x >> 6), r = wk.tile * TILE + row;
+        if (!wk.valid || r >= wk.n_rows) continue;
         const int64_t at = ((int64_t)wk.first_piece * p.Hkv + g) * TILE + row;
         const float2 *ml = (const float2 *)set.part_ml + at;
-        float top = -INFINITY;
-        for (int i = sub; i < wk.n_pieces; i += LPR) top = fmaxf(top, ml[i * step].x);
-#pragma unroll
-        for (int o = 1; o < LPR; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, WAVE));
-        const float off = top == -INFINITY ? 0.f : top;
-        float sum = 0.f;
-        f32x4 u = {0.f, 0.f, 0.f, 0.f};
         const float *pu = set.part_u + at * p.d + (c < p.d ? c : 0);
-        for (int i0 = 0; i0 < wk.n_pieces; i0 += 8) {
-            float2 w[8];
-            f32x4 x[8];
+        float top = -INFINITY, sum = 0.f;
+        f32x4 u = {0.f, 0.f, 0.f, 0.f};
+        for (int i0 = sub; i0 < wk.n_pieces; i0 += SUB * AT_ONCE) {
+            float2 a[AT_ONCE];
+            f32x4 x[AT_ONCE];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int64_t i = min(i0 + j, wk.n_pieces - 1) * step;
-                w[j] = ml[i];
+            for (int j = 0; j < AT_ONCE; ++j) {
+                const int64_t i = min(i0 + j * SUB, wk.n_pieces - 1) * step;
+                a[j] = ml[i];
                 x[j] = *(const f32x4 *)(pu + i * p.d);
             }
+            float most = top;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (i0 + j >= wk.n_pieces) break;
-                const float f = __builtin_amdgcn_exp2f(w[j].x - off);
-                sum += w[j].y * f;
-                u += x[j] * f;
+            for (int j = 0; j < AT_ONCE; ++j) most = fmaxf(most, a[j].x);      // (a repeated one changes nothing)
+            const float off = most == -INFINITY ? 0.f : most, f = __builtin_amdgcn_exp2f(top - off);
+            top = most;
+            sum *= f;
+            u *= f;
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j) {
+                if (i0 + j * SUB >= wk.n_pieces) break;
+                const float e = __builtin_amdgcn_exp2f(a[j].x - off);
+                sum += a[j].y * e;
+                u += x[j] * e;
             }
         }
-        if (c >= p.d) continue;
+#pragma unroll
+        for (int o = LPR; o < 64; o <<= 1) {               // the lane groups' states
+            const float other = __shfl_xor(top, o, WAVE), most = fmaxf(top, other), off = most == -INFINITY ? 0.f : most;
+            const float f = __builtin_amdgcn_exp2f(top - off), f1 = __builtin_amdgcn_exp2f(other - off);
+            sum = sum * f + __shfl_xor(sum, o, WAVE) * f1;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) u[j] = u[j] * f + __shfl_xor(u[j], o, WAVE) * f1;
+            top = most;
+        }
+        if (sub || c >= p.d) continue;
         const int t = (int)((uint32_t)r / (uint32_t)p.rep), h = g * p.rep + r - t * p.rep;
         const int64_t out = (int64_t)(wk.first_row + t) * p.o_stride + (int64_t)h * p.d + c;
         u *= sum == 0.f ? 0.f : 1.0f / sum;
@@ -450,21 +481,22 @@ __device__ __forceinline__ void merge_tile(const PagedAttnParams &p, const Paged
     }
 }
 template <typename T, int TILE, int DM>
-__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnParams p, int many_tiles) {
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnParams p, int for_many) {
     if constexpr (sizeof(T) == 2 && DM <= 128) {
-        if ((int)blockIdx.x < many_tiles) return merge_tile<T, PAGED_TILE, PAGED_TILE_KEYS, DM>(p, p.many, blockIdx.x);
+        if ((int)blockIdx.x < for_many) return merge_set<T, PAGED_TILE, PAGED_TILE_KEYS, DM>(p, p.many, blockIdx.x, for_many);
     }
-    merge_tile<T, TILE, 32, DM>(p, p.few, blockIdx.x - many_tiles);
+    merge_set<T, TILE, 32, DM>(p, p.few, blockIdx.x - for_many, gridDim.x - for_many);
 }
 
 template <typename T, int DM, int RB>
 int32_t launch_rows(const PagedAttnParams &p, hipStream_t s) {
     constexpr int TILE = 16 * RB;
-    unsigned many_tiles = 0, few_tiles = 0;
+    // (workgroups beyond those that are resident at once take turns)
+    int64_t merge_many = 0, merge_few = 0;
     if (p.many.target) {
         const int32_t st = launch_paged_tile(p, s);
         if (st != CASCADE_OK) return st;
-        many_tiles = (unsigned)paged_grid(p, p.many, PAGED_TILE).split_tiles;
+        merge_many = min((int64_t)1024, paged_grid(p, p.many, PAGED_TILE).split_tiles * p.Hkv * (PAGED_TILE / 4));
     }
     if (p.few.target) {
         const PagedGrid g = paged_grid(p, p.few, TILE);
@@ -473,9 +505,9 @@ int32_t launch_rows(const PagedAttnParams &p, hipStream_t s) {
         static std::atomic<uint64_t> lds_ready{0};
         CASCADE_HIP_TRY(ensure_dynamic_lds((const void *)kern, sizeof(float) * 4 * TILE * (DM + 2), lds_ready));
         hipLaunchKernelGGL(kern, dim3((unsigned)g.pieces, p.Hkv), dim3(256), lds, s, p);
-        few_tiles = (unsigned)g.split_tiles;
+        merge_few = min((int64_t)1024, g.split_tiles * p.Hkv * (TILE / 4));
     }
-    hipLaunchKernelGGL((paged_merge_kernel<T, TILE, DM>), dim3(many_tiles + few_tiles, p.Hkv, max(2, TILE * DM / 2048)), dim3(256), 0, s, p, (int)many_tiles);
+    hipLaunchKernelGGL((paged_merge_kernel<T, TILE, DM>), dim3((unsigned)(merge_many + merge_few)), dim3(256), 0, s, p, (int)merge_many);
     CASCADE_HIP_TRY(hipGetLastError());
     return CASCADE_OK;
 }
@@ -529,7 +561,9 @@ int32_t check_attn(const cascade_paged_cache *c, const cascade_paged_attn_desc *
     if (d->n_heads % c->n_kv_heads) return CASCADE_ESHAPE;
     if (d->o_dtype != c->dtype && d->o_dtype != CASCADE_F32) return CASCADE_EUNSUPPORTED;
     const int64_t row = (int64_t)d->n_heads * c->head_dim;
-    if (row > INT32_MAX || (int64_t)d->rows * (d->n_heads / c->n_kv_heads) > INT32_MAX) return CASCADE_EUNSUPPORTED;
+    if (row > INT32_MAX || (int64_t)d->rows * (d->n_heads / c->n_kv_heads) > INT32_MAX ||
+        (int64_t)d->rows * c->n_shards > INT32_MAX / 4)
+        return CASCADE_EUNSUPPORTED;
     if ((d->q_stride && d->q_stride < row) || (d->o_stride && d->o_stride < row)) return CASCADE_ESHAPE;
     const int vec = c->dtype == CASCADE_BF16 ? 8 : 4, o_vec = d->o_dtype == CASCADE_BF16 ? 8 : 4;
     if (d->q_stride % vec || d->o_stride % o_vec) return CASCADE_EUNSUPPORTED;

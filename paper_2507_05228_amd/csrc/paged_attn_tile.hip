@@ -58,7 +58,9 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
     const bool second = wave >= NW / 2;                    // (the SIMD's other wavefront)
     const int g = blockIdx.y;
     PagedWork wk;
-    if (!paged_find_work<TILE, KEYS, false>(p, p.many, blockIdx.x, wk)) return;
+    PagedPlan<TILE, KEYS> plan;
+    plan.make(p, p.many);
+    if (!plan.template pick<false>(p, p.many, blockIdx.x, wk) || !wk.valid) return;
     const int64_t list0 = (int64_t)wk.b * p.S;
 
     // ---- keys of every shard that some row of the tile sees, and whether the lists name pages for them
