@@ -417,67 +417,86 @@ __global__ __launch_bounds__(256, rows_occupancy(sizeof(T), DM, RB)) void paged_
 }
 
 // Tiles whose walk was cut, of either kernel: their partials, weighted by exp2(m - largest m).  A wavefront takes a row at a
-// time, DM / 4 lanes its columns; the lane groups that are left take every SUB-th partial, eight requested at once, with a running
-// maximum each, and meet at the end.
-template <typename T, int TILE, int KEYS, int DM>
-__device__ __forceinline__ void merge_set(const PagedAttnParams &p, const PagedSet &set, int first, int stride) {
-    constexpr int LPR = DM / 4, SUB = 64 / LPR, AT_ONCE = 8;
-    PagedPlan<TILE, KEYS> plan;
-    plan.make(p, set);
-    const int lane = threadIdx.x & 63, sub = lane / LPR, c = lane % LPR * 4;
-    const int64_t step = (int64_t)p.Hkv * TILE;
-    // units: four rows of a tile and kv head
-    for (int unit = first;; unit += stride) {
-        const int quad = unit % (TILE / 4), rest = unit / (TILE / 4), w = (int)((uint32_t)rest / (uint32_t)p.Hkv), g = rest - w * p.Hkv;
-        PagedWork wk;
-        if (!plan.template pick<true>(p, set, w, wk)) return;
-        const int row = quad * 4 + (threadIdx.x >> 6), r = wk.tile * TILE + row;
-        if (!wk.valid || r >= wk.n_rows) continue;
-        const int64_t at = ((int64_t)wk.first_piece * p.Hkv + g) * TILE + row;
-        const float2 *ml = (const float2 *)set.part_ml + at;
-        const float *pu = set.part_u + at * p.d + (c < p.d ? c : 0);
-        float top = -INFINITY, sum = 0.f;
-        f32x4 u = {0.f, 0.f, 0.f, 0.f};
-        for (int i0 = sub; i0 < wk.n_pieces; i0 += SUB * AT_ONCE) {
-            float2 a[AT_ONCE];
-            f32x4 x[AT_ONCE];
+// time (four where there are few partials), DM / 4 lanes its columns; the lane groups that are left take every SUB-th partial, with a
+// running maximum each, and meet at the end.
+// ROWS rows at once, AT_ONCE partials of each requested at once.
+template <typename T, int TILE, int DM, int ROWS, int AT_ONCE>
+__device__ __forceinline__ void merge_rows(const PagedAttnParams &p, const PagedSet &set, const PagedWork &wk, int g, int row0) {
+    constexpr int LPR = DM / 4, SUB = 64 / LPR;
+    const int lane = threadIdx.x & 63, sub = lane / LPR, c = lane % LPR * 4, tile0 = wk.tile * TILE;
+    const int64_t step = (int64_t)p.Hkv * TILE, at0 = ((int64_t)wk.first_piece * p.Hkv + g) * TILE;
+    float top[ROWS], sum[ROWS];
+    f32x4 u[ROWS];
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) { top[k] = -INFINITY; sum[k] = 0.f; u[k] = f32x4{0.f, 0.f, 0.f, 0.f}; }
+    for (int i0 = sub; i0 < wk.n_pieces; i0 += SUB * AT_ONCE) {
+        float2 a[ROWS][AT_ONCE];
+        f32x4 x[ROWS][AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k)
 #pragma unroll
             for (int j = 0; j < AT_ONCE; ++j) {
-                const int64_t i = min(i0 + j * SUB, wk.n_pieces - 1) * step;
-                a[j] = ml[i];
-                x[j] = *(const f32x4 *)(pu + i * p.d);
+                // (rows behind the last: that one again, not written)
+                const int64_t at = at0 + min(row0 + 4 * k, wk.n_rows - 1 - tile0) + min(i0 + j * SUB, wk.n_pieces - 1) * step;
+                a[k][j] = ((const float2 *)set.part_ml)[at];
+                x[k][j] = *(const f32x4 *)(set.part_u + at * p.d + (c < p.d ? c : 0));
             }
-            float most = top;
 #pragma unroll
-            for (int j = 0; j < AT_ONCE; ++j) most = fmaxf(most, a[j].x);      // (a repeated one changes nothing)
-            const float off = most == -INFINITY ? 0.f : most, f = __builtin_amdgcn_exp2f(top - off);
-            top = most;
-            sum *= f;
-            u *= f;
+        for (int k = 0; k < ROWS; ++k) {
+            float most = top[k];
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j) most = fmaxf(most, a[k][j].x);   // (a repeated one changes nothing)
+            const float off = most == -INFINITY ? 0.f : most, f = __builtin_amdgcn_exp2f(top[k] - off);
+            top[k] = most;
+            sum[k] *= f;
+            u[k] *= f;
 #pragma unroll
             for (int j = 0; j < AT_ONCE; ++j) {
                 if (i0 + j * SUB >= wk.n_pieces) break;
-                const float e = __builtin_amdgcn_exp2f(a[j].x - off);
-                sum += a[j].y * e;
-                u += x[j] * e;
+                const float e = __builtin_amdgcn_exp2f(a[k][j].x - off);
+                sum[k] += a[k][j].y * e;
+                u[k] += x[k][j] * e;
             }
         }
+    }
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) {
 #pragma unroll
         for (int o = LPR; o < 64; o <<= 1) {               // the lane groups' states
-            const float other = __shfl_xor(top, o, WAVE), most = fmaxf(top, other), off = most == -INFINITY ? 0.f : most;
-            const float f = __builtin_amdgcn_exp2f(top - off), f1 = __builtin_amdgcn_exp2f(other - off);
-            sum = sum * f + __shfl_xor(sum, o, WAVE) * f1;
+            const float other = __shfl_xor(top[k], o, WAVE), most = fmaxf(top[k], other), off = most == -INFINITY ? 0.f : most;
+            const float f = __builtin_amdgcn_exp2f(top[k] - off), f1 = __builtin_amdgcn_exp2f(other - off);
+            sum[k] = sum[k] * f + __shfl_xor(sum[k], o, WAVE) * f1;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) u[j] = u[j] * f + __shfl_xor(u[j], o, WAVE) * f1;
-            top = most;
+            for (int j = 0; j < 4; ++j) u[k][j] = u[k][j] * f + __shfl_xor(u[k][j], o, WAVE) * f1;
+            top[k] = most;
         }
-        if (sub || c >= p.d) continue;
+        const int r = tile0 + row0 + 4 * k;
+        if (sub || c >= p.d || r >= wk.n_rows) continue;
         const int t = (int)((uint32_t)r / (uint32_t)p.rep), h = g * p.rep + r - t * p.rep;
         const int64_t out = (int64_t)(wk.first_row + t) * p.o_stride + (int64_t)h * p.d + c;
-        u *= sum == 0.f ? 0.f : 1.0f / sum;
-        if (sizeof(T) == 4 || p.o_f32) *(f32x4 *)((float *)p.o + out) = u;
-        else *(bf16x4 *)((bf16_t *)p.o + out) = bf16x4{(bf16_t)u[0], (bf16_t)u[1], (bf16_t)u[2], (bf16_t)u[3]};
-        if (c == 0 && p.lse) p.lse[(int64_t)h * p.rows + wk.first_row + t] = (top + __builtin_log2f(sum)) * LN2F;
+        u[k] *= sum[k] == 0.f ? 0.f : 1.0f / sum[k];
+        if (sizeof(T) == 4 || p.o_f32) *(f32x4 *)((float *)p.o + out) = u[k];
+        else *(bf16x4 *)((bf16_t *)p.o + out) = bf16x4{(bf16_t)u[k][0], (bf16_t)u[k][1], (bf16_t)u[k][2], (bf16_t)u[k][3]};
+        if (c == 0 && p.lse) p.lse[(int64_t)h * p.rows + wk.first_row + t] = (top[k] + __builtin_log2f(sum[k])) * LN2F;
+    }
+}
+template <typename T, int TILE, int KEYS, int DM>
+__device__ __forceinline__ void merge_set(const PagedAttnParams &p, const PagedSet &set, int first, int stride) {
+    constexpr int SUB = 256 / DM, UNITS = TILE / 16;
+    PagedPlan<TILE, KEYS> plan;
+    plan.make(p, set);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // units: 16 rows of a tile and kv head, every fourth one a wavefront's
+    for (int unit = first;; unit += stride) {
+        const int part = unit % UNITS, rest = unit / UNITS, w = (int)((uint32_t)rest / (uint32_t)p.Hkv), g = rest - w * p.Hkv;
+        PagedWork wk;
+        if (!plan.template pick<true>(p, set, w, wk)) return;
+        const int left = wk.n_rows - wk.tile * TILE - part * 16;       // rows of the unit that exist
+        if (!wk.valid || left <= wave) continue;
+        const int row0 = part * 16 + wave;
+        if (wk.n_pieces <= 2 * SUB && left > 4) merge_rows<T, TILE, DM, 4, 2>(p, set, wk, g, row0);
+        else
+            for (int k = 0; k < 16 && wave + k < left; k += 4) merge_rows<T, TILE, DM, 1, 8>(p, set, wk, g, row0 + k);
     }
 }
 template <typename T, int TILE, int DM>
@@ -496,7 +515,7 @@ int32_t launch_rows(const PagedAttnParams &p, hipStream_t s) {
     if (p.many.target) {
         const int32_t st = launch_paged_tile(p, s);
         if (st != CASCADE_OK) return st;
-        merge_many = min((int64_t)1024, paged_grid(p, p.many, PAGED_TILE).split_tiles * p.Hkv * (PAGED_TILE / 4));
+        merge_many = min((int64_t)1024, paged_grid(p, p.many, PAGED_TILE).split_tiles * p.Hkv * (PAGED_TILE / 16));
     }
     if (p.few.target) {
         const PagedGrid g = paged_grid(p, p.few, TILE);
@@ -505,7 +524,7 @@ int32_t launch_rows(const PagedAttnParams &p, hipStream_t s) {
         static std::atomic<uint64_t> lds_ready{0};
         CASCADE_HIP_TRY(ensure_dynamic_lds((const void *)kern, sizeof(float) * 4 * TILE * (DM + 2), lds_ready));
         hipLaunchKernelGGL(kern, dim3((unsigned)g.pieces, p.Hkv), dim3(256), lds, s, p);
-        merge_few = min((int64_t)1024, g.split_tiles * p.Hkv * (TILE / 4));
+        merge_few = min((int64_t)1024, g.split_tiles * p.Hkv * (TILE / 16));
     }
     hipLaunchKernelGGL((paged_merge_kernel<T, TILE, DM>), dim3((unsigned)(merge_many + merge_few)), dim3(256), 0, s, p, (int)merge_many);
     CASCADE_HIP_TRY(hipGetLastError());
@@ -526,6 +545,8 @@ int32_t launch_type(const PagedAttnParams &p, hipStream_t s) {
 
 // Sizes, and which sequences go to which kernel: bf16 with head dimensions of 64 and 128 has paged_attn_tile.hip for the
 // sequences of many rows, if the rows at hand can make one; with a single sequence it takes that with however many rows it has.
+// With no more rows than sequences it is left out (one token each, most likely; its launch costs 4 us for nothing then, and a
+// sequence that has several all the same is taken by the other kernel).
 void set_sizes(PagedAttnParams &p, const cascade_paged_cache *c, const cascade_paged_attn_desc *d) {
     p.rows = d->rows; p.H = d->n_heads; p.Hkv = c->n_kv_heads; p.rep = p.H / p.Hkv; p.d = c->head_dim;
     p.S = c->n_shards; p.B = c->n_seqs; p.max_pages = c->max_pages; p.page_shift = page_shift(c); p.n_pages = c->n_pages;
@@ -535,7 +556,7 @@ void set_sizes(PagedAttnParams &p, const cascade_paged_cache *c, const cascade_p
         x.inv_target = 1.0f / x.target;
         x.min_steps = 4;
     };
-    const bool tiles = c->dtype == CASCADE_BF16 && (p.d == 64 || p.d == 128) && (int64_t)p.rows * p.rep > PAGED_FEW;
+    const bool tiles = c->dtype == CASCADE_BF16 && (p.d == 64 || p.d == 128) && (int64_t)p.rows * p.rep > PAGED_FEW && (p.B == 1 || p.rows > p.B);
     if (tiles) set(p.many, p.B == 1 ? 0 : PAGED_FEW, INT32_MAX, PAGED_TILE_TARGET);
     if (!tiles || p.B > 1) set(p.few, 0, tiles ? PAGED_FEW : INT32_MAX, PAGED_FEW_TARGET);
 }
