@@ -33,9 +33,8 @@ struct PagedAttnParams {
     PagedSet few, many;                                    // paged_attn_rows.hip, paged_attn_tile.hip
 };
 
-constexpr int PAGED_FEW_TARGET = 512;                      // pieces of a launch, all kv heads together
 constexpr int PAGED_TILE = 256, PAGED_TILE_KEYS = 64, PAGED_TILE_TARGET = 256;      // paged_attn_tile.hip: rows of a tile, keys of a step; pieces
-constexpr int PAGED_FEW = 32;                              // flattened rows of a sequence up to which it goes to paged_attn_rows.hip
+constexpr int PAGED_FEW = 256;                             // flattened rows of a sequence up to which it goes to paged_attn_rows.hip
 
 struct PagedWork {
     int b, first_row, n_rows;                              // sequence, its first row in q, its flattened rows

@@ -19,6 +19,7 @@
 namespace {
 
 constexpr float RAISE = 8.0f;
+constexpr int FEW_TILES = 8;                               // up to which a merge has a workgroup for a row
 
 template <typename T> struct Kind;
 template <> struct Kind<bf16_t> {
@@ -499,6 +500,92 @@ __device__ __forceinline__ void merge_set(const PagedAttnParams &p, const PagedS
             for (int k = 0; k < 16 && wave + k < left; k += 4) merge_rows<T, TILE, DM, 1, 8>(p, set, wk, g, row0 + k);
     }
 }
+// Few tiles, cut into many pieces: a workgroup to a row, its wavefronts a quarter of the partials each.
+template <typename T, int TILE, int KEYS, int DM>
+__device__ __forceinline__ void merge_set_by_workgroups(const PagedAttnParams &p, const PagedSet &set) {
+    constexpr int LPR = DM / 4, SUB = 64 / LPR, AT_ONCE = 8, GROUPS = 4 * SUB;
+    __shared__ float state[4][DM + 2];
+    PagedPlan<TILE, KEYS> plan;
+    plan.make(p, set);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane % LPR * 4;
+    const int group = wave * SUB + lane / LPR;
+    const int64_t step = (int64_t)p.Hkv * TILE;
+    for (int unit = blockIdx.x;; unit += gridDim.x) {
+        const int row = unit % TILE, rest = unit / TILE, w = (int)((uint32_t)rest / (uint32_t)p.Hkv), g = rest - w * p.Hkv;
+        PagedWork wk;
+        if (!plan.template pick<true>(p, set, w, wk)) return;
+        const int r = wk.tile * TILE + row;
+        if (!wk.valid || r >= wk.n_rows) continue;         // (the same for the whole workgroup)
+        const int64_t at0 = ((int64_t)wk.first_piece * p.Hkv + g) * TILE + row;
+        float top = -INFINITY, sum = 0.f;
+        f32x4 u = {0.f, 0.f, 0.f, 0.f};
+        for (int i0 = group; i0 < wk.n_pieces; i0 += GROUPS * AT_ONCE) {
+            float2 a[AT_ONCE];
+            f32x4 x[AT_ONCE];
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j) {
+                const int64_t at = at0 + min(i0 + j * GROUPS, wk.n_pieces - 1) * step;
+                a[j] = ((const float2 *)set.part_ml)[at];
+                x[j] = *(const f32x4 *)(set.part_u + at * p.d + (c < p.d ? c : 0));
+            }
+            float most = top;
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j) most = fmaxf(most, a[j].x);
+            const float off = most == -INFINITY ? 0.f : most, f = __builtin_amdgcn_exp2f(top - off);
+            top = most;
+            sum *= f;
+            u *= f;
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j) {
+                if (i0 + j * GROUPS >= wk.n_pieces) break;
+                const float e = __builtin_amdgcn_exp2f(a[j].x - off);
+                sum += a[j].y * e;
+                u += x[j] * e;
+            }
+        }
+#pragma unroll
+        for (int o = LPR; o < 64; o <<= 1) {
+            const float other = __shfl_xor(top, o, WAVE), most = fmaxf(top, other), off = most == -INFINITY ? 0.f : most;
+            const float f = __builtin_amdgcn_exp2f(top - off), f1 = __builtin_amdgcn_exp2f(other - off);
+            sum = sum * f + __shfl_xor(sum, o, WAVE) * f1;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) u[j] = u[j] * f + __shfl_xor(u[j], o, WAVE) * f1;
+            top = most;
+        }
+        __syncthreads();                                   // (the last row's states have been read)
+        if (lane < LPR) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) state[wave][c + j] = u[j];
+            if (lane == 0) { state[wave][DM] = top; state[wave][DM + 1] = sum; }
+        }
+        __syncthreads();
+        if (wave || lane >= LPR || c >= p.d) continue;
+        float most = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) most = fmaxf(most, state[k][DM]);
+        const float off = most == -INFINITY ? 0.f : most;
+        sum = 0.f;
+        u = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float f = __builtin_amdgcn_exp2f(state[k][DM] - off);
+            sum += state[k][DM + 1] * f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) u[j] += state[k][c + j] * f;
+        }
+        const int t = (int)((uint32_t)r / (uint32_t)p.rep), h = g * p.rep + r - t * p.rep;
+        const int64_t out = (int64_t)(wk.first_row + t) * p.o_stride + (int64_t)h * p.d + c;
+        u *= sum == 0.f ? 0.f : 1.0f / sum;
+        if (sizeof(T) == 4 || p.o_f32) *(f32x4 *)((float *)p.o + out) = u;
+        else *(bf16x4 *)((bf16_t *)p.o + out) = bf16x4{(bf16_t)u[0], (bf16_t)u[1], (bf16_t)u[2], (bf16_t)u[3]};
+        if (c == 0 && p.lse) p.lse[(int64_t)h * p.rows + wk.first_row + t] = (most + __builtin_log2f(sum)) * LN2F;
+    }
+}
+template <typename T, int TILE, int DM>
+__global__ __launch_bounds__(256) void paged_merge_few_kernel(PagedAttnParams p) {
+    merge_set_by_workgroups<T, TILE, 32, DM>(p, p.few);
+}
+
 template <typename T, int TILE, int DM>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnParams p, int for_many) {
     if constexpr (sizeof(T) == 2 && DM <= 128) {
@@ -524,6 +611,11 @@ int32_t launch_rows(const PagedAttnParams &p, hipStream_t s) {
         static std::atomic<uint64_t> lds_ready{0};
         CASCADE_HIP_TRY(ensure_dynamic_lds((const void *)kern, sizeof(float) * 4 * TILE * (DM + 2), lds_ready));
         hipLaunchKernelGGL(kern, dim3((unsigned)g.pieces, p.Hkv), dim3(256), lds, s, p);
+        if (!p.many.target && g.split_tiles <= FEW_TILES) {
+            hipLaunchKernelGGL((paged_merge_few_kernel<T, TILE, DM>), dim3((unsigned)min((int64_t)2048, g.split_tiles * p.Hkv * TILE)), dim3(256), 0, s, p);
+            CASCADE_HIP_TRY(hipGetLastError());
+            return CASCADE_OK;
+        }
         merge_few = min((int64_t)1024, g.split_tiles * p.Hkv * (TILE / 16));
     }
     hipLaunchKernelGGL((paged_merge_kernel<T, TILE, DM>), dim3((unsigned)(merge_many + merge_few)), dim3(256), 0, s, p, (int)merge_many);
@@ -543,22 +635,24 @@ int32_t launch_type(const PagedAttnParams &p, hipStream_t s) {
     return p.d <= 64 ? launch_dim<T, 64>(p, s) : p.d <= 128 ? launch_dim<T, 128>(p, s) : launch_dim<T, 256>(p, s);
 }
 
-// Sizes, and which sequences go to which kernel: bf16 with head dimensions of 64 and 128 has paged_attn_tile.hip for the
+// Sizes, and which sequences go to which kernel; as many pieces as workgroups are resident at once (32 / 8 heads of 128, one token
+// of 32 sequences of 1650 to 8200 keys, three workgroups a CU: 256, 512, 768, 1024 pieces 171, 129, 126, 125 us; 8 sequences of 4096:
+// 34, 32.5, 30, 33; five tokens, two workgroups a CU: 35.6, 36, 42.5, 45): bf16 with head dimensions of 64 and 128 has paged_attn_tile.hip for the
 // sequences of many rows, if the rows at hand can make one; with a single sequence it takes that with however many rows it has.
 // With no more rows than sequences it is left out (one token each, most likely; its launch costs 4 us for nothing then, and a
 // sequence that has several all the same is taken by the other kernel).
 void set_sizes(PagedAttnParams &p, const cascade_paged_cache *c, const cascade_paged_attn_desc *d) {
     p.rows = d->rows; p.H = d->n_heads; p.Hkv = c->n_kv_heads; p.rep = p.H / p.Hkv; p.d = c->head_dim;
     p.S = c->n_shards; p.B = c->n_seqs; p.max_pages = c->max_pages; p.page_shift = page_shift(c); p.n_pages = c->n_pages;
-    auto set = [&](PagedSet &x, int32_t above, int32_t upto, int target) {
+    auto set = [&](PagedSet &x, int32_t above, int32_t upto, int target, int min_steps) {
         x.above = above; x.upto = upto;
         x.target = max(1, target / p.Hkv);
         x.inv_target = 1.0f / x.target;
-        x.min_steps = 4;
+        x.min_steps = min_steps;
     };
     const bool tiles = c->dtype == CASCADE_BF16 && (p.d == 64 || p.d == 128) && (int64_t)p.rows * p.rep > PAGED_FEW && (p.B == 1 || p.rows > p.B);
-    if (tiles) set(p.many, p.B == 1 ? 0 : PAGED_FEW, INT32_MAX, PAGED_TILE_TARGET);
-    if (!tiles || p.B > 1) set(p.few, 0, tiles ? PAGED_FEW : INT32_MAX, PAGED_FEW_TARGET);
+    if (tiles) set(p.many, p.B == 1 ? 0 : PAGED_FEW, INT32_MAX, PAGED_TILE_TARGET, 4);
+    if (!tiles || p.B > 1) set(p.few, 0, tiles ? PAGED_FEW : INT32_MAX, 256 * rows_occupancy(c->dtype == CASCADE_BF16 ? 2 : 4, p.d, rows_tile(p) / 16), 8);
 }
 size_t set_parts(PagedAttnParams &p, float *workspace) {
     size_t floats = 0;
