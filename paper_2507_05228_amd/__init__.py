@@ -577,20 +577,34 @@ def make_rope_desc(rot_dim, theta, layout=ROPE_HALF, scaling=ROPE_UNSCALED, fact
     return RopeDesc(layout, rot_dim, scaling, original_len, theta, factor, low, high, amplitude)
 
 
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def _on(stream, t):
+    """The stream's handle as a number (of the current stream: 0.3 us instead of 3 for a stream object); t, a tensor of the call,
+    must be on the current device, where the kernels will run."""
+    import torch
+    device = torch.cuda.current_device()
+    if t.get_device() != device:
+        raise CascadeError(EINVAL, f"a tensor on device {t.get_device()}, the current device is {device}")
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+
+
 def _head_rows(t, where):
     """Row stride of a [rows, heads, d] tensor whose heads lie back to back."""
     if t.dim() == 3:
         (rows, heads, d), (sr, sh, sd) = t.shape, t.stride()
-        if sd == 1 and (heads < 2 or sh == d):
+        if sd == 1 and (heads < 2 or sh == d) and t.is_cuda:
             return sr if rows > 1 else heads * d
-    raise CascadeError(ESHAPE, f"{where}: [rows, heads, d] with dense heads")
+    raise CascadeError(ESHAPE, f"{where}: [rows, heads, d] with dense heads, on the GPU")
 
 
-def _checked(where, dtype, **tensors):
-    """Tensors of a call that are contiguous, on the GPU, and of the given type (None passes)."""
-    for name, t in tensors.items():
-        if t is not None and (t.dtype != dtype or not t.is_contiguous() or not t.is_cuda):
-            raise CascadeError(ESHAPE, f"{where}: {name} must be a contiguous {dtype} tensor on the GPU")
+def _checked(where, dtype, *tensors):
+    """Tensors of a call: contiguous, on the GPU, and of the given type (None passes)."""
+    for t in tensors:
+        if t is not None and not (t.dtype == dtype and t.is_cuda and t.is_contiguous()):
+            raise CascadeError(ESHAPE, f"{where}: contiguous {dtype} tensors on the GPU")
 
 
 def _counted(where, *checks):
@@ -604,11 +618,11 @@ def cascade_rope(desc, x, positions, y=None, stream=None):
     import torch
     lib = load_library()
     y = x if y is None else y
-    _checked("cascade_rope", torch.int32, positions=positions)
+    _checked("cascade_rope", torch.int32, positions)
     _counted("cascade_rope", (x.dim() == 3 and y.shape == x.shape and y.dtype == x.dtype, "y like x"),
              (positions is None or positions.numel() == x.shape[0], "a position per row"))
-    st = lib.cascade_rope(C.byref(desc), _dtype_code(x), x.shape[0], x.shape[1], x.shape[2], _ptr(positions), _ptr(x),
-                          _head_rows(x, "cascade_rope"), _ptr(y), _head_rows(y, "cascade_rope"), _stream(stream))
+    st = lib.cascade_rope(C.byref(desc), _dtype_code(x), x.shape[0], x.shape[1], x.shape[2], _at(positions), _at(x),
+                          _head_rows(x, "cascade_rope"), _at(y), _head_rows(y, "cascade_rope"), _on(stream, x))
     _check(st, "cascade_rope")
 
 
@@ -616,8 +630,8 @@ def make_paged_cache(k_pages, v_pages, page_table, kv_len, page_refs):
     """PagedCache of k_pages, v_pages [layers, pages, Hkv, page_size, d], page_table int32 [seqs, shards, max_pages], kv_len
     int32 [seqs, shards] and page_refs int32 [pages].  The cache keeps the tensors alive."""
     import torch
-    _checked("make_paged_cache", k_pages.dtype, k_pages=k_pages, v_pages=v_pages)
-    _checked("make_paged_cache", torch.int32, page_table=page_table, kv_len=kv_len, page_refs=page_refs)
+    _checked("make_paged_cache", k_pages.dtype, k_pages, v_pages)
+    _checked("make_paged_cache", torch.int32, page_table, kv_len, page_refs)
     _counted("make_paged_cache", (k_pages.dim() == 5 and v_pages.shape == k_pages.shape, "k_pages, v_pages [layers, pages, Hkv, page_size, d]"),
              (page_table.dim() == 3 and kv_len.shape == page_table.shape[:2], "page_table [seqs, shards, max_pages], kv_len [seqs, shards]"),
              (page_refs.shape == k_pages.shape[1:2], "page_refs [pages]"))
@@ -632,13 +646,13 @@ def cascade_paged_extend(cache, q_start, slots, visible, accepted, row_shard=Non
     """q_start int32 [seqs + 1]; slots int32 [rows], visible int32 [rows, shards], accepted int32 [seqs] are written."""
     import torch
     lib = load_library()
-    _checked("cascade_paged_extend", torch.int32, q_start=q_start, slots=slots, visible=visible, accepted=accepted, row_shard=row_shard)
+    _checked("cascade_paged_extend", torch.int32, q_start, slots, visible, accepted, row_shard)
     rows = slots.numel()
     _counted("cascade_paged_extend", (q_start.numel() == cache.n_seqs + 1, "q_start [seqs + 1]"),
              (visible.numel() == rows * cache.n_shards, "visible [rows, shards]"), (accepted.numel() == cache.n_seqs, "accepted [seqs]"),
              (row_shard is None or row_shard.numel() == rows, "row_shard [rows]"))
-    _check(lib.cascade_paged_extend(C.byref(cache), rows, _ptr(q_start), _ptr(row_shard), _ptr(slots), _ptr(visible), _ptr(accepted),
-                                    _stream(stream)), "cascade_paged_extend")
+    _check(lib.cascade_paged_extend(C.byref(cache), rows, _at(q_start), _at(row_shard), _at(slots), _at(visible), _at(accepted),
+                                    _on(stream, slots)), "cascade_paged_extend")
 
 
 def cascade_paged_append(cache, layer, slots, k, v, positions=None, rope=None, q=None, q_out=None, stream=None):
@@ -646,7 +660,7 @@ def cascade_paged_append(cache, layer, slots, k, v, positions=None, rope=None, q
     import torch
     lib = load_library()
     where = "cascade_paged_append"
-    _checked(where, torch.int32, slots=slots, positions=positions)
+    _checked(where, torch.int32, slots, positions)
     rows = slots.numel()
     _counted(where, (k.dim() == 3 and k.shape == v.shape == (rows, cache.n_kv_heads, cache.head_dim), "k, v [rows, Hkv, d]"),
              (_dtype_code(k) == _dtype_code(v) == cache.dtype, "k, v of the cache's type"),
@@ -659,9 +673,9 @@ def cascade_paged_append(cache, layer, slots, k, v, positions=None, rope=None, q
         _counted(where, (q.dim() == 3 and q.shape[0] == rows and q.shape[2] == cache.head_dim and q_out.shape == q.shape, "q, q_out [rows, H, d]"),
                  (_dtype_code(q) == _dtype_code(q_out) == cache.dtype, "q, q_out of the cache's type"))
         heads, qs, qos = q.shape[1], _head_rows(q, where), _head_rows(q_out, where)
-    st = lib.cascade_paged_append(C.byref(cache), layer, rows, _ptr(slots), _ptr(k), _ptr(v), _head_rows(k, where),
-                                  None if rope is None else C.byref(rope), _ptr(positions), heads, _ptr(q), qs, _ptr(q_out), qos,
-                                  _stream(stream))
+    st = lib.cascade_paged_append(C.byref(cache), layer, rows, _at(slots), _at(k), _at(v), _head_rows(k, where),
+                                  None if rope is None else C.byref(rope), _at(positions), heads, _at(q), qs, _at(q_out), qos,
+                                  _on(stream, slots))
     _check(st, where)
 
 
@@ -676,16 +690,16 @@ def cascade_paged_attn(cache, layer, q, o, q_start, scale, visible=None, lse=Non
     import torch
     lib = load_library()
     where = "cascade_paged_attn"
-    _checked(where, torch.int32, q_start=q_start, visible=visible)
-    _checked(where, torch.float32, lse=lse)
+    _checked(where, torch.int32, q_start, visible)
+    _checked(where, torch.float32, lse)
     _counted(where, (q.dim() == 3 and q.shape[2] == cache.head_dim and o.shape == q.shape, "q, o [rows, H, d]"),
              (_dtype_code(q) == cache.dtype, "q of the cache's type"), (q_start.numel() == cache.n_seqs + 1, "q_start [seqs + 1]"),
              (visible is None or visible.numel() == q.shape[0] * cache.n_shards, "visible [rows, shards]"),
              (lse is None or lse.numel() == q.shape[0] * q.shape[1], "lse [H, rows]"))
     desc = PagedAttnDesc(q.shape[0], q.shape[1], scale, _dtype_code(o), _head_rows(q, where), _head_rows(o, where))
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    st = lib.cascade_paged_attn(C.byref(cache), layer, C.byref(desc), _ptr(q_start), _ptr(visible), _ptr(q), _ptr(o), _ptr(lse),
-                                _ptr(workspace), ws_bytes, _stream(stream))
+    st = lib.cascade_paged_attn(C.byref(cache), layer, C.byref(desc), _at(q_start), _at(visible), _at(q), _at(o), _at(lse),
+                                _at(workspace), ws_bytes, _on(stream, q))
     _check(st, where)
 
 
@@ -693,8 +707,8 @@ def cascade_pages_free(cache, seqs, stream=None):
     """seqs int32 [n]."""
     import torch
     lib = load_library()
-    _checked("cascade_pages_free", torch.int32, seqs=seqs)
-    _check(lib.cascade_pages_free(C.byref(cache), seqs.numel(), _ptr(seqs), _stream(stream)), "cascade_pages_free")
+    _checked("cascade_pages_free", torch.int32, seqs)
+    _check(lib.cascade_pages_free(C.byref(cache), seqs.numel(), _at(seqs), _on(stream, seqs)), "cascade_pages_free")
 
 
 def cascade_pages_workspace_bytes(cache):
@@ -705,29 +719,29 @@ def cascade_pages_fork(cache, src, dst, accepted, workspace, stream=None):
     """src, dst, accepted int32 [n]."""
     import torch
     lib = load_library()
-    _checked("cascade_pages_fork", torch.int32, src=src, dst=dst, accepted=accepted)
+    _checked("cascade_pages_fork", torch.int32, src, dst, accepted)
     _counted("cascade_pages_fork", (src.numel() == dst.numel() == accepted.numel(), "src, dst, accepted [n]"))
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib.cascade_pages_fork(C.byref(cache), src.numel(), _ptr(src), _ptr(dst), _ptr(accepted), _ptr(workspace), ws_bytes,
-                                  _stream(stream)), "cascade_pages_fork")
+    _check(lib.cascade_pages_fork(C.byref(cache), src.numel(), _at(src), _at(dst), _at(accepted), _at(workspace), ws_bytes,
+                                  _on(stream, src)), "cascade_pages_fork")
 
 
 def cascade_pages_compact(cache, n_live, workspace, stream=None):
     """n_live int32 [1] or None."""
     import torch
     lib = load_library()
-    _checked("cascade_pages_compact", torch.int32, n_live=n_live)
+    _checked("cascade_pages_compact", torch.int32, n_live)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib.cascade_pages_compact(C.byref(cache), _ptr(n_live), _ptr(workspace), ws_bytes, _stream(stream)), "cascade_pages_compact")
+    _check(lib.cascade_pages_compact(C.byref(cache), _at(n_live), _at(workspace), ws_bytes, _on(stream, cache.tensors[0])), "cascade_pages_compact")
 
 
 def cascade_pages_copy(cache, src, dst, stream=None):
     """src, dst int32 [n]."""
     import torch
     lib = load_library()
-    _checked("cascade_pages_copy", torch.int32, src=src, dst=dst)
+    _checked("cascade_pages_copy", torch.int32, src, dst)
     _counted("cascade_pages_copy", (src.numel() == dst.numel(), "src, dst [n]"))
-    _check(lib.cascade_pages_copy(C.byref(cache), src.numel(), _ptr(src), _ptr(dst), _stream(stream)), "cascade_pages_copy")
+    _check(lib.cascade_pages_copy(C.byref(cache), src.numel(), _at(src), _at(dst), _on(stream, src)), "cascade_pages_copy")
 
 
 def cascade_mfma_ceiling(lds_operands, iters=200000, stream=None):

@@ -52,23 +52,50 @@ __device__ __forceinline__ int32_t list_len(const Lists &l, int64_t list) {
 }
 __device__ __forceinline__ int32_t pages_of(const Lists &l, int32_t rows) { return (rows + (1 << l.page_shift) - 1) >> l.page_shift; }
 
-__device__ int32_t count_free(const Lists &l, int32_t *scratch, int &flip) {
-    int32_t mine = 0, total;
-    for (int p = threadIdx.x; p < l.n_pages; p += WG) mine += l.refs[p] == 0;
+__device__ __forceinline__ int32_t block_max(int32_t v, int32_t *scratch, int &flip) {     // of values from 0 on
+    int32_t *part = scratch + flip * WAVES, top = 0;
+    flip ^= 1;
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v = max(v, __shfl_xor(v, o, WAVE));
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) top = max(top, part[w]);
+    return top;
+}
+// The slot of a row of a list; -1 where the list has no page for it
+__device__ __forceinline__ int32_t slot_of(const Lists &l, int64_t list, int32_t row) {
+    if ((uint32_t)row >= (uint32_t)(l.max_pages << l.page_shift)) return -1;
+    const int32_t page = l.table[list * l.max_pages + (row >> l.page_shift)];
+    return (uint32_t)page < (uint32_t)l.n_pages ? (page << l.page_shift) + (row & ((1 << l.page_shift) - 1)) : -1;
+}
+
+// Bit i: page p0 + i is free
+__device__ __forceinline__ uint32_t free_mask(const Lists &l, int64_t p0) {
+    uint32_t free = 0;
+#pragma unroll
+    for (int i = 0; i < REFS_PER_THREAD; ++i)
+        if (p0 + i < l.n_pages && l.refs[p0 + i] == 0) free |= 1u << i;
+    return free;
+}
+// `head`: the mask of this thread's first pages, which take_free can have again (few pools have more than WG * REFS_PER_THREAD)
+__device__ int32_t count_free(const Lists &l, uint32_t &head, int32_t *scratch, int &flip) {
+    head = free_mask(l, (int64_t)threadIdx.x * REFS_PER_THREAD);
+    int32_t mine = __popc(head), total;
+    for (int64_t base = WG * REFS_PER_THREAD; base < l.n_pages; base += WG * REFS_PER_THREAD)
+        mine += __popc(free_mask(l, base + (int64_t)threadIdx.x * REFS_PER_THREAD));
     block_scan(mine, scratch, flip, total);
     return total;
 }
 
-// take(page, rank) for the `wanted` lowest free pages (at least so many are free), whose references become 1
+// take(page, rank) for the `wanted` lowest free pages (at least so many are free), whose references become 1.
+// again: head is the mask of this thread's first pages as they are
 template <typename F>
-__device__ void take_free(const Lists &l, int32_t wanted, int32_t *scratch, int &flip, F take) {
+__device__ void take_free(const Lists &l, int32_t wanted, bool again, uint32_t head, int32_t *scratch, int &flip, F take) {
     int32_t rank0 = 0;
     for (int64_t base = 0; base < l.n_pages && rank0 < wanted; base += WG * REFS_PER_THREAD) {
         const int64_t p0 = base + (int64_t)threadIdx.x * REFS_PER_THREAD;
-        uint32_t free = 0;
-#pragma unroll
-        for (int i = 0; i < REFS_PER_THREAD; ++i)
-            if (p0 + i < l.n_pages && l.refs[p0 + i] == 0) free |= 1u << i;
+        const uint32_t free = base == 0 && again ? head : free_mask(l, p0);
         int32_t total, rank = rank0 + block_scan(__popc(free), scratch, flip, total);
 #pragma unroll
         for (int i = 0; i < REFS_PER_THREAD; ++i) {
@@ -110,53 +137,49 @@ struct ExtendParams {
     const int32_t *q_start, *row_shard;
     int32_t *slots, *visible, *accepted;
     int32_t rows, seqs_per_round;
+    int32_t rows_here;                                     // the rows' slots and limits in this launch (one shard only)
 };
+__device__ __forceinline__ int32_t start_of(const ExtendParams &p, int b) { return min(max(p.q_start[b], 0), p.rows); }
 
+// Pages, lists and lengths, by one workgroup; sequences in rounds of as many as LDS has words for.
 __global__ __launch_bounds__(WG) void paged_extend_kernel(ExtendParams p) {
     extern __shared__ int32_t smem[];
     const Lists &l = p.l;
     const int S = l.n_shards, tid = threadIdx.x;
     const int round_lists = p.seqs_per_round * S;
     int32_t *count = smem, *first = count + round_lists;   // new rows of a list; rank of its first new page
-    int32_t *before = first + round_lists;                 // rows of the list's shard in the round before its sequence
-    int32_t *ok = before + round_lists;                    // per sequence
-    int32_t *part = ok + p.seqs_per_round;                 // [WAVES][S] rows of each shard in a wavefront's 64
+    int32_t *len = first + round_lists, *ok = len + round_lists;   // its rows so far; per sequence
+    int32_t *start = ok + p.seqs_per_round;                // first row of every sequence, and of the one behind
     __shared__ int32_t scratch[2 * WAVES];
     int flip = 0;
-    auto start_of = [&](int b) { return min(max(p.q_start[b], 0), p.rows); };
-
-    int32_t n_free = count_free(l, scratch, flip);
+    uint32_t head;
+    int32_t n_free = 0;
     bool exhausted = false;                                // (the same in every thread)
     for (int b0 = 0; b0 < l.n_seqs; b0 += p.seqs_per_round) {
         const int n_b = min(p.seqs_per_round, l.n_seqs - b0), n_l = n_b * S;
-        const int t0 = start_of(b0), t1 = max(start_of(b0 + n_b), t0);
-        // the round's sequence of a row (t0 <= t < t1)
-        auto seq_of = [&](int t) {
-            int lo = 0, hi = n_b;
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (p.q_start[b0 + mid] <= t) lo = mid; else hi = mid;
-            }
-            return lo;
-        };
-        __syncthreads();                                   // the round before is done with the lists' words
-        for (int i = tid; i < n_l; i += WG) count[i] = 0;
-        for (int i = tid; i < n_b; i += WG) ok[i] = 1;
-        __syncthreads();
+        const int64_t list0 = (int64_t)b0 * S;
+        if (b0) __syncthreads();                           // the round before is done with the lists' words
+        for (int i = tid; i < n_l; i += WG) { count[i] = 0; len[i] = list_len(l, list0 + i); }
+        for (int i = tid; i <= n_b; i += WG) {
+            start[i] = start_of(p, b0 + i);
+            if (i < n_b) ok[i] = 1;
+        }
+        if (b0 == 0) n_free = count_free(l, head, scratch, flip);      // (a barrier for the words above too)
+        else __syncthreads();
+        const int t0 = start[0], t1 = max(start[n_b], t0);
         if (!p.row_shard) {                                // one shard
-            for (int i = tid; i < n_b; i += WG) count[i] = max(start_of(b0 + i + 1) - start_of(b0 + i), 0);
+            for (int i = tid; i < n_b; i += WG) count[i] = max(start[i + 1] - start[i], 0);
         } else {
             for (int t = t0 + tid; t < t1; t += WG) {
                 const uint32_t s = p.row_shard[t];
-                if (s < (uint32_t)S) atomicAdd(&count[seq_of(t) * S + s], 1);
+                if (s < (uint32_t)S) atomicAdd(&count[last_at_most(start, n_b, t) * S + s], 1);
             }
         }
         __syncthreads();
-        const int64_t list0 = (int64_t)b0 * S;
         auto need = [&](int i) {                           // pages; -1: more rows than a list has
-            const int64_t n = (int64_t)list_len(l, list0 + i) + count[i];
+            const int64_t n = (int64_t)len[i] + count[i];
             if (n > (int64_t)l.max_pages << l.page_shift) return -1;
-            return pages_of(l, (int32_t)n) - pages_of(l, (int32_t)n - count[i]);
+            return pages_of(l, (int32_t)n) - pages_of(l, len[i]);
         };
         for (int i = tid; i < n_l; i += WG)
             if (need(i) < 0) ok[i / S] = 0;
@@ -164,106 +187,95 @@ __global__ __launch_bounds__(WG) void paged_extend_kernel(ExtendParams p) {
         const int32_t needed = scan_lists(n_l, first, scratch, flip, [&](int i) { return ok[i / S] ? need(i) : 0; });
         // A sequence is taken if all pages up to its own are there, or if it needs none.  Those that are taken and need some come
         // before all that find none, so that `first` needs no second pass.
-        auto pages_end = [&](int b) { return b + 1 < n_b ? first[(b + 1) * S] : needed; };
         int32_t most = 0;
         for (int b = tid; b < n_b; b += WG) {
-            const int32_t lo = first[b * S], hi = pages_end(b);
+            const int32_t lo = first[b * S], hi = b + 1 < n_b ? first[(b + 1) * S] : needed;
             if (hi > lo) {
                 if (exhausted || hi > n_free) ok[b] = 0;
                 else most = hi;
             }
             p.accepted[b0 + b] = ok[b];
         }
-        // the pages of all that are taken: the largest `most` (they ascend with b)
-        int32_t granted = 0;
-        {
-            int32_t *top = scratch + flip * WAVES;
-            flip ^= 1;
-            int32_t m = most;
-#pragma unroll
-            for (int o = 32; o; o >>= 1) m = max(m, __shfl_xor(m, o, WAVE));
-            if ((tid & 63) == 0) top[tid >> 6] = m;
-            __syncthreads();
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) granted = max(granted, top[w]);
-        }
-        take_free(l, granted, scratch, flip, [&](int32_t page, int32_t rank) {
+        const int32_t granted = block_max(most, scratch, flip);    // the pages of all that are taken (`most` ascends with b)
+        take_free(l, granted, b0 == 0, head, scratch, flip, [&](int32_t page, int32_t rank) {
             const int i = last_at_most(first, n_l, rank);
-            const int32_t at = pages_of(l, list_len(l, list0 + i)) + rank - first[i];
-            l.table[(list0 + i) * l.max_pages + at] = page;
+            l.table[(list0 + i) * l.max_pages + pages_of(l, len[i]) + rank - first[i]] = page;
         });
         n_free -= granted;
         exhausted |= needed > granted;
-
-        if (p.row_shard) {                                 // rows of a shard in the round before each sequence
-            for (int s = tid; s < S; s += WG) {
-                int32_t sum = 0;
-                for (int b = 0; b < n_b; ++b) { before[b * S + s] = sum; sum += count[b * S + s]; }
-            }
-        }
-        __syncthreads();                                   // pages, lengths as they were, and counts are there
-        auto slot_of = [&](int64_t list, int32_t row) {
-            const int32_t page = l.table[list * l.max_pages + (row >> l.page_shift)];
-            return (uint32_t)page < (uint32_t)l.n_pages ? (page << l.page_shift) + (row & ((1 << l.page_shift) - 1)) : -1;
-        };
-        if (!p.row_shard) {
+        for (int i = tid; i < n_l; i += WG)
+            if (ok[i / S] && count[i]) l.len[list0 + i] = len[i] + count[i];
+        if (p.rows_here) {
+            __syncthreads();                               // the pages are in the lists
             for (int t = t0 + tid; t < t1; t += WG) {
-                const int b = seq_of(t), i = t - start_of(b0 + b);
+                const int b = last_at_most(start, n_b, t), i = t - start[b], row = len[b] + i;
                 const bool taken = ok[b] && (uint32_t)i < (uint32_t)count[b];
-                const int32_t row = list_len(l, list0 + b) + i;
-                p.slots[t] = taken ? slot_of(list0 + b, row) : -1;
+                p.slots[t] = taken ? slot_of(l, list0 + b, row) : -1;
                 p.visible[t] = taken ? row + 1 : 0;
             }
-        } else {
-            // 64 rows a wavefront: a row's rank in its shard is a population count of a ballot, plus the rows of the
-            // wavefronts before, plus those of earlier passes (held by the thread of that shard)
-            const int wave = tid >> 6, lane = tid & 63;
-            const uint64_t up_to = ~0ull >> (63 - lane);
-            int32_t *seen = part + WAVES * S;              // [S] rows of earlier passes
-            for (int s = tid; s < S; s += WG) seen[s] = 0;
-            for (int base = t0; base < t1; base += WG) {
-                const int t = base + tid;
-                const int shard = t < t1 ? p.row_shard[t] : -1;
-                for (int s = 0; s < S; ++s) {
-                    const int n = __popcll(__ballot(shard == s));
-                    if (lane == 0) part[wave * S + s] = n;
-                }
-                __syncthreads();
-                for (int s = tid; s < S; s += WG) {        // exclusive sums over the wavefronts
-                    int32_t sum = seen[s];
-                    for (int w = 0; w < WAVES; ++w) {
-                        const int32_t n = part[w * S + s];
-                        part[w * S + s] = sum;
-                        sum += n;
-                    }
-                    seen[s] = sum;
-                }
-                __syncthreads();
-                const int b = t < t1 ? seq_of(t) : 0;
-                const bool taken = ok[b] != 0;
-                int32_t mine = -1;
-                for (int s = 0; s < S; ++s) {
-                    const int32_t rank = part[wave * S + s] + __popcll(__ballot(shard == s) & up_to) - before[b * S + s];
-                    if (t >= t1) continue;
-                    const int32_t end = list_len(l, list0 + b * S + s) + rank;
-                    p.visible[(int64_t)t * S + s] = taken ? end : 0;
-                    if (s == shard) mine = end - 1;
-                }
-                if (t < t1) p.slots[t] = taken && (uint32_t)shard < (uint32_t)S ? slot_of(list0 + b * S + shard, mine) : -1;
-                __syncthreads();                           // the next pass writes `part`
-            }
         }
-        __syncthreads();                                   // every length has been read
-        for (int i = tid; i < n_l; i += WG)
-            if (ok[i / S] && count[i]) l.len[list0 + i] = list_len(l, list0 + i) + count[i];
     }
-    // rows of no sequence
-    const int lo = start_of(0), hi = max(start_of(l.n_seqs), lo);
-    for (int t = tid; t < p.rows; t += WG) {
-        if (t >= lo && t < hi) continue;
-        p.slots[t] = -1;
-        for (int s = 0; s < S; ++s) p.visible[(int64_t)t * S + s] = 0;
+    if (!p.rows_here) return;
+    const int lo = start_of(p, 0), hi = max(start_of(p, l.n_seqs), lo);
+    for (int t = tid; t < p.rows; t += WG)
+        if (t < lo || t >= hi) { p.slots[t] = -1; p.visible[t] = 0; }       // rows of no sequence
+}
+
+// Slots and limits of 64 rows a wavefront, from the new lengths backwards: a row of shard s sees all rows of the shard but
+// those behind it.  Behind it are those of the same sequence in the wavefront (population counts of ballots) and those beyond,
+// which the wavefront counts into LDS for the sequence that its last row belongs to.
+__global__ __launch_bounds__(256) void paged_rows_slots_kernel(ExtendParams p) {
+    extern __shared__ int32_t smem[];                      // [4][S]
+    const Lists &l = p.l;
+    const int S = l.n_shards, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int t0 = (blockIdx.x * 4 + wave) * 64, t = t0 + lane;
+    int32_t *beyond = smem + wave * S;
+    for (int s = lane; s < S; s += 64) beyond[s] = 0;
+    // the sequence of a row: the last that begins at or before it
+    auto seq_of = [&](int row) {
+        int lo = 0, hi = l.n_seqs;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (p.q_start[mid] <= row) lo = mid; else hi = mid;
+        }
+        return lo;
+    };
+    const int b = seq_of(min(t, p.rows - 1)), begin = start_of(p, b), end = max(start_of(p, b + 1), begin);
+    const bool inside = t < p.rows && t >= begin && t < end, taken = inside && p.accepted[b];
+    const int shard = !inside ? -1 : p.row_shard ? p.row_shard[t] : 0;
+    const int open = __shfl(b, 63, WAVE), open_end = __shfl(end, 63, WAVE);
+    __builtin_amdgcn_wave_barrier();
+    if (p.row_shard)
+        for (int r0 = t0 + 64 + lane; r0 < open_end; r0 += 512) {      // eight loads in flight
+            uint32_t s[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[j] = r0 + 64 * j < open_end ? p.row_shard[r0 + 64 * j] : ~0u;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (s[j] < (uint32_t)S) atomicAdd(&beyond[s[j]], 1);
+        }
+    else if (lane == 0) beyond[0] = max(open_end - t0 - 64, 0);
+    __syncthreads();
+    // rows behind this one in its sequence, within the wavefront
+    const int last = min(end - t0, 64);                    // (lanes from here on belong to others)
+    const uint64_t mine = last >= 64 ? ~0ull : (1ull << max(last, 0)) - 1;
+    const uint64_t behind = lane == 63 ? 0 : mine & (~0ull << (lane + 1));
+    int own_end = 0;
+    for (int s0 = 0; s0 < S; s0 += 4) {
+        int v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int s = s0 + j, n = __popcll(__ballot(shard == s) & behind) + (b == open && s < S ? beyond[s] : 0);
+            v[j] = taken && s < S ? l.len[(int64_t)b * S + s] - n : 0;
+            if (s == shard) own_end = v[j];
+        }
+        if (t >= p.rows) continue;
+        int32_t *out = p.visible + (int64_t)t * S + s0;
+        if (S % 4 == 0 && (uintptr_t)p.visible % 16 == 0) *(int4 *)out = make_int4(v[0], v[1], v[2], v[3]);
+        else
+            for (int j = 0; j < 4 && s0 + j < S; ++j) out[j] = v[j];
     }
+    if (t < p.rows) p.slots[t] = taken && (uint32_t)shard < (uint32_t)S ? slot_of(l, (int64_t)b * S + shard, own_end - 1) : -1;
 }
 
 // ---------------------------------------------------------------------------- freed sequences
@@ -297,17 +309,19 @@ __global__ __launch_bounds__(WG) void pages_fork_kernel(ForkParams p) {
     int32_t *first = smem, *ok = first + n_l, *rows = ok + p.n;     // per list, per pair, per list
     __shared__ int32_t scratch[2 * WAVES];
     int flip = 0;
+    for (int i = tid; i < p.n; i += WG) rows[i] = p.dst[i];
+    uint32_t head;
+    const int32_t n_free = count_free(l, head, scratch, flip);     // (a barrier for the words above too)
     for (int i = tid; i < p.n; i += WG) {
-        const int src = p.src[i], dst = p.dst[i];
+        const int src = p.src[i], dst = rows[i];
         bool good = (uint32_t)src < (uint32_t)l.n_seqs && (uint32_t)dst < (uint32_t)l.n_seqs && src != dst;
-        for (int j = 0; good && j < i; ++j) good = p.dst[j] != dst;
         for (int s = 0; good && s < S; ++s) good = l.len[(int64_t)dst * S + s] <= 0;
+        for (int j = 0; j < i; ++j) good &= rows[j] != dst;
         ok[i] = good;
     }
     __syncthreads();
     for (int i = tid; i < n_l; i += WG) rows[i] = ok[i / S] ? list_len(l, (int64_t)p.src[i / S] * S + i % S) : 0;
     const int32_t mask = (1 << l.page_shift) - 1;
-    const int32_t n_free = count_free(l, scratch, flip);
     __syncthreads();
     const int32_t needed = scan_lists(n_l, first, scratch, flip, [&](int i) { return (int32_t)((rows[i] & mask) != 0); });
     // as in an extension: those that are taken and need pages come first
@@ -320,23 +334,13 @@ __global__ __launch_bounds__(WG) void pages_fork_kernel(ForkParams p) {
         }
         p.accepted[i] = ok[i];
     }
-    int32_t granted = 0;
-    {
-        int32_t *top = scratch + flip * WAVES;
-        flip ^= 1;
-#pragma unroll
-        for (int o = 32; o; o >>= 1) most = max(most, __shfl_xor(most, o, WAVE));
-        if ((tid & 63) == 0) top[tid >> 6] = most;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) granted = max(granted, top[w]);
-    }
+    const int32_t granted = block_max(most, scratch, flip);
     for (int i = tid; i < n_l; i += WG) {
         p.list_len[i] = ok[i / S] ? rows[i] : 0;
         p.list_page[i] = -1;
     }
     __syncthreads();
-    take_free(l, granted, scratch, flip, [&](int32_t page, int32_t rank) { p.list_page[last_at_most(first, n_l, rank)] = page; });
+    take_free(l, granted, true, head, scratch, flip, [&](int32_t page, int32_t rank) { p.list_page[last_at_most(first, n_l, rank)] = page; });
 }
 
 // Grid (lists, 2 * layers, kv heads): the used rows of a list's last page, which are contiguous per head.  The first
@@ -389,17 +393,18 @@ __global__ __launch_bounds__(WG) void pages_compact_kernel(Lists l, int32_t *n_l
                                                            int32_t *count) {
     __shared__ int32_t scratch[2 * WAVES];
     int flip = 0;
-    const int32_t n_live = l.n_pages - count_free(l, scratch, flip);
+    uint32_t head;
+    const int32_t n_live = l.n_pages - count_free(l, head, scratch, flip);
     int32_t moved = 0, holes = 0;
     for (int64_t base = 0; base < l.n_pages; base += WG * REFS_PER_THREAD) {
         const int64_t p0 = base + (int64_t)threadIdx.x * REFS_PER_THREAD;
+        const uint32_t free = base ? free_mask(l, p0) : head;
         uint32_t hole = 0, mover = 0;
 #pragma unroll
         for (int i = 0; i < REFS_PER_THREAD; ++i) {
             if (p0 + i >= l.n_pages) continue;
-            const bool free = l.refs[p0 + i] == 0;
-            if (free && p0 + i < n_live) hole |= 1u << i;
-            if (!free && p0 + i >= n_live) mover |= 1u << i;
+            if ((free >> i & 1) && p0 + i < n_live) hole |= 1u << i;
+            if (!(free >> i & 1) && p0 + i >= n_live) mover |= 1u << i;
         }
         int32_t n_holes, n_moved;
         int32_t h = holes + block_scan(__popc(hole), scratch, flip, n_holes), m = moved + block_scan(__popc(mover), scratch, flip, n_moved);
@@ -496,10 +501,13 @@ extern "C" int32_t cascade_paged_extend(const cascade_paged_cache *cache, int32_
     p.rows = rows;
     const int S = cache->n_shards;
     p.seqs_per_round = min(cache->n_seqs, max(1, 4096 / S));
-    const int bytes = 4 * (p.seqs_per_round * (3 * S + 1) + (WAVES + 1) * S);
+    // one launch for a few rows of one shard, else the rows' part by as many wavefronts as it has 64 rows
+    p.rows_here = !row_shard_dev && rows <= 2 * WG;
+    const int bytes = 4 * (p.seqs_per_round * (3 * S + 2) + 1);
     static std::atomic<uint64_t> lds_ready{0};
-    CASCADE_HIP_TRY(ensure_dynamic_lds((const void *)paged_extend_kernel, 144 * 1024, lds_ready));
+    CASCADE_HIP_TRY(ensure_dynamic_lds((const void *)paged_extend_kernel, 4 * (4096 * 5 + 1), lds_ready));
     hipLaunchKernelGGL(paged_extend_kernel, dim3(1), dim3(WG), bytes, (hipStream_t)stream, p);
+    if (!p.rows_here) hipLaunchKernelGGL(paged_rows_slots_kernel, dim3((rows + 255) / 256), dim3(256), 16 * S, (hipStream_t)stream, p);
     CASCADE_HIP_TRY(hipGetLastError());
     return CASCADE_OK;
 }
