@@ -40,7 +40,6 @@ struct PagedWork {
     int b, first_row, n_rows;                              // sequence, its first row in q, its flattened rows
     int tile, steps;                                       // steps: of the sequence's whole walk
     int piece, n_pieces, first_piece;                      // first_piece: number of this tile's first partial (n_pieces > 1)
-    int k0, k1;                                            // steps of this piece
     bool valid;
 };
 
@@ -128,7 +127,6 @@ struct PagedPlan {
                 out.piece = MERGE ? 0 : i - tile * out.n_pieces;
                 out.first_piece = parts_before + of(parts_incl - parts) + tile * out.n_pieces;
                 out.tile = of(tiles) - 1 - tile;
-                paged_cut(out.steps, out.piece, out.n_pieces, out.k0, out.k1);
                 // (more partials than the launch has room for: only where sequences overlap, which they must not)
                 out.valid = out.n_pieces == 1 || out.first_piece + out.n_pieces <= set.max_parts;
                 return true;

@@ -75,22 +75,50 @@ __global__ __launch_bounds__(256, rows_occupancy(sizeof(T), DM, RB)) void paged_
     PagedWork wk;
     if (!plan.template pick<false>(p, p.few, blockIdx.x, wk) || !wk.valid) return;
 
-    // first step of every shard, and its length (several shards only)
+    // Keys that some row of the tile sees.  With one token those are all that the cache holds, as a rule, and a look at its limit
+    // would only delay the first loads; several shards: first step of every shard, and its keys.
     int32_t *cum = (int32_t *)smem, *lens = cum + p.S + 1;
     const int64_t list0 = (int64_t)wk.b * p.S;
+    const int tok0 = (int)((uint32_t)(wk.tile * TILE) / (uint32_t)p.rep);
+    const int toks = (int)((uint32_t)(min((wk.tile + 1) * TILE, wk.n_rows) - 1) / (uint32_t)p.rep) - tok0 + 1;
+    const int32_t *tile_limits = p.visible && toks > 1 ? p.visible + (int64_t)(wk.first_row + tok0) * p.S : nullptr;
+    int only_len = 0;
     if (p.S > 1) {
         if (wave == 0) {
             int carry = 0;
             for (int s0 = 0; s0 < p.S; s0 += 64) {
-                const int s = s0 + lane, n = s < p.S ? paged_len(p, list0 + s) : 0, st = (n + KEYS - 1) / KEYS;
-                const int incl = wave_inclusive(st);
+                const int s = s0 + lane;
+                int n = s < p.S ? paged_len(p, list0 + s) : 0;
+                if (tile_limits && s < p.S) {
+                    int most = 0;
+                    for (int t0 = 0; t0 < toks; t0 += 4) {
+                        int v[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v[j] = tile_limits[(int64_t)min(t0 + j, toks - 1) * p.S + s];
+                        most = max(max(most, max(v[0], v[1])), max(v[2], v[3]));
+                    }
+                    n = min(n, most);
+                }
+                const int st = (n + KEYS - 1) / KEYS, incl = wave_inclusive(st);
                 if (s < p.S) { lens[s] = n; cum[s] = carry + incl - st; }
-                carry += __shfl(incl, 63, WAVE);
+                carry += __builtin_amdgcn_readlane(incl, 63);
             }
             if (lane == 0) cum[p.S] = carry;
         }
         __syncthreads();
+    } else {
+        only_len = paged_len(p, list0);
+        if (tile_limits) {
+            static_assert(TILE <= 64, "a lane for every token");
+            int most = lane < toks ? tile_limits[lane] : 0;
+#pragma unroll
+            for (int o = 32; o; o >>= 1) most = max(most, __shfl_xor(most, o, WAVE));
+            only_len = min(only_len, most);
+        }
+        only_len = __builtin_amdgcn_readfirstlane(max(only_len, 0));
     }
+    int k0, k1;                                            // steps of this piece
+    paged_cut(__builtin_amdgcn_readfirstlane(p.S > 1 ? cum[p.S] : (only_len + KEYS - 1) / KEYS), wk.piece, wk.n_pieces, k0, k1);
 
     // ---- query rows of this lane (column c16 of each block of 16)
     const T *qp = (const T *)p.q;
@@ -129,7 +157,6 @@ __global__ __launch_bounds__(256, rows_occupancy(sizeof(T), DM, RB)) void paged_
     // Where step k lies: read a step before its loads are requested
     struct Place { int j0, shard, len, id[2]; };
     int shard = 0;
-    const int only_len = p.S > 1 ? 0 : __builtin_amdgcn_readfirstlane(paged_len(p, list0));
     auto locate = [&](int k) {
         Place x;
         int j0 = k * KEYS, len = only_len;
@@ -316,9 +343,9 @@ __global__ __launch_bounds__(256, rows_occupancy(sizeof(T), DM, RB)) void paged_
 
     // this wavefront's quarter of the piece
     int a, b;
-    paged_cut(wk.k1 - wk.k0, wave, 4, a, b);
-    a += wk.k0;
-    b += wk.k0;
+    paged_cut(k1 - k0, wave, 4, a, b);
+    a += k0;
+    b += k0;
     if (a < b) {
         // (the requests ahead are not conditional, behind the end they are of no rows: with a branch around them the compiler
         // cannot count the loads in flight and waits for all of them)
@@ -622,12 +649,16 @@ int32_t launch_rows(const PagedAttnParams &p, hipStream_t s) {
     CASCADE_HIP_TRY(hipGetLastError());
     return CASCADE_OK;
 }
-// 32 rows a tile where sequences have more than 16 on average, else 16; heads of more than 128 have no registers for 32
-int rows_tile(const PagedAttnParams &p) { return (int64_t)p.rows * p.rep > (int64_t)16 * p.B && p.d <= 128 ? 32 : 16; }
+// 32 rows a tile where sequences have more than 16 on average, else 16.  Heads of more than 128 have no registers for 32, and fp32
+// heads up to 64 are faster with 16 (12 heads of 64, 1024 rows over 4024 keys: 163 us against 176; 100, 37 and 1 rows over 1000, 448
+// and 1: 23 against 28; 32 / 8 heads of 128, 256 rows over 2256 keys: 116 against 102).
+int rows_tile(const PagedAttnParams &p, bool f32) {
+    return (int64_t)p.rows * p.rep > (int64_t)16 * p.B && p.d <= 128 && !(f32 && p.d <= 64) ? 32 : 16;
+}
 template <typename T, int DM>
 int32_t launch_dim(const PagedAttnParams &p, hipStream_t s) {
-    if constexpr (DM <= 128)
-        if (rows_tile(p) == 32) return launch_rows<T, DM, 2>(p, s);
+    if constexpr (DM == 128 || (DM == 64 && sizeof(T) == 2))
+        if (rows_tile(p, sizeof(T) == 4) == 32) return launch_rows<T, DM, 2>(p, s);
     return launch_rows<T, DM, 1>(p, s);
 }
 template <typename T>
@@ -650,11 +681,11 @@ void set_sizes(PagedAttnParams &p, const cascade_paged_cache *c, const cascade_p
         x.inv_target = 1.0f / x.target;
         x.min_steps = min_steps;
     };
-    const bool tiles = c->dtype == CASCADE_BF16 && (p.d == 64 || p.d == 128) && (int64_t)p.rows * p.rep > PAGED_FEW && (p.B == 1 || p.rows > p.B);
+    const bool f32 = c->dtype == CASCADE_F32, tiles = !f32 && (p.d == 64 || p.d == 128) && (int64_t)p.rows * p.rep > PAGED_FEW && (p.B == 1 || p.rows > p.B);
     if (tiles) set(p.many, p.B == 1 ? 0 : PAGED_FEW, INT32_MAX, PAGED_TILE_TARGET, 4);
-    if (!tiles || p.B > 1) set(p.few, 0, tiles ? PAGED_FEW : INT32_MAX, 256 * rows_occupancy(c->dtype == CASCADE_BF16 ? 2 : 4, p.d, rows_tile(p) / 16), 8);
+    if (!tiles || p.B > 1) set(p.few, 0, tiles ? PAGED_FEW : INT32_MAX, 256 * rows_occupancy(f32 ? 4 : 2, p.d, rows_tile(p, f32) / 16), 8);
 }
-size_t set_parts(PagedAttnParams &p, float *workspace) {
+size_t set_parts(PagedAttnParams &p, bool f32, float *workspace) {
     size_t floats = 0;
     auto set = [&](PagedSet &x, int tile) {
         if (!x.target) return;
@@ -665,7 +696,7 @@ size_t set_parts(PagedAttnParams &p, float *workspace) {
         floats += align_up(parts * p.Hkv * tile * (p.d + 2), 4);
     };
     set(p.many, PAGED_TILE);
-    set(p.few, rows_tile(p));
+    set(p.few, rows_tile(p, f32));
     return floats;
 }
 
@@ -691,7 +722,7 @@ extern "C" size_t cascade_paged_attn_workspace_bytes(const cascade_paged_cache *
     if (check_attn(cache, desc) != CASCADE_OK) return 0;
     PagedAttnParams p = {};
     set_sizes(p, cache, desc);
-    return align_up(set_parts(p, nullptr) * sizeof(float), 256);
+    return align_up(set_parts(p, cache->dtype == CASCADE_F32, nullptr) * sizeof(float), 256);
 }
 
 extern "C" int32_t cascade_paged_attn(const cascade_paged_cache *cache, int32_t layer, const cascade_paged_attn_desc *desc,
@@ -713,7 +744,7 @@ extern "C" int32_t cascade_paged_attn(const cascade_paged_cache *cache, int32_t 
     p.q_stride = desc->q_stride ? desc->q_stride : row;
     p.o_stride = desc->o_stride ? desc->o_stride : row;
     set_sizes(p, cache, desc);
-    set_parts(p, (float *)workspace);
+    set_parts(p, cache->dtype == CASCADE_F32, (float *)workspace);
     p.scale_log2 = desc->scale * 1.4426950408889634f;
     p.o_f32 = desc->o_dtype == CASCADE_F32;
     return cache->dtype == CASCADE_BF16 ? launch_type<bf16_t>(p, (hipStream_t)stream) : launch_type<float>(p, (hipStream_t)stream);
