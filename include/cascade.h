@@ -520,7 +520,8 @@ typedef struct cascade_paged_cache {
     int32_t n_layers, n_pages;
     int32_t n_kv_heads, head_dim;     /* head_dim: a multiple of 8 (bf16) or 4 (f32), at most 256 */
     int32_t page_size;                /* rows: a power of two, 16 .. 65536             */
-    int32_t n_seqs, n_shards;         /* n_shards: at most 1024                        */
+    int32_t n_seqs, n_shards;         /* n_shards: at most 1024; lists, pages and rows
+                                         of the pools, of a list: 31 bits each         */
     int32_t max_pages;                /* of a list                                     */
     void *k_pages, *v_pages;          /* [n_layers, n_pages, H_KV, page_size, d], 16-byte aligned */
     int32_t *page_table;              /* [n_seqs, n_shards, max_pages]; unused entries -1 */
@@ -573,9 +574,11 @@ CASCADE_API int32_t cascade_paged_append(const cascade_paged_cache *cache, int32
  *   sequence are left as they were.  What a row does not see never reaches it, be it
  *   NaN.  With o in fp32, (lse, 1, o) is a partial that cascade_lse_merge takes
  *   (CASCADE_U_NORMALISED), where other parties hold more shards.
- * q, o 16-byte aligned, strides in elements (0: dense) and multiples of 16 bytes.  Calls
- * that may overlap in time need a workspace each (16-byte aligned); its contents need
- * not be kept between calls.
+ * q, o 16-byte aligned, strides in elements (0: dense) and multiples of 16 bytes; o must
+ * not overlap q.  Calls that may overlap in time need a workspace each (16-byte aligned);
+ * its contents need not be kept between calls.  Two sequences must not share rows.
+ * A call with the same arguments gives the same bits each time; those of a row may depend
+ * on the other rows and lengths of the call, which decide how the work is cut.
  * Errors: EINVAL, ESHAPE (n_heads % H_KV, strides, layer), EUNSUPPORTED (alignment,
  * sizes), EWORKSPACE, EHIP.                                                         */
 typedef struct cascade_paged_attn_desc {

@@ -18,6 +18,8 @@ static inline int32_t check_paged_cache(const cascade_paged_cache *c) {
     if (c->n_shards > 1024 || c->n_kv_heads > 65535 || (int64_t)c->n_pages * c->page_size > INT32_MAX ||
         (int64_t)c->max_pages * c->page_size > INT32_MAX || (int64_t)c->n_seqs * c->n_shards * c->max_pages > INT32_MAX)
         return CASCADE_EUNSUPPORTED;
+    // steps of 32 rows over all lists of a sequence, too
+    if ((int64_t)c->n_shards * c->max_pages * c->page_size > ((int64_t)1 << 35)) return CASCADE_EUNSUPPORTED;
     if (((uintptr_t)c->k_pages | (uintptr_t)c->v_pages) % 16) return CASCADE_EUNSUPPORTED;
     return CASCADE_OK;
 }

@@ -279,3 +279,142 @@ def test_partials_of_several_parties_merge(cas):
     ref = attention(whole, 0, q, [0, rows], limits, 0.125)
     live = slice(1, rows)
     check_attention(whole, out.view(rows, H, d)[live], None, (ref[0][live], ref[1][:, live], ref[2][live], ref[3][live]), 260)
+
+
+def test_which_kernel_takes_which_rows(cas):
+    """Sequences of more than 256 flattened rows go to the tiles, the others to the kernel for few rows; fp32 and other head
+    dimensions always; no more rows than sequences: the kernel for few rows alone."""
+    import torch
+    from launched import kernels_of
+    from paged_reference import DT, Cache, i32, starts
+
+    def names(dtype, d, new, H=8, Hkv=2):
+        cache = Cache(cas, dtype, Hkv, d, 16, np.add(new, 40)[:, None], seed=1)
+        q = torch.randn((sum(new), H, d), device="cuda").to(DT[dtype])
+        o, q_start = torch.empty_like(q), i32(starts(new))
+        ws = cas.new_workspace(cas.cascade_paged_attn_workspace_bytes(cache.handle, sum(new), H))
+        got = kernels_of(lambda: cas.cascade_paged_attn(cache.handle, 0, q, o, q_start, 0.1, workspace=ws))
+        return ["tile" if "paged_tile" in n else "rows" if "paged_rows" in n else "merge" for n in got]
+    assert names("bf16", 128, [100]) == ["tile", "merge"]
+    assert names("bf16", 64, [100, 1]) == ["tile", "rows", "merge"]
+    assert names("bf16", 128, [64]) == ["rows", "merge"]
+    assert names("bf16", 96, [300]) == ["rows", "merge"] and names("f32", 64, [300]) == ["rows", "merge"]
+    assert names("bf16", 128, [1] * 100) == ["rows", "merge"]
+
+
+@pytest.mark.parametrize("new,rows", [([70], 200), ([64, 0, 0], 64), ([0] * 40 + [41], 41), ([0, 0, 0, 90], 90)])
+def test_batches_that_guess_the_kernel_wrong(cas, new, rows):
+    """Rows that make tiles possible where there are few, and as many sequences as rows where one has them all."""
+    import torch
+    from paged_reference import Cache, attention, causal, check_attention, i32, starts
+    context = [30 + i for i in range(len(new))]
+    if len(new) == 3:
+        new, context = new + [0] * 61, context + [5] * 61   # as many sequences as rows
+    cache = Cache(cas, "bf16", 2, 64, 16, np.add(new, context)[:, None], seed=21)
+    q = torch.randn((rows, 8, 64), device="cuda").bfloat16()
+    visible = torch.zeros((rows, 1), dtype=torch.int32, device="cuda")
+    visible[:sum(new)] = i32(causal(context, new, 1))
+    o, lse = torch.full_like(q, 7.0), torch.full((8, rows), 7.0, device="cuda")
+    ws = cas.new_workspace(cas.cascade_paged_attn_workspace_bytes(cache.handle, rows, 8))
+    ws.fill_(0xff)
+    cas.cascade_paged_attn(cache.handle, 0, q, o, i32(starts(new)), 0.125, visible=visible, lse=lse, workspace=ws)
+    torch.cuda.synchronize()
+    ref, n = attention(cache, 0, q, starts(new), visible, 0.125), sum(new)
+    check_attention(cache, o[:n], lse[:, :n], (ref[0][:n], ref[1][:, :n], ref[2][:n], ref[3][:n]), 200)
+    assert bool((o[n:] == 7).all()) and bool((lse[:, n:] == 7).all())
+
+
+@pytest.mark.parametrize("shards,page", [(1, 16), (1, 256), (5, 32), (130, 16)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_tiles(cas, shards, page, d):
+    """Many rows: several tiles a sequence, ends inside pages and tiles, empty shards, pieces of a walk."""
+    run(cas, "bf16", 8, 2, d, page, [0, 700, 63, 2000], [257, 64, 300, 90], shards=shards, seed=22)
+    run(cas, "bf16", 6, 2, d, page, [1300], [129], shards=shards, mask=None, seed=23)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("at", [3, 200, 340])
+def test_values_that_are_not_finite_in_tiles(cas, bad, at):
+    """One value of a shard's row, early (every row of the tiles sees it), where the limit passes, and last of all."""
+    import torch
+    from paged_reference import Cache, attention, causal, check_attention, i32, starts
+    new, context = [150], [200]
+    cache = Cache(cas, "bf16", 2, 128, 16, [[175, 175]], seed=24)
+    token = min(at, 349)
+    s, r = token % 2, token // 2
+    cache.vp[0, cache.table[0, s, r // 16].item(), 0, r % 16, 77] = bad
+    q = torch.randn((150, 8, 128), device="cuda").bfloat16()
+    visible = i32(causal(context, new, 2))
+    o = torch.full_like(q, 7.0)
+    ws = cas.new_workspace(cas.cascade_paged_attn_workspace_bytes(cache.handle, 150, 8))
+    cas.cascade_paged_attn(cache.handle, 0, q, o, i32(starts(new)), 0.09, visible=visible, workspace=ws)
+    torch.cuda.synchronize()
+    sees = torch.arange(150, device="cuda") + 200 >= token
+    hit = o[:, :4, 77]
+    assert bool((torch.isnan(hit[sees]) if math.isnan(bad) else hit[sees] == bad).all())
+    finite = torch.isfinite(o)
+    finite[:, :4, 77] |= sees[:, None]
+    assert bool(finite.all())
+    cache.vp[0, cache.table[0, s, r // 16].item(), 0, r % 16, 77] = 0.0
+    ref = attention(cache, 0, q, starts(new), visible, 0.09)
+    o[:, :4, 77] = torch.where(sees[:, None], ref[0][:, :4, 77].bfloat16(), o[:, :4, 77])
+    check_attention(cache, o, None, ref, 350)
+
+
+def test_pools_beyond_32_bits_of_bytes(cas):
+    """Pages whose bytes lie behind the first 4 GiB of a layer's pool, and whose elements lie behind 2^31."""
+    import torch
+    from paged_reference import Cache, attention, causal, check_attention, dealt, i32, starts
+    page, Hkv, d, n_pages = 64, 8, 128, 34000              # 131072 bytes a page
+    new, context = [1, 70], [500, 300]
+    small = Cache(cas, "bf16", Hkv, d, page, dealt(np.add(context, new), 1), seed=25)
+    used = small.kp.shape[1]
+    kp, vp = (torch.empty((2, n_pages, Hkv, page, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    far = n_pages - used - 1
+    kp[1, far:far + used], vp[1, far:far + used] = small.kp[0], small.vp[0]
+    refs = torch.zeros(n_pages, dtype=torch.int32, device="cuda")
+    refs[far:far + used] = small.refs
+    big = cas.make_paged_cache(kp, vp, torch.where(small.table >= 0, small.table + far, -1).int(), small.lens, refs)
+    q, visible = torch.randn((71, 32, d), device="cuda").bfloat16(), i32(causal(context, new, 1))
+    o, lse = torch.empty_like(q), torch.empty((32, 71), device="cuda")
+    ws = cas.new_workspace(cas.cascade_paged_attn_workspace_bytes(big, 71, 32))
+    cas.cascade_paged_attn(big, 1, q, o, i32(starts(new)), d ** -0.5, visible=visible, lse=lse, workspace=ws)
+    torch.cuda.synchronize()
+    check_attention(small, o, lse, attention(small, 0, q, starts(new), visible, d ** -0.5), 501)
+    # rows written there, and a page copied from there
+    slots = i32([(n_pages - 1) * page + 5, (n_pages - 1) * page + 6])
+    k, v = torch.randn((2, Hkv, d), device="cuda").bfloat16(), torch.randn((2, Hkv, d), device="cuda").bfloat16()
+    cas.cascade_paged_append(big, 1, slots, k, v)
+    kp[0, 3] = 1.0
+    cas.cascade_pages_copy(big, i32([n_pages - 1]), i32([3]))
+    torch.cuda.synchronize()
+    assert torch.equal(kp[1, n_pages - 1, :, 5:7].transpose(0, 1), k) and torch.equal(vp[1, 3, :, 5:7].transpose(0, 1), v)
+
+
+def test_two_graphs_share_a_workspace_in_turn(cas):
+    import torch
+    from paged_reference import Cache, attention, causal, check_attention, i32, starts
+    jobs = []
+    ws = None
+    for new, context in (([90, 1], [3000, 500]), ([1, 1, 1], [4000, 20, 900])):
+        cache = Cache(cas, "bf16", 2, 128, 16, np.add(new, context)[:, None], seed=26)
+        q, visible, q_start = torch.randn((sum(new), 8, 128), device="cuda").bfloat16(), i32(causal(context, new, 1)), i32(starts(new))
+        jobs.append((cache, q, visible, q_start, torch.empty_like(q), torch.empty((8, sum(new)), device="cuda"), new))
+    ws = cas.new_workspace(max(cas.cascade_paged_attn_workspace_bytes(c.handle, q.shape[0], 8) for c, q, *_ in jobs))
+    graphs = []
+    for cache, q, visible, q_start, o, lse, _ in jobs:
+        def call():
+            cas.cascade_paged_attn(cache.handle, 0, q, o, q_start, 0.09, visible=visible, lse=lse, workspace=ws)
+        call()
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            call()
+    for _ in range(3):
+        for graph, (cache, q, visible, q_start, o, lse, new) in zip(graphs, jobs):
+            q.copy_(torch.randn(q.shape, device="cuda"))
+            o.fill_(7.0)
+            graph.replay()
+        torch.cuda.synchronize()
+        for cache, q, visible, q_start, o, lse, new in jobs:
+            check_attention(cache, o, lse, attention(cache, 0, q, starts(new), visible, 0.09), 4001)

@@ -46,7 +46,8 @@ BAD_CACHES = [(dict(k_pages=None), cas.EINVAL), (dict(page_refs=None), cas.EINVA
               (dict(head_dim=20), cas.EUNSUPPORTED), (dict(head_dim=264), cas.EUNSUPPORTED), (dict(page_size=8), cas.EUNSUPPORTED),
               (dict(page_size=48), cas.EUNSUPPORTED), (dict(page_size=1 << 17), cas.EUNSUPPORTED), (dict(n_shards=1025), cas.EUNSUPPORTED),
               (dict(n_pages=1 << 27), cas.EUNSUPPORTED), (dict(max_pages=1 << 27), cas.EUNSUPPORTED),
-              (dict(n_seqs=1 << 20, max_pages=1 << 12), cas.EUNSUPPORTED), (dict(v_pages=P + 8), cas.EUNSUPPORTED),
+              (dict(n_seqs=1 << 20, max_pages=1 << 12), cas.EUNSUPPORTED),
+              (dict(n_shards=64, max_pages=1 << 15, page_size=1 << 15, n_pages=1 << 10), cas.EUNSUPPORTED), (dict(v_pages=P + 8), cas.EUNSUPPORTED),
               (dict(dtype=cas.F32, head_dim=66), cas.EUNSUPPORTED)]
 
 
