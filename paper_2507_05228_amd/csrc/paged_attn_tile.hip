@@ -5,14 +5,24 @@
 // S^T = K Q^T and O^T = V^T P^T in 32x32x16 products: a lane holds scores of one query row, and the exponentials are, as they
 // lie, the right operand of the second product, with its 16 keys counted 4 h .. 4 h + 3, 8 + 4 h .. 8 + 4 h + 3 for lane half
 // h = lane / 32.  K and V rows go from their pages straight into LDS (a page piece of 16 rows is a descriptor of its own, cut
-// where the rows that the tile sees end: what lies behind arrives as zeros), two buffers each; the left operand of the
-// second product, four keys of one column a lane, is what the transposing LDS read of gfx950 returns.  16-byte pieces of a row
-// are permuted in LDS so that neither kind of read meets a bank twice.
+// where the rows that the tile sees end), three buffers each; the left operand of the second product, four keys of one column
+// a lane, is what the transposing LDS read returns.  16-byte pieces of a row are permuted in LDS so that neither kind of read
+// meets a bank twice (counted: no conflicts).
 //
-// One barrier a step.  Behind it: scores of step t + 1 (matrix pipe) next to the exponentials of step t (vector pipe), then the
-// output product of step t next to the maxima of step t + 1: one basic block, which the compiler interleaves.  K is requested two
-// steps ahead of its use, V one.  Steps that some row of the tile does not see whole mask their scores before the maxima are
-// taken, and look for values that are not finite (paged_attn_rows.hip has the reason).
+// A step has a vector half (the request of K two steps and of V one step ahead, the mask, maxima, exponentials of step t) and a
+// matrix half (scores of step t + 1, output product of step t).  Wavefronts w and w + 4 share a SIMD; the second four run half a
+// step behind the first, a barrier between the halves, so that a SIMD's matrix pipe works for one while the other takes
+// exponentials.  In front of a transposing read the compiler waits for every load into LDS that is under way: the wait in the
+// middle of the matrix half says so, and what it waits for was requested half a step before.  What the two halves of a
+// workgroup read and write at a time: at slot 2 t the first four request into the buffers of K(t + 2) and V(t + 1), last read at
+// slot 2 t - 2, while the others read K(t) and V(t - 1); every wavefront has waited for its own part of a tile at least one
+// barrier before anyone reads it.
+//
+// One sequence, 4096 rows over 16384 keys, 32 / 8 heads of 128 (0.96 TFLOP under the causal limit): 900 to 925 us, 1.05 PFLOP/s,
+// where a large library product reaches 1.21; the matrix pipes are busy 59 % of the time at the 1.7 GHz that the device holds
+// under this load.  All wavefronts in phase: 1027 us against 915 in the same run; page numbers through vector loads: 974 against
+// 915 (their wait is one for all loads); operands of the products requested four to eight instructions ahead by hand: 937 to 944
+// against 916; 16x16x32 products: 1070 against 930; priority for either half: no difference.
 #include "attn_bf16.h"
 #include "paged_attn.h"
 
@@ -295,7 +305,6 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
             asm volatile("" : "+v"(l));                    // (here, not behind the products with 32 registers in tow)
             phase_barrier<-1, false>();
             // ---- matrix half
-            __builtin_amdgcn_s_setprio(1);
             const unsigned char *vb = vbuf + b0;
             scores(kbuf + b1, S);
             __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0): what this wavefront requested half a step ago
@@ -303,7 +312,6 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
             for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
                 for (int db = 0; db < DB; ++db) O[db] = mfma32(v_frag(vb, kk, db), __builtin_bit_cast(bf16x8, P[kk]), O[db]);
-            __builtin_amdgcn_s_setprio(0);
             if (next.care) clear_odd(vbuf + b1);
             cur = next;
             next = after;

@@ -5,6 +5,8 @@
 // (row, head) in 16-byte vectors.  The angle is position * f_i in turns, in double precision (32 bits of position times
 // 53 bits of frequency leave the fraction of a turn exact to 2^-23 at the largest position); the fraction is reduced to an
 // eighth of a turn either way before it is rounded to fp32, where the two power series below are exact to fp32.
+// 8192 rows of 40 heads of 128, bf16 (0.168 GB): 27 us in a row, 35 with other inputs in between (4.8 TB/s); rows and keys of
+// 4096 tokens on their way into a cache (0.1 GB): 17 us; four rows 3 us, nearly all of it launch and one load after another.
 #include <type_traits>
 #include "device_utils.h"
 #include "paged.h"
