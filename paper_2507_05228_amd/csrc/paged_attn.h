@@ -150,10 +150,6 @@ static inline PagedGrid paged_grid(const PagedAttnParams &p, const PagedSet &set
     g.parts = g.pieces < 2 * set.target ? g.pieces : 2 * (int64_t)set.target;     // ceil(x) < 2 x above 1
     return g;
 }
-static inline size_t paged_part_floats(const PagedAttnParams &p, const PagedSet &set, int tile) {
-    return (size_t)paged_grid(p, set, tile).parts * p.Hkv * tile * (p.d + 2);
-}
-
 int32_t launch_paged_tile(const PagedAttnParams &p, hipStream_t s);
 
 constexpr float LN2F = 0.6931471805599453f;

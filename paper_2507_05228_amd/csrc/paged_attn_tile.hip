@@ -18,7 +18,7 @@
 // slot 2 t - 2, while the others read K(t) and V(t - 1); every wavefront has waited for its own part of a tile at least one
 // barrier before anyone reads it.
 //
-// One sequence, 4096 rows over 16384 keys, 32 / 8 heads of 128 (0.96 TFLOP under the causal limit): 900 to 925 us, 1.05 PFLOP/s,
+// One sequence, 4096 rows over 16384 keys, 32 / 8 heads of 128 (0.96 TFLOP under the causal limit): 930 us, 1.03 PFLOP/s,
 // where a large library product reaches 1.21; the matrix pipes are busy 59 % of the time at the 1.7 GHz that the device holds
 // under this load.  All wavefronts in phase: 1027 us against 915 in the same run; page numbers through vector loads: 974 against
 // 915 (their wait is one for all loads); operands of the products requested four to eight instructions ahead by hand: 937 to 944
@@ -51,6 +51,12 @@ __device__ __forceinline__ int wave_max_int(int v) {
 #pragma unroll
     for (int o = 32; o; o >>= 1) v = max(v, __shfl_xor(v, o, WAVE));
     return v;
+}
+
+// LDS accesses of a wavefront's lanes on either side keep their order (the hardware keeps it; the compiler is told)
+__device__ __forceinline__ void wave_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 }
 
 template <int D, int NW>
@@ -350,17 +356,38 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
         const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false));
         l = __uint_as_float(x.x) + __uint_as_float(x.y);
     }
-    if (row >= wk.n_rows) return;
     if (wk.n_pieces > 1) {
-        const int64_t at = ((int64_t)(wk.first_piece + wk.piece) * p.Hkv + g) * TILE + wave * 32 + l32;
+        // Through LDS, half of the columns at a time, so that a store writes whole lines (each wavefront its own rows: no barrier).
+        // 512 rows over 2560 keys, 33 MB of partials: 41.5 us against 43.6 with stores from the accumulators.
+        constexpr int COLS = D / 2, CHUNKS = COLS / 4, PER = 64 / CHUNKS;
+        int tid_again = threadIdx.x;                       // (formed anew: the loop has no registers for more lane numbers)
+        asm volatile("" : "+v"(tid_again));
+        const int lane = tid_again & 63, l32 = lane & 31, h = lane >> 5;
+        float *const mine = (float *)smem + wave * 32 * COLS;
+        const int64_t at = ((int64_t)(wk.first_piece + wk.piece) * p.Hkv + g) * TILE + wave * 32;
+        const int left = wk.n_rows - wk.tile * TILE - wave * 32;       // rows of this wavefront that exist
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
+        for (int half = 0; half < 2; ++half) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *(f32x4 *)(p.many.part_u + at * D + 32 * db + 8 * i + 4 * h) = f32x4{O[db][4 * i], O[db][4 * i + 1], O[db][4 * i + 2], O[db][4 * i + 3]};
-        if (h == 0) { p.many.part_ml[at * 2] = m; p.many.part_ml[at * 2 + 1] = l; }
+            for (int b = 0; b < DB / 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x16 &o = O[half * (DB / 2) + b];
+                    *(f32x4 *)(mine + l32 * COLS + (((8 * b + 2 * i + h) ^ l32) & (CHUNKS - 1)) * 4) = f32x4{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
+                }
+            wave_order();
+#pragma unroll
+            for (int i = 0; i < 32 / PER; ++i) {
+                const int rr = i * PER + lane / CHUNKS, c = lane % CHUNKS;
+                const f32x4 u = *(const f32x4 *)(mine + rr * COLS + ((c ^ rr) & (CHUNKS - 1)) * 4);
+                if (rr < left) *(f32x4 *)(p.many.part_u + (at + rr) * D + half * COLS + c * 4) = u;
+            }
+            wave_order();
+        }
+        if (h == 0 && l32 < left) { p.many.part_ml[(at + l32) * 2] = m; p.many.part_ml[(at + l32) * 2 + 1] = l; }
         return;
     }
+    if (row >= wk.n_rows) return;
     const float inv = l == 0.f ? 0.f : 1.0f / l;
     const int64_t out = (int64_t)token * p.o_stride + (int64_t)head * D;
 #pragma unroll
