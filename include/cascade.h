@@ -511,7 +511,10 @@ CASCADE_API int32_t cascade_rope(const cascade_rope_desc *desc, int32_t dtype, i
  * page page_table[sequence][s][r / page_size] at row r % page_size.  A page is free if
  * its page_refs is 0.  Only pages whose rows are all in use are ever shared
  * (page_refs above 1): rows are only written behind the end of a list, in a page that
- * list holds alone.  One set of lists serves the pools of all layers.
+ * list holds alone.  One set of lists serves the pools of all layers.  After the caller
+ * has set them up (all lists -1, lengths and references 0), lists, lengths and references
+ * are changed by the calls below alone: a list that is cut short from outside keeps pages
+ * that the next extension would lose, and may end in one that others share.
  * The descriptor is read during the call; what it points to belongs to the caller.
  * Page ids and lengths are read on the device: an id outside [0, n_pages) holds no
  * keys (they are skipped like masked ones), lengths count up to max_pages * page_size. */
