@@ -77,9 +77,9 @@ __global__ __launch_bounds__(256, rows_occupancy(sizeof(T), DM, RB)) void paged_
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     PagedPlan<TILE, KEYS> plan;
     plan.make(p, p.few);
-    const int g = blockIdx.y;
+    const int piece = (int)(blockIdx.x / (uint32_t)p.Hkv), g = blockIdx.x - piece * p.Hkv;
     PagedWork wk;
-    if (!plan.template pick<false>(p, p.few, blockIdx.x, wk) || !wk.valid) return;
+    if (!plan.template pick<false>(p, p.few, piece, wk) || !wk.valid) return;
 
     // Keys that some row of the tile sees.  With one token those are all that the cache holds, as a rule, and a look at its limit
     // would only delay the first loads; several shards: first step of every shard, and its keys.
@@ -643,7 +643,7 @@ int32_t launch_rows(const PagedAttnParams &p, hipStream_t s) {
         auto kern = paged_rows_kernel<T, DM, RB>;
         static std::atomic<uint64_t> lds_ready{0};
         CASCADE_HIP_TRY(ensure_dynamic_lds((const void *)kern, sizeof(float) * 4 * TILE * (DM + 2), lds_ready));
-        hipLaunchKernelGGL(kern, dim3((unsigned)g.pieces, p.Hkv), dim3(256), lds, s, p);
+        hipLaunchKernelGGL(kern, dim3((unsigned)(g.pieces * p.Hkv)), dim3(256), lds, s, p);
         if (!p.many.target && g.split_tiles <= FEW_TILES) {
             hipLaunchKernelGGL((paged_merge_few_kernel<T, TILE, DM>), dim3((unsigned)min((int64_t)2048, g.split_tiles * p.Hkv * TILE)), dim3(256), 0, s, p);
             CASCADE_HIP_TRY(hipGetLastError());
@@ -719,6 +719,11 @@ int32_t check_attn(const cascade_paged_cache *c, const cascade_paged_attn_desc *
     if ((d->q_stride && d->q_stride < row) || (d->o_stride && d->o_stride < row)) return CASCADE_ESHAPE;
     const int vec = c->dtype == CASCADE_BF16 ? 8 : 4, o_vec = d->o_dtype == CASCADE_BF16 ? 8 : 4;
     if (d->q_stride % vec || d->o_stride % o_vec) return CASCADE_EUNSUPPORTED;
+    // a launch has less than 2^32 threads
+    PagedAttnParams p = {};
+    set_sizes(p, c, d);
+    if (p.many.target && paged_grid(p, p.many, PAGED_TILE).pieces * p.Hkv >= 1 << 23) return CASCADE_EUNSUPPORTED;
+    if (p.few.target && paged_grid(p, p.few, rows_tile(p, c->dtype == CASCADE_F32)).pieces * p.Hkv >= 1 << 24) return CASCADE_EUNSUPPORTED;
     return CASCADE_OK;
 }
 

@@ -72,11 +72,11 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void paged_tile_kernel(PagedAttnPa
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool second = wave >= NW / 2;                    // (the SIMD's other wavefront)
-    const int g = blockIdx.y;
+    const int piece = (int)(blockIdx.x / (uint32_t)p.Hkv), g = blockIdx.x - piece * p.Hkv;
     PagedWork wk;
     PagedPlan<TILE, KEYS> plan;
     plan.make(p, p.many);
-    if (!plan.template pick<false>(p, p.many, blockIdx.x, wk) || !wk.valid) return;
+    if (!plan.template pick<false>(p, p.many, piece, wk) || !wk.valid) return;
     const int64_t list0 = (int64_t)wk.b * p.S;
 
     // ---- keys of every shard that some row of the tile sees, and whether the lists name pages for them
@@ -409,7 +409,7 @@ int32_t launch_dim(const PagedAttnParams &p, hipStream_t s) {
     const int lds = 6 * KEYS * 2 * D + 4 * (3 * p.S + 3);
     static std::atomic<uint64_t> lds_ready{0};
     CASCADE_HIP_TRY(ensure_dynamic_lds((const void *)kern, 6 * KEYS * 2 * D + 4 * (3 * 1024 + 3), lds_ready));
-    hipLaunchKernelGGL(kern, dim3((unsigned)paged_grid(p, p.many, PAGED_TILE).pieces, p.Hkv), dim3(64 * NW), lds, s, p);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(paged_grid(p, p.many, PAGED_TILE).pieces * p.Hkv)), dim3(64 * NW), lds, s, p);
     CASCADE_HIP_TRY(hipGetLastError());
     return CASCADE_OK;
 }

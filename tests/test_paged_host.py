@@ -124,6 +124,18 @@ def test_attention_arguments(lib, desc, args, status):
                                   None, a["ws"], a["bytes"], None) == status
 
 
+@pytest.mark.parametrize("heads,dtype,d,rows", [(4, 0, 64, 1 << 27), (4, 1, 40, 1 << 27), (1024, 0, 4, 1 << 19)])
+def test_attention_of_more_rows_than_a_launch_holds(lib, heads, dtype, d, rows):
+    """16 rows of a kv head a workgroup of 256: 2^28 rows times heads are 2^32 threads."""
+    c = cache(dtype=dtype, head_dim=d, n_kv_heads=heads, n_seqs=1, n_pages=4, max_pages=4, page_size=16)
+    desc = cas.PagedAttnDesc(rows, heads, 1.0, dtype, 0, 0)
+    assert rows * heads >= 1 << 28
+    assert lib.cascade_paged_attn_workspace_bytes(C.byref(c), C.byref(desc)) == 0
+    assert lib.cascade_paged_attn(C.byref(c), 0, C.byref(desc), P, None, P, P, None, P, 1 << 40, None) == cas.EUNSUPPORTED
+    desc.rows = rows >> 4
+    assert lib.cascade_paged_attn_workspace_bytes(C.byref(c), C.byref(desc)) > 0
+
+
 def test_page_arguments(lib):
     c, many = C.byref(cache()), C.byref(cache(n_shards=3))
     assert lib.cascade_paged_extend(c, 0, P, None, P, P, P, None) == cas.EINVAL
