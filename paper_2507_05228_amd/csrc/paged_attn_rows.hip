@@ -520,9 +520,10 @@ __device__ __forceinline__ void merge_set(const PagedAttnParams &p, const PagedS
     PagedPlan<TILE, KEYS> plan;
     plan.make(p, set);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // units: 16 rows of a tile and kv head, every fourth one a wavefront's
+    // units: 16 rows of a tile and kv head, every fourth one a wavefront's; heads side by side as in the kernels that wrote the
+    // partials, so that with 8 of them a die reads what its cache may still hold (512 rows over 2560 keys: 43.9 -> 41 us)
     for (int unit = first;; unit += stride) {
-        const int part = unit % UNITS, rest = unit / UNITS, w = (int)((uint32_t)rest / (uint32_t)p.Hkv), g = rest - w * p.Hkv;
+        const int rest = (int)((uint32_t)unit / (uint32_t)p.Hkv), g = unit - rest * p.Hkv, part = rest % UNITS, w = rest / UNITS;
         PagedWork wk;
         if (!plan.template pick<true>(p, set, w, wk)) return;
         const int left = wk.n_rows - wk.tile * TILE - part * 16;       // rows of the unit that exist
@@ -544,7 +545,7 @@ __device__ __forceinline__ void merge_set_by_workgroups(const PagedAttnParams &p
     const int group = wave * SUB + lane / LPR;
     const int64_t step = (int64_t)p.Hkv * TILE;
     for (int unit = blockIdx.x;; unit += gridDim.x) {
-        const int row = unit % TILE, rest = unit / TILE, w = (int)((uint32_t)rest / (uint32_t)p.Hkv), g = rest - w * p.Hkv;
+        const int rest = (int)((uint32_t)unit / (uint32_t)p.Hkv), g = unit - rest * p.Hkv, row = rest % TILE, w = rest / TILE;
         PagedWork wk;
         if (!plan.template pick<true>(p, set, w, wk)) return;
         const int r = wk.tile * TILE + row;
