@@ -674,11 +674,14 @@ int32_t launch_type(const PagedAttnParams &p, hipStream_t s) {
 }
 
 // Sizes, and which sequences go to which kernel; as many pieces as workgroups are resident at once (32 / 8 heads of 128, one token
-// of 32 sequences of 1650 to 8200 keys, three workgroups a CU: 256, 512, 768, 1024 pieces 171, 129, 126, 125 us; 8 sequences of 4096:
-// 34, 32.5, 30, 33; five tokens, two workgroups a CU: 35.6, 36, 42.5, 45): bf16 with head dimensions of 64 and 128 has paged_attn_tile.hip for the
-// sequences of many rows, if the rows at hand can make one; with a single sequence it takes that with however many rows it has.
-// With no more rows than sequences it is left out (one token each, most likely; its launch costs 4 us for nothing then, and a
-// sequence that has several all the same is taken by the other kernel).
+// of 32 sequences of 1650 to 8200 keys, three workgroups a CU: 256, 512, 768, 1024 pieces 171, 129, 126, 125 us; 8 sequences of
+// 4096: 34, 32.5, 30, 33; five tokens, two workgroups a CU: 35.6, 36, 42.5, 45).  Beside sequences of many rows, where tiles hold
+// 32 rows that a short sequence does not fill, 384 pieces instead of 512 leave fewer that start when others end (15 of one and
+// four rows in 8 shards beside one of 509: 104 -> 98 us, 20 of one and three beside 300: 114 -> 109.5; without such a sequence 512
+// are ahead, four of five rows 32 against 33, 64 rows over 4160 keys 28.5 against 30).  Kernels: bf16 with head dimensions of 64
+// and 128 has paged_attn_tile.hip for the sequences of many rows, if the rows at hand can make one; with a single sequence it
+// takes that with however many rows it has. With no more rows than sequences it is left out (one token each, most likely; its
+// launch costs 4 us for nothing then, and a sequence that has several all the same is taken by the other kernel).
 void set_sizes(PagedAttnParams &p, const cascade_paged_cache *c, const cascade_paged_attn_desc *d) {
     p.rows = d->rows; p.H = d->n_heads; p.Hkv = c->n_kv_heads; p.rep = p.H / p.Hkv; p.d = c->head_dim;
     p.S = c->n_shards; p.B = c->n_seqs; p.max_pages = c->max_pages; p.page_shift = page_shift(c); p.n_pages = c->n_pages;
@@ -690,7 +693,8 @@ void set_sizes(PagedAttnParams &p, const cascade_paged_cache *c, const cascade_p
     };
     const bool f32 = c->dtype == CASCADE_F32, tiles = !f32 && (p.d == 64 || p.d == 128) && (int64_t)p.rows * p.rep > PAGED_FEW && (p.B == 1 || p.rows > p.B);
     if (tiles) set(p.many, p.B == 1 ? 0 : PAGED_FEW, INT32_MAX, PAGED_TILE_TARGET, 4);
-    if (!tiles || p.B > 1) set(p.few, 0, tiles ? PAGED_FEW : INT32_MAX, 256 * rows_occupancy(f32 ? 4 : 2, p.d, rows_tile(p, f32) / 16), 8);
+    const int tile = rows_tile(p, f32);
+    if (!tiles || p.B > 1) set(p.few, 0, tiles ? PAGED_FEW : INT32_MAX, tiles && tile == 32 ? 384 : 256 * rows_occupancy(f32 ? 4 : 2, p.d, tile / 16), 8);
 }
 size_t set_parts(PagedAttnParams &p, bool f32, float *workspace) {
     size_t floats = 0;

@@ -18,11 +18,12 @@
 // slot 2 t - 2, while the others read K(t) and V(t - 1); every wavefront has waited for its own part of a tile at least one
 // barrier before anyone reads it.
 //
-// One sequence, 4096 rows over 16384 keys, 32 / 8 heads of 128 (0.96 TFLOP under the causal limit): 930 us, 1.03 PFLOP/s,
-// where a large library product reaches 1.21; the matrix pipes are busy 59 % of the time at the 1.7 GHz that the device holds
-// under this load.  All wavefronts in phase: 1027 us against 915 in the same run; page numbers through vector loads: 974 against
-// 915 (their wait is one for all loads); operands of the products requested four to eight instructions ahead by hand: 937 to 944
-// against 916; 16x16x32 products: 1070 against 930; priority for either half: no difference.
+// One sequence, 4096 rows over 16384 keys, 32 / 8 heads of 128 (0.96 TFLOP under the causal limit): 832 us, 1.16 PFLOP/s, where
+// a large library product reaches 1.21; the matrix pipes are busy 58 % of the time at the 1.7 to 1.9 GHz that the device holds under
+// this load, the LDS about as long.  Each of the following against what was the kernel then: all wavefronts in phase 1027 against 915;
+// page numbers through vector loads 974 against 915 (their wait is one for all loads); operands of the products requested four to eight
+// instructions ahead by hand 937 to 944 against 916; 16x16x32 products 1070 against 930; requests behind the reads of V 855 against
+// 827; tiles of 128 rows 1526 against 893; priority for either half: no difference.
 #include "attn_bf16.h"
 #include "paged_attn.h"
 
