@@ -38,8 +38,12 @@ struct PagedAttnParams {
     PagedSet few, many;                                    // paged_attn_rows.hip, paged_attn_tile.hip
 };
 
-constexpr int PAGED_TILE = 256, PAGED_TILE_KEYS = 64, PAGED_TILE_TARGET = 256;      // paged_attn_tile.hip: rows of a tile, keys of a step; pieces
-constexpr int PAGED_FEW = 256;                             // flattened rows of a sequence up to which it goes to paged_attn_rows.hip
+// paged_attn_tile.hip: rows of a tile, keys of a step, and pieces, a workgroup for every CU (128 / 256 / 512 pieces: 256 rows over 8448
+// keys, 32 / 8 heads of 128, 70 / 61 / 77 us; 509 rows in 8 shards among short ones 117 / 99 / 111)
+constexpr int PAGED_TILE = 256, PAGED_TILE_KEYS = 64, PAGED_TILE_TARGET = 256;
+// Flattened rows of a sequence up to which it goes to paged_attn_rows.hip: up to one tile (64 / 256: 24 rows x 4 heads over 3024 keys 27 /
+// 21 us, 64 x 4 over 4160 36 / 29; 256 / 512: 100 x 4 over 4196 37 / 43, four such over 3100 52 / 73)
+constexpr int PAGED_FEW = 256;
 
 struct PagedWork {
     int b, first_row, n_rows;                              // sequence, its first row in q, its flattened rows
