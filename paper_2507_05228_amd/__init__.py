@@ -592,12 +592,13 @@ def _on(stream, t):
 
 
 def _head_rows(t, where):
-    """Row stride of a [rows, heads, d] tensor whose heads lie back to back."""
+    """Row stride of a [rows, heads, d] tensor whose heads lie back to back and whose rows do not overlap (a broadcast's stride
+    of 0 would mean dense rows to the library, which would walk over memory that the tensor does not have)."""
     if t.dim() == 3:
         (rows, heads, d), (sr, sh, sd) = t.shape, t.stride()
-        if sd == 1 and (heads < 2 or sh == d) and t.is_cuda:
+        if sd == 1 and (heads < 2 or sh == d) and (rows < 2 or sr >= heads * d) and t.is_cuda:
             return sr if rows > 1 else heads * d
-    raise CascadeError(ESHAPE, f"{where}: [rows, heads, d] with dense heads, on the GPU")
+    raise CascadeError(ESHAPE, f"{where}: [rows, heads, d] with dense heads and rows that do not overlap, on the GPU")
 
 
 def _checked(where, dtype, *tensors):
@@ -614,7 +615,7 @@ def _counted(where, *checks):
 
 
 def cascade_rope(desc, x, positions, y=None, stream=None):
-    """x [rows, heads, d] (heads dense, rows at any stride), positions int32 [rows]; y like x (None: in place)."""
+    """x [rows, heads, d] (heads dense, rows at any stride from heads * d on), positions int32 [rows]; y like x (None: in place)."""
     import torch
     lib = load_library()
     y = x if y is None else y
