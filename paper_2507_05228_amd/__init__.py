@@ -581,14 +581,19 @@ def _at(t):
     return None if t is None else t.data_ptr()
 
 
-def _on(stream, t):
-    """The stream's handle as a number (of the current stream: 0.3 us instead of 3 for a stream object); t, a tensor of the call,
-    must be on the current device, where the kernels will run."""
+def _on(stream, *tensors):
+    """The stream's handle as a number (of the current stream: 0.3 us instead of 3 for a stream object).  The tensors of the call
+    (None passes) must be on the current device, where the kernels will run, and so must the stream."""
     import torch
     device = torch.cuda.current_device()
-    if t.get_device() != device:
-        raise CascadeError(EINVAL, f"a tensor on device {t.get_device()}, the current device is {device}")
-    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise CascadeError(EINVAL, f"a tensor on device {t.get_device()}, the current device is {device}")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device)
+    if stream.device_index != device:
+        raise CascadeError(EINVAL, f"a stream of device {stream.device_index}, the current device is {device}")
+    return stream.cuda_stream
 
 
 def _head_rows(t, where):
@@ -623,16 +628,19 @@ def cascade_rope(desc, x, positions, y=None, stream=None):
     _counted("cascade_rope", (x.dim() == 3 and y.shape == x.shape and y.dtype == x.dtype, "y like x"),
              (positions is None or positions.numel() == x.shape[0], "a position per row"))
     st = lib.cascade_rope(C.byref(desc), _dtype_code(x), x.shape[0], x.shape[1], x.shape[2], _at(positions), _at(x),
-                          _head_rows(x, "cascade_rope"), _at(y), _head_rows(y, "cascade_rope"), _on(stream, x))
+                          _head_rows(x, "cascade_rope"), _at(y), _head_rows(y, "cascade_rope"), _on(stream, x, y, positions))
     _check(st, "cascade_rope")
 
 
 def make_paged_cache(k_pages, v_pages, page_table, kv_len, page_refs):
     """PagedCache of k_pages, v_pages [layers, pages, Hkv, page_size, d], page_table int32 [seqs, shards, max_pages], kv_len
-    int32 [seqs, shards] and page_refs int32 [pages].  The cache keeps the tensors alive."""
+    int32 [seqs, shards] and page_refs int32 [pages], all on one device.  The cache keeps the tensors alive; its device must be the
+    current one when a call is made, and every tensor of the call must be there."""
     import torch
     _checked("make_paged_cache", k_pages.dtype, k_pages, v_pages)
     _checked("make_paged_cache", torch.int32, page_table, kv_len, page_refs)
+    if len({t.get_device() for t in (k_pages, v_pages, page_table, kv_len, page_refs)}) > 1:
+        raise CascadeError(EINVAL, "make_paged_cache: tensors on several devices")
     _counted("make_paged_cache", (k_pages.dim() == 5 and v_pages.shape == k_pages.shape, "k_pages, v_pages [layers, pages, Hkv, page_size, d]"),
              (page_table.dim() == 3 and kv_len.shape == page_table.shape[:2], "page_table [seqs, shards, max_pages], kv_len [seqs, shards]"),
              (page_refs.shape == k_pages.shape[1:2], "page_refs [pages]"))
@@ -653,7 +661,7 @@ def cascade_paged_extend(cache, q_start, slots, visible, accepted, row_shard=Non
              (visible.numel() == rows * cache.n_shards, "visible [rows, shards]"), (accepted.numel() == cache.n_seqs, "accepted [seqs]"),
              (row_shard is None or row_shard.numel() == rows, "row_shard [rows]"))
     _check(lib.cascade_paged_extend(C.byref(cache), rows, _at(q_start), _at(row_shard), _at(slots), _at(visible), _at(accepted),
-                                    _on(stream, slots)), "cascade_paged_extend")
+                                    _on(stream, cache.tensors[0], q_start, slots, visible, accepted, row_shard)), "cascade_paged_extend")
 
 
 def cascade_paged_append(cache, layer, slots, k, v, positions=None, rope=None, q=None, q_out=None, stream=None):
@@ -676,7 +684,7 @@ def cascade_paged_append(cache, layer, slots, k, v, positions=None, rope=None, q
         heads, qs, qos = q.shape[1], _head_rows(q, where), _head_rows(q_out, where)
     st = lib.cascade_paged_append(C.byref(cache), layer, rows, _at(slots), _at(k), _at(v), _head_rows(k, where),
                                   None if rope is None else C.byref(rope), _at(positions), heads, _at(q), qs, _at(q_out), qos,
-                                  _on(stream, slots))
+                                  _on(stream, cache.tensors[0], slots, k, v, positions, q, q_out))
     _check(st, where)
 
 
@@ -700,7 +708,7 @@ def cascade_paged_attn(cache, layer, q, o, q_start, scale, visible=None, lse=Non
     desc = PagedAttnDesc(q.shape[0], q.shape[1], scale, _dtype_code(o), _head_rows(q, where), _head_rows(o, where))
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     st = lib.cascade_paged_attn(C.byref(cache), layer, C.byref(desc), _at(q_start), _at(visible), _at(q), _at(o), _at(lse),
-                                _at(workspace), ws_bytes, _on(stream, q))
+                                _at(workspace), ws_bytes, _on(stream, cache.tensors[0], q, o, q_start, visible, lse, workspace))
     _check(st, where)
 
 
@@ -709,7 +717,7 @@ def cascade_pages_free(cache, seqs, stream=None):
     import torch
     lib = load_library()
     _checked("cascade_pages_free", torch.int32, seqs)
-    _check(lib.cascade_pages_free(C.byref(cache), seqs.numel(), _at(seqs), _on(stream, seqs)), "cascade_pages_free")
+    _check(lib.cascade_pages_free(C.byref(cache), seqs.numel(), _at(seqs), _on(stream, cache.tensors[0], seqs)), "cascade_pages_free")
 
 
 def cascade_pages_workspace_bytes(cache):
@@ -724,7 +732,7 @@ def cascade_pages_fork(cache, src, dst, accepted, workspace, stream=None):
     _counted("cascade_pages_fork", (src.numel() == dst.numel() == accepted.numel(), "src, dst, accepted [n]"))
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib.cascade_pages_fork(C.byref(cache), src.numel(), _at(src), _at(dst), _at(accepted), _at(workspace), ws_bytes,
-                                  _on(stream, src)), "cascade_pages_fork")
+                                  _on(stream, cache.tensors[0], src, dst, accepted, workspace)), "cascade_pages_fork")
 
 
 def cascade_pages_compact(cache, n_live, workspace, stream=None):
@@ -733,7 +741,8 @@ def cascade_pages_compact(cache, n_live, workspace, stream=None):
     lib = load_library()
     _checked("cascade_pages_compact", torch.int32, n_live)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib.cascade_pages_compact(C.byref(cache), _at(n_live), _at(workspace), ws_bytes, _on(stream, cache.tensors[0])), "cascade_pages_compact")
+    _check(lib.cascade_pages_compact(C.byref(cache), _at(n_live), _at(workspace), ws_bytes, _on(stream, cache.tensors[0], n_live, workspace)),
+           "cascade_pages_compact")
 
 
 def cascade_pages_copy(cache, src, dst, stream=None):
@@ -742,7 +751,7 @@ def cascade_pages_copy(cache, src, dst, stream=None):
     lib = load_library()
     _checked("cascade_pages_copy", torch.int32, src, dst)
     _counted("cascade_pages_copy", (src.numel() == dst.numel(), "src, dst [n]"))
-    _check(lib.cascade_pages_copy(C.byref(cache), src.numel(), _at(src), _at(dst), _on(stream, src)), "cascade_pages_copy")
+    _check(lib.cascade_pages_copy(C.byref(cache), src.numel(), _at(src), _at(dst), _on(stream, cache.tensors[0], src, dst)), "cascade_pages_copy")
 
 
 def cascade_mfma_ceiling(lds_operands, iters=200000, stream=None):

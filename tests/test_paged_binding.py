@@ -1,5 +1,5 @@
 """What the binding of the paged cache's operators refuses before it hands addresses to the library.  The tensors here are host
-tensors that say they are on a GPU: a call that is not refused ends at the missing GPU, not in a launch."""
+tensors that say they are on a GPU, and the library is a list of the calls that reach it."""
 import pytest
 import torch
 
@@ -13,6 +13,23 @@ class OnGpu(torch.Tensor):
 
     def get_device(self):
         return self.device_id
+
+
+class Library:
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        return lambda *args: self.calls.append((name, args)) or cas.OK
+
+
+@pytest.fixture(autouse=True)
+def library(monkeypatch):
+    lib = Library()
+    monkeypatch.setattr(cas, "load_library", lambda: lib)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 4711, raising=False)
+    return lib
 
 
 def gpu(t, device=0):
@@ -37,14 +54,79 @@ def overlapping(rows, n, d=64):
     return gpu(torch.zeros(rows * n * d, dtype=torch.bfloat16).as_strided((rows, n, d), (d, d, 1)))
 
 
-def pool(device=0):
-    return cas.make_paged_cache(heads(8, 2).new_zeros(1, 4, 2, 16, 64), heads(8, 2).new_zeros(1, 4, 2, 16, 64), i32(2, 1, 3), i32(2, 1), i32(4))
+def pool_tensors():
+    return [*(gpu(torch.zeros(1, 4, 2, 16, 64, dtype=torch.bfloat16)) for _ in range(2)), i32(2, 1, 3), i32(2, 1), i32(4)]
+
+
+def pool():
+    return cas.make_paged_cache(*pool_tensors())
 
 
 def refused(status, call, *args, **kw):
     with pytest.raises(cas.CascadeError) as e:
         call(*args, **kw)
     assert e.value.status == status
+
+
+def calls():
+    """Every operator's call as it should be: (function, positional arguments, keyword arguments); a tensor each."""
+    rope = cas.make_rope_desc(64, 1e4)
+    room = lambda: gpu(torch.zeros(256, dtype=torch.uint8))  # noqa: E731
+    return [(cas.cascade_rope, [rope, heads(3, 4), i32(3), heads(3, 4)], {}),
+            (cas.cascade_paged_extend, [pool(), i32(3), i32(3), i32(3, 1), i32(2)], dict(row_shard=i32(3))),
+            (cas.cascade_paged_append, [pool(), 0, i32(3), heads(3, 2), heads(3, 2)],
+             dict(positions=i32(3), rope=rope, q=heads(3, 4), q_out=heads(3, 4))),
+            (cas.cascade_paged_attn, [pool(), 0, heads(3, 4), heads(3, 4), i32(3), 0.1],
+             dict(visible=i32(3, 1), lse=gpu(torch.zeros(4, 3)), workspace=room())),
+            (cas.cascade_pages_free, [pool(), i32(2)], {}),
+            (cas.cascade_pages_fork, [pool(), i32(2), i32(2), i32(2), room()], {}),
+            (cas.cascade_pages_compact, [pool(), i32(1), room()], {}),
+            (cas.cascade_pages_copy, [pool(), i32(2), i32(2)], {})]
+
+
+CALLS = range(8)
+
+
+def tensors_of(args, kw):
+    return [t for t in [*args, *kw.values()] if isinstance(t, torch.Tensor)]
+
+
+@pytest.mark.parametrize("i", CALLS)
+def test_a_good_call_reaches_the_library(i, library):
+    call, args, kw = calls()[i]
+    call(*args, **kw)
+    assert library.calls[0][0] == call.__name__ and library.calls[0][1][-1] == 4711
+
+
+@pytest.mark.parametrize("i", CALLS)
+def test_a_tensor_of_another_device(i, library):
+    call, args, kw = calls()[i]
+    for t in tensors_of(args, kw):
+        t.device_id = 1
+        refused(cas.EINVAL, call, *args, **kw)
+        t.device_id = 0
+    assert not library.calls
+
+
+@pytest.mark.parametrize("i", CALLS)
+def test_a_cache_or_a_stream_of_another_device(i, library):
+    call, args, kw = calls()[i]
+    if isinstance(args[0], cas.PagedCache):
+        for t in args[0].tensors:
+            t.device_id = 1
+        refused(cas.EINVAL, call, *args, **kw)
+    call, args, kw = calls()[i]
+    refused(cas.EINVAL, call, *args, **kw, stream=type("S", (), dict(cuda_stream=5, device_index=1))())
+    assert not library.calls
+    call(*args, **kw, stream=type("S", (), dict(cuda_stream=5, device_index=0))())
+    assert library.calls[0][1][-1] == 5
+
+
+def test_a_cache_on_two_devices():
+    for i in range(5):
+        tensors = pool_tensors()
+        tensors[i].device_id = 1
+        refused(cas.EINVAL, cas.make_paged_cache, *tensors)
 
 
 @pytest.mark.parametrize("odd", [broadcast, overlapping])
