@@ -613,6 +613,15 @@ def _checked(where, dtype, *tensors):
             raise CascadeError(ESHAPE, f"{where}: contiguous {dtype} tensors on the GPU")
 
 
+def _room(workspace, where):
+    """Address and bytes of a workspace: dense, on the GPU (None passes, and the library refuses it)."""
+    if workspace is None:
+        return None, 0
+    if not (workspace.is_cuda and workspace.is_contiguous()):
+        raise CascadeError(EWORKSPACE, f"{where}: a contiguous workspace on the GPU")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
 def _counted(where, *checks):
     for ok, what in checks:
         if not ok:
@@ -706,9 +715,9 @@ def cascade_paged_attn(cache, layer, q, o, q_start, scale, visible=None, lse=Non
              (visible is None or visible.numel() == q.shape[0] * cache.n_shards, "visible [rows, shards]"),
              (lse is None or lse.numel() == q.shape[0] * q.shape[1], "lse [H, rows]"))
     desc = PagedAttnDesc(q.shape[0], q.shape[1], scale, _dtype_code(o), _head_rows(q, where), _head_rows(o, where))
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    ws, ws_bytes = _room(workspace, where)
     st = lib.cascade_paged_attn(C.byref(cache), layer, C.byref(desc), _at(q_start), _at(visible), _at(q), _at(o), _at(lse),
-                                _at(workspace), ws_bytes, _on(stream, cache.tensors[0], q, o, q_start, visible, lse, workspace))
+                                ws, ws_bytes, _on(stream, cache.tensors[0], q, o, q_start, visible, lse, workspace))
     _check(st, where)
 
 
@@ -730,8 +739,8 @@ def cascade_pages_fork(cache, src, dst, accepted, workspace, stream=None):
     lib = load_library()
     _checked("cascade_pages_fork", torch.int32, src, dst, accepted)
     _counted("cascade_pages_fork", (src.numel() == dst.numel() == accepted.numel(), "src, dst, accepted [n]"))
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib.cascade_pages_fork(C.byref(cache), src.numel(), _at(src), _at(dst), _at(accepted), _at(workspace), ws_bytes,
+    ws, ws_bytes = _room(workspace, "cascade_pages_fork")
+    _check(lib.cascade_pages_fork(C.byref(cache), src.numel(), _at(src), _at(dst), _at(accepted), ws, ws_bytes,
                                   _on(stream, cache.tensors[0], src, dst, accepted, workspace)), "cascade_pages_fork")
 
 
@@ -740,8 +749,8 @@ def cascade_pages_compact(cache, n_live, workspace, stream=None):
     import torch
     lib = load_library()
     _checked("cascade_pages_compact", torch.int32, n_live)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib.cascade_pages_compact(C.byref(cache), _at(n_live), _at(workspace), ws_bytes, _on(stream, cache.tensors[0], n_live, workspace)),
+    ws, ws_bytes = _room(workspace, "cascade_pages_compact")
+    _check(lib.cascade_pages_compact(C.byref(cache), _at(n_live), ws, ws_bytes, _on(stream, cache.tensors[0], n_live, workspace)),
            "cascade_pages_compact")
 
 

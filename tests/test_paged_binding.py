@@ -129,6 +129,17 @@ def test_a_cache_on_two_devices():
         refused(cas.EINVAL, cas.make_paged_cache, *tensors)
 
 
+@pytest.mark.parametrize("room", [torch.zeros(256, dtype=torch.uint8), gpu(torch.zeros(1, dtype=torch.uint8).expand(256)),
+                                  gpu(torch.zeros(512, dtype=torch.uint8)[::2])])
+def test_a_workspace_on_the_host_or_with_gaps(room, library):
+    for call, args, kw in calls():
+        if "workspace" in kw:
+            refused(cas.EWORKSPACE, call, *args, **{**kw, "workspace": room})
+        elif any(t.dtype == torch.uint8 for t in tensors_of(args, kw)):
+            refused(cas.EWORKSPACE, call, *args[:-1], room)
+    assert not library.calls
+
+
 @pytest.mark.parametrize("odd", [broadcast, overlapping])
 def test_rows_that_share_memory(odd):
     """A row stride of 0 is the library's word for dense rows: a broadcast would be read, or written, far beyond its one row."""
