@@ -1,0 +1,19 @@
+"""Sizes of the paged cache next to what its 32-bit counts hold (host only: nothing is launched)."""
+import ctypes as C
+
+import pytest
+
+import paper_2507_05228_amd as cas
+from test_paged_host import P, cache, lib  # noqa: F401
+
+
+@pytest.mark.parametrize("max_pages", [(1 << 27) - 1, (1 << 27) - 4])
+def test_lists_whose_last_step_would_pass_31_bits(lib, max_pages):  # noqa: F811
+    """A walk goes in steps of up to 64 keys; the end of the last one counts in 32 bits too."""
+    c = cache(n_seqs=1, page_size=16, max_pages=max_pages)
+    desc = cas.PagedAttnDesc(4, 4, 1.0, cas.BF16, 0, 0)
+    assert lib.cascade_paged_attn_workspace_bytes(C.byref(c), C.byref(desc)) == 0
+    assert lib.cascade_paged_attn(C.byref(c), 0, C.byref(desc), P, None, P, P, None, P, 1 << 40, None) == cas.EUNSUPPORTED
+    assert lib.cascade_paged_extend(C.byref(c), 1, P, P, P, P, P, None) == cas.EUNSUPPORTED
+    c.max_pages = (1 << 27) - 5
+    assert lib.cascade_paged_attn_workspace_bytes(C.byref(c), C.byref(desc)) > 0
