@@ -193,7 +193,8 @@ __global__ __launch_bounds__(256, rows_occupancy(sizeof(T), DM, RB)) void paged_
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) limit_off[rb] = (uint32_t)(token[rb] - wk.first_row) * (uint32_t)(p.S * 4);
     auto seen_of = [&](const Step &x, int rb) {            // keys of a step that a row sees
-        const int n = p.visible ? min(x.rows, x.limit[rb] - x.j0) : x.rows;
+        // (limits below 0 are 0: the lowest of the type would pass 2^31 in the difference)
+        const int n = p.visible ? min(x.rows, max(x.limit[rb], 0) - x.j0) : x.rows;
         return min(max(n, 0), KEYS);
     };
     // The rows of 16 keys that exist: what lies behind them is outside the descriptor and arrives as zeros
