@@ -581,6 +581,8 @@ CASCADE_API int32_t cascade_paged_append(const cascade_paged_cache *cache, int32
  * q, o 16-byte aligned, strides in elements (0: dense) and multiples of 16 bytes; o must
  * not overlap q.  Calls that may overlap in time need a workspace each (16-byte aligned);
  * its contents need not be kept between calls.  Two sequences must not share rows.
+ * Over a bf16 cache the weights enter the product with the values in 16 bits; where a sequence has more than 256 rows
+ * times heads of a kv head (head dimensions 64 and 128), rounded to bf16.
  * A call with the same arguments gives the same bits each time; those of a row may depend
  * on the other rows and lengths of the call, which decide how the work is cut.
  * Errors: EINVAL, ESHAPE (n_heads % H_KV, strides, layer), EUNSUPPORTED (alignment,

@@ -18,13 +18,19 @@
 // way.  32 sequences of 1650 to 8200 keys, 32 / 8 heads of 128 (0.64 GB): 121 us, 5.3 TB/s (copying reaches 5.1).
 //
 // The exponent offset of a row moves when a score exceeds it by more than 2^8 (in log2 units), so that nearly every step
-// leaves the accumulators alone; sums of exponentials and products are fp32, the exponentials enter the second product in the
-// cache's type (rounded to bf16: 2^-8 of a weight at most, as everywhere in this library).
+// leaves the accumulators alone; sums of exponentials and products are fp32.  Over a bf16 cache an exponential enters the second
+// product as two bf16 numbers (off by 2^-15 + 2^-18 at most): one rounding to bf16 would be as far off as that of the result, and the
+// decode kernel for slabs has fp32 weights.  The matrix pipes have the time while the cache is read: with one number instead of two,
+// 32 sequences of 1650 to 8200 keys 128.5 / 128.7 us, four of 333 to 2048 13.7 / 13.7, 64 rows over 4160 32.2 / 32.2; only long chunks of
+// other head dimensions are bound by them, 1024 rows over 4024 keys, 32 / 8 heads of 96, 104 / 120.
 #include "paged_attn.h"
 
 namespace {
 
 constexpr float RAISE = 8.0f;
+// An exponential goes into the products as two bf16 numbers, its upper half (cut off) and what that leaves of OVER times it: more
+// than nothing and of the same sign, so that a value that is infinite stays so in both products
+constexpr float OVER = 1.0f + 0x1p-18f;
 // Tiles up to which a merge has a workgroup for a row (0 / 8 / 32: one row over 32768 keys 37 / 30 / 30 us, nine over 3000 20 / 16 / 16;
 // 100, 37 and 1 rows in fp32 19.5 / 19.5 / 21.5, sixteen rows of four sequences 30 / 30 / 27.5)
 constexpr int FEW_TILES = 8;
@@ -317,11 +323,17 @@ __global__ __launch_bounds__(256, rows_occupancy(sizeof(T), DM, RB)) void paged_
                 }
         }
         if constexpr (BF) {
-            bf16x8 P[RB];
+            u32x4 P[2][RB];                                // [0] upper halves of the exponentials, [1] what they leave
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) P[rb][j] = (bf16_t)s[rb][j / 4][j % 4];
+                for (int j = 0; j < 4; ++j) {
+                    const float e0 = s[rb][j / 2][j % 2 * 2], e1 = s[rb][j / 2][j % 2 * 2 + 1];
+                    const uint32_t b0 = __float_as_uint(e0), b1 = __float_as_uint(e1);
+                    P[0][rb][j] = __builtin_amdgcn_perm(b1, b0, 0x07060302);
+                    P[1][rb][j] = __builtin_bit_cast(uint32_t, bf16x2{(bf16_t)fmaf(e0, OVER, -__uint_as_float(b0 & 0xffff0000u)),
+                                                                      (bf16_t)fmaf(e1, OVER, -__uint_as_float(b1 & 0xffff0000u))});
+                }
 #pragma unroll
             for (int w = 0; w < VW; ++w) {                 // columns RUN c16 + 2 w and + 1 (mod RUN)
                 u32x4 even, odd;
@@ -332,10 +344,13 @@ __global__ __launch_bounds__(256, rows_occupancy(sizeof(T), DM, RB)) void paged_
                     odd[j] = __builtin_amdgcn_perm(b, a, 0x07060302);
                 }
 #pragma unroll
-                for (int rb = 0; rb < RB; ++rb) {
-                    O[rb][2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), P[rb], O[rb][2 * w], 0, 0, 0);
-                    O[rb][2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), P[rb], O[rb][2 * w + 1], 0, 0, 0);
-                }
+                for (int half = 0; half < 2; ++half)
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) {
+                        const bf16x8 e = __builtin_bit_cast(bf16x8, P[half][rb]);
+                        O[rb][2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), e, O[rb][2 * w], 0, 0, 0);
+                        O[rb][2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), e, O[rb][2 * w + 1], 0, 0, 0);
+                    }
             }
         } else {
 #pragma unroll

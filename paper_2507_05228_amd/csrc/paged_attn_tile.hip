@@ -18,6 +18,10 @@
 // slot 2 t - 2, while the others read K(t) and V(t - 1); every wavefront has waited for its own part of a tile at least one
 // barrier before anyone reads it.
 //
+// The exponentials are rounded to bf16 in front of the second product (off by 2^-8 at most; their sum takes them in fp32), as in the
+// attention of whole layers: a second product for what the rounding leaves, as paged_attn_rows.hip has it, would be half as much
+// again for the matrix pipes, which bound this kernel.
+//
 // One sequence, 4096 rows over 16384 keys, 32 / 8 heads of 128 (0.96 TFLOP under the causal limit): 832 us, 1.16 PFLOP/s, where
 // a large library product reaches 1.21; the matrix pipes are busy 58 % of the time at the 1.7 to 1.9 GHz that the device holds under
 // this load, the LDS about as long.  Each of the following against what was the kernel then: all wavefronts in phase 1027 against 915;
