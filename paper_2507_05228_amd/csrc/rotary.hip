@@ -198,12 +198,25 @@ int32_t launch_rotary(RotaryParams p, bool interleaved, uintptr_t alignment, hip
     // Rows of a workgroup: enough workgroups for the 256 CUs first, then as many rows as share one evaluation of the angles
     const int most = p.rot ? max(1, min(MAX_ROWS, 2 * MAX_PAIRS / p.rot)) : MAX_ROWS;
     p.rows_per_wg = max(1, min(most, p.rows / 1024));
-    const dim3 grid((p.rows + p.rows_per_wg - 1) / p.rows_per_wg);
-    if (wide && interleaved) hipLaunchKernelGGL((rotary_kernel<T, VEC, true>), grid, dim3(256), 0, s, p);
-    else if (wide) hipLaunchKernelGGL((rotary_kernel<T, VEC, false>), grid, dim3(256), 0, s, p);
-    else if (interleaved) hipLaunchKernelGGL((rotary_kernel<T, 1, true>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((rotary_kernel<T, 1, false>), grid, dim3(256), 0, s, p);
-    CASCADE_HIP_TRY(hipGetLastError());
+    // A launch has less than 2^32 threads: 2^23 workgroups' rows at a time
+    const auto moved = [](auto *x, int64_t elems) { return x ? (decltype(x))((const T *)x + elems) : x; };
+    const int64_t at_once = (int64_t)p.rows_per_wg << 23;
+    for (int64_t first = 0; first < p.rows; first += at_once) {
+        RotaryParams c = p;
+        c.rows = (int32_t)min(at_once, p.rows - first);
+        c.q = moved(p.q, first * p.q_stride);
+        c.q_out = moved(p.q_out, first * p.q_out_stride);
+        c.k = moved(p.k, first * p.kv_stride);
+        c.v = moved(p.v, first * p.kv_stride);
+        if (p.positions) c.positions = p.positions + first;
+        if (p.slots) c.slots = p.slots + first;
+        const dim3 grid((unsigned)(((int64_t)c.rows + p.rows_per_wg - 1) / p.rows_per_wg));
+        if (wide && interleaved) hipLaunchKernelGGL((rotary_kernel<T, VEC, true>), grid, dim3(256), 0, s, c);
+        else if (wide) hipLaunchKernelGGL((rotary_kernel<T, VEC, false>), grid, dim3(256), 0, s, c);
+        else if (interleaved) hipLaunchKernelGGL((rotary_kernel<T, 1, true>), grid, dim3(256), 0, s, c);
+        else hipLaunchKernelGGL((rotary_kernel<T, 1, false>), grid, dim3(256), 0, s, c);
+        CASCADE_HIP_TRY(hipGetLastError());
+    }
     return CASCADE_OK;
 }
 
