@@ -547,7 +547,7 @@ typedef struct cascade_paged_cache {
  * free page, later ones that need one are refused too.  Rows behind the last sequence
  * (a padded batch) have slot -1 and see nothing; so does a row whose shard id is outside
  * [0, n_shards), but it sees what its neighbours see.
- * Errors: EINVAL, EUNSUPPORTED (sizes above), EHIP.                                 */
+ * Errors: EINVAL, EUNSUPPORTED (sizes above, rows above 2^31 - 1025), EHIP.                                 */
 CASCADE_API int32_t cascade_paged_extend(const cascade_paged_cache *cache, int32_t rows, const int32_t *q_start_dev,
                              const int32_t *row_shard_dev, int32_t *slots, int32_t *visible, int32_t *accepted,
                              void *stream);

@@ -498,6 +498,7 @@ extern "C" int32_t cascade_paged_extend(const cascade_paged_cache *cache, int32_
     const int32_t st = check_paged_cache(cache);
     if (st != CASCADE_OK) return st;
     if (rows <= 0 || !q_start_dev || !slots || !visible || !accepted || (cache->n_shards > 1 && !row_shard_dev)) return CASCADE_EINVAL;
+    if (rows > INT32_MAX - 1024) return CASCADE_EUNSUPPORTED;      // (rows are walked over 1024 at a time, counted in 32 bits)
     ExtendParams p = {};
     p.l = lists_of(cache);
     p.q_start = q_start_dev; p.row_shard = row_shard_dev; p.slots = slots; p.visible = visible; p.accepted = accepted;

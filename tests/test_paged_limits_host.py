@@ -17,3 +17,10 @@ def test_lists_whose_last_step_would_pass_31_bits(lib, max_pages):  # noqa: F811
     assert lib.cascade_paged_extend(C.byref(c), 1, P, P, P, P, P, None) == cas.EUNSUPPORTED
     c.max_pages = (1 << 27) - 5
     assert lib.cascade_paged_attn_workspace_bytes(C.byref(c), C.byref(desc)) > 0
+
+
+@pytest.mark.parametrize("rows", [2 ** 31 - 1024, 2 ** 31 - 1])
+def test_extensions_whose_last_walk_would_pass_31_bits(lib, rows):  # noqa: F811
+    """Rows are walked over 1024 at a time, by threads that stop at the first row behind the last."""
+    for n_shards, shard in ((1, None), (1, P), (3, P)):
+        assert lib.cascade_paged_extend(C.byref(cache(n_shards=n_shards)), rows, P, shard, P, P, P, None) == cas.EUNSUPPORTED
