@@ -64,7 +64,8 @@ __device__ __forceinline__ float rows_sum(float v) {
     return v + __shfl_xor(v, 32, WAVE);
 }
 
-// Wavefronts per SIMD that the registers allow: keys and values of a step, queries and accumulators, and some 70 more
+// Wavefronts per SIMD that the registers allow, from below: keys and values of a step, queries and accumulators, and some 70 more
+// (bf16 heads up to 64 and 65 to 128, 16 rows a tile, take 109 and 167 registers, room for one wavefront more than this counts)
 constexpr int rows_occupancy(int size, int DM, int RB) {
     const int regs = DM / 4 * size + (DM / 16 * size + DM / 4) * RB + 70;
     return regs <= 168 ? 3 : regs <= 256 ? 2 : 1;
@@ -686,14 +687,18 @@ int32_t launch_dim(const PagedAttnParams &p, hipStream_t s) {
         if (rows_tile(p, sizeof(T) == 4) == 32) return launch_rows<T, DM, 2>(p, s);
     return launch_rows<T, DM, 1>(p, s);
 }
+// (fp32 heads of more than 128 need more than the 512 registers there are: 28 bytes a lane are spilled, written in front of the walk and
+// read behind it and, 8 of them, in steps that move the exponent offset)
 template <typename T>
 int32_t launch_type(const PagedAttnParams &p, hipStream_t s) {
     return p.d <= 64 ? launch_dim<T, 64>(p, s) : p.d <= 128 ? launch_dim<T, 128>(p, s) : launch_dim<T, 256>(p, s);
 }
 
-// Sizes, and which sequences go to which kernel; as many pieces as workgroups are resident at once (32 / 8 heads of 128, one token
-// of 32 sequences of 1650 to 8200 keys, three workgroups a CU: 256, 512, 768, 1024 pieces 171, 129, 126, 125 us; 8 sequences of
-// 4096: 34, 32.5, 30, 33; five tokens, two workgroups a CU: 35.6, 36, 42.5, 45).  Beside sequences of many rows, where tiles hold
+// Sizes, and which sequences go to which kernel; as many pieces as workgroups are resident at once by rows_occupancy (32 / 8 heads of
+// 128, five tokens of 8 sequences of 3000 keys, two workgroups a CU: 256, 512, 768, 1024 pieces 35.6, 36, 42.5, 45 us).  One token each
+// would have room for three of them, but gains only where walks are very long, and loses where partials count, 512 / 768 pieces: 32
+// sequences of 1650 to 8200 keys 128 / 128, 16 of 16000 217 / 209, 8 of 4096 34.9 / 34.8, 32 of 4000 with 64 / 8 heads 99 / 101, one of 32000
+// 34.5 / 36.3, two tokens of 8 of 3000 28.3 / 29.3.  Beside sequences of many rows, where tiles hold
 // 32 rows that a short sequence does not fill, 384 pieces instead of 512 leave fewer that start when others end (15 of one and
 // four rows in 8 shards beside one of 509: 104 -> 98 us, 20 of one and three beside 300: 114 -> 109.5; without such a sequence 512
 // are ahead, four of five rows 32 against 33, 64 rows over 4160 keys 28.5 against 30).  Kernels: bf16 with head dimensions of 64
