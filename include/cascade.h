@@ -516,6 +516,9 @@ CASCADE_API int32_t cascade_rope(const cascade_rope_desc *desc, int32_t dtype, i
  * are changed by the calls below alone: a list that is cut short from outside keeps pages
  * that the next extension would lose, and may end in one that others share.
  * The descriptor is read during the call; what it points to belongs to the caller.
+ * Calls look at all n_seqs sequences, those without new rows too, and attention takes n_seqs for how many have rows
+ * when it chooses a kernel.  A descriptor of neighbouring sequences alone (page_table and kv_len moved to the first
+ * of them, n_seqs their number) serves every call but cascade_pages_compact, which has to know all lists.
  * Page ids and lengths are read on the device: an id outside [0, n_pages) holds no
  * keys (they are skipped like masked ones), lengths count up to max_pages * page_size. */
 typedef struct cascade_paged_cache {

@@ -644,7 +644,8 @@ def cascade_rope(desc, x, positions, y=None, stream=None):
 def make_paged_cache(k_pages, v_pages, page_table, kv_len, page_refs):
     """PagedCache of k_pages, v_pages [layers, pages, Hkv, page_size, d], page_table int32 [seqs, shards, max_pages], kv_len
     int32 [seqs, shards] and page_refs int32 [pages], all on one device.  The cache keeps the tensors alive; its device must be the
-    current one when a call is made, and every tensor of the call must be there."""
+    current one when a call is made, and every tensor of the call must be there.  page_table[a:b] and kv_len[a:b] make a cache of these
+    sequences alone, which serves all calls but cascade_pages_compact and is the faster one where others are idle."""
     import torch
     _checked("make_paged_cache", k_pages.dtype, k_pages, v_pages)
     _checked("make_paged_cache", torch.int32, page_table, kv_len, page_refs)

@@ -704,7 +704,11 @@ int32_t launch_type(const PagedAttnParams &p, hipStream_t s) {
 // are ahead, four of five rows 32 against 33, 64 rows over 4160 keys 28.5 against 30).  Kernels: bf16 with head dimensions of 64
 // and 128 has paged_attn_tile.hip for the sequences of many rows, if the rows at hand can make one; with a single sequence it
 // takes that with however many rows it has. With no more rows than sequences it is left out (one token each, most likely; its
-// launch costs 4 us for nothing then, and a sequence that has several all the same is taken by the other kernel).
+// launch costs 4 us for nothing then, and a sequence that has several all the same is taken by the other kernel).  That holds for
+// caches with many idle sequences too, although a chunk of fewer rows than there are sequences is guessed wrong: every workgroup looks at
+// all sequences, so that the launch itself is dear there.  Without / with it, 32 / 8 heads of 128: one token of 100, 512 and 1024
+// sequences of 64 keys 20.6 / 27.9, 117 / 149 and 334 / 394 us; in a cache of 1024 sequences one with 65, 512 and 1000 rows over 2000 and
+// themselves 109 / 151, 355 / 369 and 458 / 418, and 70 through a descriptor of that sequence alone.
 void set_sizes(PagedAttnParams &p, const cascade_paged_cache *c, const cascade_paged_attn_desc *d) {
     p.rows = d->rows; p.H = d->n_heads; p.Hkv = c->n_kv_heads; p.rep = p.H / p.Hkv; p.d = c->head_dim;
     p.S = c->n_shards; p.B = c->n_seqs; p.max_pages = c->max_pages; p.page_shift = page_shift(c); p.n_pages = c->n_pages;
