@@ -526,9 +526,9 @@ typedef struct cascade_paged_cache {
     int32_t n_layers, n_pages;
     int32_t n_kv_heads, head_dim;     /* head_dim: a multiple of 8 (bf16) or 4 (f32), at most 256 */
     int32_t page_size;                /* rows: a power of two, 16 .. 65536             */
-    int32_t n_seqs, n_shards;         /* n_shards: at most 1024; lists, pages and rows
-                                         of the pools: 31 bits each; rows of a list:
-                                         at most 2^31 - 65                             */
+    int32_t n_seqs, n_shards;         /* n_shards: at most 1024; rows of the pools: 31
+                                         bits; rows of a list: at most 2^31 - 65; entries
+                                         of page_table: at most 2^31 - 4097            */
     int32_t max_pages;                /* of a list                                     */
     void *k_pages, *v_pages;          /* [n_layers, n_pages, H_KV, page_size, d], 16-byte aligned */
     int32_t *page_table;              /* [n_seqs, n_shards, max_pages]; unused entries -1 */

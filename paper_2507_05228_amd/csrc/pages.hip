@@ -238,7 +238,7 @@ __global__ __launch_bounds__(256) void paged_rows_slots_kernel(ExtendParams p) {
     auto seq_of = [&](int row) {
         int lo = 0, hi = l.n_seqs;
         while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
+            const int mid = lo + ((hi - lo) >> 1);
             if (p.q_start[mid] <= row) lo = mid; else hi = mid;
         }
         return lo;

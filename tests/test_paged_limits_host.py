@@ -24,3 +24,15 @@ def test_extensions_whose_last_walk_would_pass_31_bits(lib, rows):  # noqa: F811
     """Rows are walked over 1024 at a time, by threads that stop at the first row behind the last."""
     for n_shards, shard in ((1, None), (1, P), (3, P)):
         assert lib.cascade_paged_extend(C.byref(cache(n_shards=n_shards)), rows, P, shard, P, P, P, None) == cas.EUNSUPPORTED
+
+
+@pytest.mark.parametrize("change", [dict(n_seqs=2 ** 31 - 1), dict(n_seqs=2 ** 31 - 4096), dict(n_seqs=1, n_shards=662, max_pages=3243933)])
+def test_lists_whose_last_round_would_pass_31_bits(lib, change):  # noqa: F811
+    """Sequences are taken 4096 at a time, entries of a list by 256 threads at a time."""
+    c = cache(**{**dict(n_shards=1, max_pages=1), **change})
+    assert c.n_seqs * c.n_shards * c.max_pages in (2 ** 31 - 1, 2 ** 31 - 4096, 2 ** 31 - 2)
+    c = C.byref(c)
+    assert lib.cascade_paged_extend(c, 1, P, P, P, P, P, None) == cas.EUNSUPPORTED
+    assert lib.cascade_pages_free(c, 1, P, None) == cas.EUNSUPPORTED
+    assert lib.cascade_pages_workspace_bytes(c) == 0
+    assert lib.cascade_pages_workspace_bytes(C.byref(cache(n_shards=1, max_pages=1, n_seqs=2 ** 31 - 4097))) > 0
