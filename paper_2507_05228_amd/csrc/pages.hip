@@ -3,9 +3,12 @@
 // The state is plain arrays (lists, lengths, references) and a page is free if nothing refers to it: there is no list of free
 // pages whose order could depend on timing.  Whoever needs pages gets the lowest free ones, list by list, so that the same
 // calls give the same lists every time.  The index work is one workgroup with prefix sums, bound by latency: a scan of the
-// references (32 KB for 8192 pages) and some ten barriers, 9 us for 8 sequences, 11 for 32 lists; forks of 16 sequences 8 us.
-// The rows' slots and limits go to as many wavefronts as there are 64 rows (4096 rows in 16 shards: 8 us; in the one workgroup,
-// whose scattered stores held it up, 47).  Copies of pages are spread over the chip and bound by HBM: 0.27 GB read and written in
+// references (32 KB for 8192 pages) and some ten barriers, 9 us for 8 sequences, 11 for 32 lists; forks of 16 sequences 8 us.  Not all
+// of that must be: the eight references of a thread, and the lengths, the starts and the references, are waited for one after the
+// other, and a pool of 100000 pages has thirteen such rounds (64 sequences, a row each: 45 us against 7 with 5000 pages).
+// The rows' slots and limits go to as many wavefronts as there are 64 rows (4096 rows in 16 shards: 8 us, most of them for the
+// shards' lengths, one load after the other; in the one workgroup, whose scattered stores held it up, 47); each of them counts
+// the rows behind its own to the end of the sequence, which is quadratic in a sequence's rows.  Copies of pages are spread over the chip and bound by HBM: 0.27 GB read and written in
 // 39 us, 6.9 TB/s (part of it stays in the last-level cache).
 #include "device_utils.h"
 #include "paged.h"
