@@ -87,6 +87,7 @@ class PagedCache(C.Structure):
                 ("head_dim", C.c_int32), ("page_size", C.c_int32), ("n_seqs", C.c_int32), ("n_shards", C.c_int32),
                 ("max_pages", C.c_int32), ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_table", C.c_void_p),
                 ("kv_len", C.c_void_p), ("page_refs", C.c_void_p)]
+    tensors = (None,) * 5                                  # of make_paged_cache; a descriptor of bare addresses has none
 
 
 class PagedAttnDesc(C.Structure):
@@ -591,7 +592,7 @@ def _on(stream, *tensors):
             raise CascadeError(EINVAL, f"a tensor on device {t.get_device()}, the current device is {device}")
     if stream is None:
         return torch._C._cuda_getCurrentRawStream(device)
-    if stream.device_index != device:
+    if getattr(stream, "device_index", device) != device:  # (whatever has a handle serves as a stream, as in the other calls)
         raise CascadeError(EINVAL, f"a stream of device {stream.device_index}, the current device is {device}")
     return stream.cuda_stream
 

@@ -154,3 +154,11 @@ def test_rows_that_share_memory(odd):
     q_start = i32(3)
     refused(cas.ESHAPE, cas.cascade_paged_attn, cache, 0, odd(3, 4), q, q_start, 0.1)
     refused(cas.ESHAPE, cas.cascade_paged_attn, cache, 0, q, odd(3, 4), q_start, 0.1)
+
+
+@pytest.mark.parametrize("i", range(1, 8))
+def test_a_descriptor_of_bare_addresses_and_a_bare_stream(i, library):
+    call, (cache, *args), kw = calls()[i]
+    bare = cas.PagedCache(*(getattr(cache, name) for name, _ in cas.PagedCache._fields_))
+    call(bare, *args, **kw, stream=type("S", (), dict(cuda_stream=5))())
+    assert library.calls[0][0] == call.__name__ and library.calls[0][1][-1] == 5
