@@ -632,6 +632,115 @@ CASCADE_API int32_t cascade_pages_compact(const cascade_paged_cache *cache, int3
 CASCADE_API int32_t cascade_pages_copy(const cascade_paged_cache *cache, int32_t n, const int32_t *src_dev,
                            const int32_t *dst_dev, void *stream);
 
+/* ------------------------------------------------------------------ a token's step around its attention
+ * What stands between and behind the projections of a generated token (and of a prompt): the
+ * residual's addition with the norm, products of few rows with 4-bit weights, and the choice of
+ * the next token.  Every call takes rows in the order they lie in, without a plan.
+ *
+ * Values in 8 bits stand for q * scale, one fp32 scale for a group of neighbouring columns of a
+ * row (or for the whole row).                                                       */
+#define CASCADE_Q8_NONE 0
+#define CASCADE_Q8_INT8 1          /* -127 .. 127                                      */
+#define CASCADE_Q8_E4M3 2          /* 8-bit floats of 4 exponent and 3 mantissa bits, largest 448 */
+
+/* The residual's addition and the norm behind it:
+ *   s = x + delta;  sum = s;  y = norm(s) * gain (+ bias);  q * q_scale = y in 8 bits
+ * delta NULL: s = x.  Any of sum, y and q (with q_scale) may be NULL, one is wanted.  s, its
+ * statistics and y are fp32 and each output is rounded once: y does not see the rounding of sum.
+ * Of a group with largest magnitude A, q_scale = max(A / 127, 2^-100) and q = y / q_scale rounded
+ * to nearest even (E4M3: 448 in the place of 127); a group that holds an infinity or NaN has
+ * q_scale = NaN and q = 0.
+ * sum and y may each be x or delta (with the same stride); outputs must not overlap otherwise.  */
+typedef struct cascade_add_norm_desc {
+    int32_t dtype;        /* of x, delta, gain, bias, sum and y                       */
+    int32_t rows, d_model;          /* d_model: at most 32768                          */
+    int32_t norm_kind;    /* CASCADE_NORM_LAYERNORM | CASCADE_NORM_RMSNORM            */
+    float   eps;
+    int32_t q_format;     /* CASCADE_Q8_*                                             */
+    int32_t q_group;      /* columns of a scale: 32, 64, 128 or 256, dividing d_model; 0: the row */
+    int64_t x_stride, delta_stride, sum_stride, y_stride, q_stride;   /* of rows, in elements; 0: dense */
+} cascade_add_norm_desc;
+
+/* x, delta, sum, y [rows, D], gain, bias [D], q [rows, D] bytes, q_scale [rows, D / q_group] (dense).
+ * Errors: EINVAL, ESHAPE (strides below a row, a shared tensor with two strides, d_model %
+ * q_group), EUNSUPPORTED (dtype, d_model, q_group), EHIP.                           */
+CASCADE_API int32_t cascade_add_norm(const cascade_add_norm_desc *desc, const void *x, const void *delta, const void *gain,
+                         const void *bias, void *sum, void *y, void *q, float *q_scale, void *stream);
+
+/* Weights in 4 bits: W[n][k] = scale[n][k / group] * (code[n][k] - zero[n][k / group]), codes and
+ * zeros 0 .. 15.  cascade_w4_pack lays them out once in the order in which the product's matrix instructions take
+ * them: `packed` (256-byte aligned, cascade_w4_bytes) is opaque, belongs to the caller, and holds
+ * scales and zeros too.                                                             */
+typedef struct cascade_w4_weights {
+    int32_t dtype;        /* of the scales, and of the product's bias, residual and Y  */
+    int32_t n_out, k;     /* k: a multiple of group, at most 2^20                      */
+    int32_t group;        /* reduction elements of a scale: 32, 64 or 128              */
+    int32_t zero_points;  /* 0: zero is 8 everywhere                                   */
+    int32_t reserved;     /* 0                                                         */
+    void *packed;
+} cascade_w4_weights;
+
+CASCADE_API size_t cascade_w4_bytes(const cascade_w4_weights *weights);
+
+/* codes [n_out, k] bytes, scales [n_out, k / group] in dtype, zeros [n_out, k / group] bytes (NULL
+ * exactly where zero_points is 0); of codes and zeros the low 4 bits count.
+ * Errors: EINVAL, ESHAPE (k % group), EUNSUPPORTED (dtype, group, k, alignment), EHIP. */
+CASCADE_API int32_t cascade_w4_pack(const cascade_w4_weights *weights, const void *codes, const void *scales, const void *zeros,
+                        void *stream);
+
+/* Y = epilogue(X W^T), the few-row counterpart of cascade_shard_gemm: every weight is read once for
+ * up to 64 rows (more rows: once for every 64 of them; prompts are better served by weights in bf16).
+ * X [rows, k] in the weights' dtype, or in 8 bits with x_scale [rows, k / x_group] (dense).  W_up:
+ * EPI_SWIGLU only, of the same sizes, dtype, group and zero_points.  Codes, zeros and 8-bit X enter
+ * the products exactly, sums are fp32 (of INT8 X: whole numbers within a group, then fp32).
+ * An infinity or NaN in a row of X reaches that row's outputs as in the formula, others' not.
+ * X and its stride: multiples of 16 bytes.  Y may be residual (with the same stride) and must not
+ * overlap X.  Calls that may overlap in time need a workspace each (16-byte aligned; contents need
+ * not be kept between calls).  A call with the same arguments gives the same bits each time; those of a row may depend on the
+ * number of rows.
+ * Errors: EINVAL, ESHAPE (strides, W_up), EUNSUPPORTED (dtype, group, x_format, alignment, an
+ * epilogue other than these, BIAS with SWIGLU), EWORKSPACE, EHIP.                   */
+typedef struct cascade_w4_gemm_desc {
+    int32_t rows;
+    int32_t x_format;     /* CASCADE_Q8_*; NONE: X in the weights' dtype              */
+    int32_t x_group;      /* 8-bit X: columns of a scale: 32, 64, 128 or 256, dividing k; 0: the row */
+    int32_t epilogue;     /* CASCADE_EPI_BIAS | GELU_ERF | GELU_TANH | SWIGLU | RESIDUAL */
+    int64_t x_stride, residual_stride, y_stride;    /* of rows, in elements; 0: dense  */
+} cascade_w4_gemm_desc;
+
+CASCADE_API size_t cascade_w4_gemm_workspace_bytes(const cascade_w4_weights *weights, const cascade_w4_gemm_desc *desc);
+CASCADE_API int32_t cascade_w4_gemm(const cascade_w4_weights *weights, const cascade_w4_weights *weights_up,
+                        const cascade_w4_gemm_desc *desc, const void *X, const float *x_scale, const void *bias,
+                        const void *residual, void *Y, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Next tokens from logits by given random numbers, each row with its own settings (device arrays of
+ * `rows` values, so that a captured step serves changing requests; NULL: off, temperature 1).
+ * Order of a row: logits descending, equal ones by index; NaN counts as -inf.
+ *   w_i = exp((l_i - l_max) / temperature); 1 where l_i = l_max, 0 where they are infinitely far apart
+ *   top_k   keeps the first top_k in order                     (<= 0: all)
+ *   top_p   of these, the shortest prefix with at least top_p of their mass (NaN or >= 1: all)
+ *   min_p   of these, those with w_i >= min_p                  (NaN or <= 0: all)
+ * and the first in order is always kept.  token = the first in order at which the running sum of
+ * the kept w exceeds uniform * W, W their sum (NaN or below 0: the first; too large: the last with w above 0).
+ * prob (NULL: not wanted) = w_token / W.  temperature <= 0 or NaN: the first in order, prob 1, the
+ * choice of cascade_greedy_token.  A row of -inf and NaN alone: token 0, prob 0.
+ * Weights and sums are exact to about 2^-30: a uniform nearer than that to a border between two tokens may fall to either.
+ * The same arguments give the same tokens each time, whatever the other rows.       */
+typedef struct cascade_sample_desc {
+    int32_t dtype;        /* of the logits                                            */
+    int32_t rows, vocab;  /* vocab: at most 2^20                                       */
+    int32_t reserved;     /* 0                                                         */
+    int64_t stride;       /* of rows, in elements; 0: dense                            */
+} cascade_sample_desc;
+
+/* uniform [rows] in [0, 1); token [rows] int32.  workspace: 16-byte aligned; calls that may overlap in time need one each, its contents
+ * need not be kept between calls.
+ * Errors: EINVAL, ESHAPE (stride), EUNSUPPORTED (dtype, vocab), EWORKSPACE, EHIP.   */
+CASCADE_API size_t cascade_sample_workspace_bytes(const cascade_sample_desc *desc);
+CASCADE_API int32_t cascade_sample(const cascade_sample_desc *desc, const void *logits, const float *temperature, const int32_t *top_k,
+                       const float *top_p, const float *min_p, const float *uniform, int32_t *token, float *prob,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
 /* ------------------------------------------------------------------ measured ceiling
  * Not a step of the method: the rate (TFLOP/s) this device sustains on back-to-back
  * bf16 16x16x32 MFMAs with random operands, for the roofline figures quoted next

@@ -25,6 +25,7 @@ ATTN_FUSED, ATTN_MATERIALISED = 0, 1
 NORM_PRE, NORM_POST = 0, 1
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 ROPE_UNSCALED, ROPE_LINEAR, ROPE_RAMP = 0, 1, 2
+Q8_NONE, Q8_INT8, Q8_E4M3 = 0, 1, 2
 EPI_BIAS, EPI_GELU_ERF, EPI_GELU_TANH, EPI_SWIGLU, EPI_ROPE, EPI_RESIDUAL = 1, 2, 4, 8, 16, 32
 
 EXPORTS = ["cascade_plan_create", "cascade_plan_create_rs", "cascade_plan_maps", "cascade_plan_maps_host",
@@ -37,7 +38,8 @@ EXPORTS = ["cascade_plan_create", "cascade_plan_create_rs", "cascade_plan_maps",
            "cascade_lm_head_workspace_bytes", "cascade_lm_head", "cascade_greedy_token", "cascade_layer_kv_to_cache", "cascade_norm",
            "cascade_decode_partial_attn", "cascade_mfma_ceiling", "cascade_rope", "cascade_paged_extend", "cascade_paged_append",
            "cascade_paged_attn_workspace_bytes", "cascade_paged_attn", "cascade_pages_free", "cascade_pages_workspace_bytes",
-           "cascade_pages_fork", "cascade_pages_compact", "cascade_pages_copy"]
+           "cascade_pages_fork", "cascade_pages_compact", "cascade_pages_copy", "cascade_add_norm", "cascade_w4_bytes", "cascade_w4_pack",
+           "cascade_w4_gemm_workspace_bytes", "cascade_w4_gemm", "cascade_sample_workspace_bytes", "cascade_sample"]
 N_STAGE_EVENTS = 10
 STAGE_NAMES = ["gather_norm1", "qkv_gemm", "rope", "attention", "lse_merge", "o_proj", "norm2", "ffn_up", "ffn_down"]
 
@@ -93,6 +95,29 @@ class PagedCache(C.Structure):
 class PagedAttnDesc(C.Structure):
     _fields_ = [("rows", C.c_int32), ("n_heads", C.c_int32), ("scale", C.c_float), ("o_dtype", C.c_int32),
                 ("q_stride", C.c_int64), ("o_stride", C.c_int64)]
+
+
+
+class AddNormDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("rows", C.c_int32), ("d_model", C.c_int32), ("norm_kind", C.c_int32), ("eps", C.c_float),
+                ("q_format", C.c_int32), ("q_group", C.c_int32), ("x_stride", C.c_int64), ("delta_stride", C.c_int64),
+                ("sum_stride", C.c_int64), ("y_stride", C.c_int64), ("q_stride", C.c_int64)]
+
+
+class W4Weights(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_out", C.c_int32), ("k", C.c_int32), ("group", C.c_int32), ("zero_points", C.c_int32),
+                ("reserved", C.c_int32), ("packed", C.c_void_p)]
+    tensors = (None,)                                      # of make_w4_weights
+
+
+class W4GemmDesc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("x_format", C.c_int32), ("x_group", C.c_int32), ("epilogue", C.c_int32),
+                ("x_stride", C.c_int64), ("residual_stride", C.c_int64), ("y_stride", C.c_int64)]
+
+
+class SampleDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("rows", C.c_int32), ("vocab", C.c_int32), ("reserved", C.c_int32), ("stride", C.c_int64)]
+
 
 _WEIGHT_FIELDS = ["wq", "wk", "wv", "wo", "w_gate", "w_up", "w_down", "bq", "bk", "bv", "bo", "b_up", "b_down",
                   "norm1_g", "norm1_b", "norm2_g", "norm2_b"]
@@ -192,10 +217,18 @@ def load_library():
             "cascade_pages_free": [PC, I32, VP, VP],
             "cascade_pages_fork": [PC, I32, VP, VP, VP, VP, C.c_size_t, VP],
             "cascade_pages_compact": [PC, VP, VP, C.c_size_t, VP],
-            "cascade_pages_copy": [PC, I32, VP, VP, VP]}.items():
+            "cascade_pages_copy": [PC, I32, VP, VP, VP],
+            "cascade_add_norm": [P(AddNormDesc), VP, VP, VP, VP, VP, VP, VP, VP, VP],
+            "cascade_w4_pack": [P(W4Weights), VP, VP, VP, VP],
+            "cascade_w4_gemm": [P(W4Weights), P(W4Weights), P(W4GemmDesc), VP, VP, VP, VP, VP, VP, C.c_size_t, VP],
+            "cascade_sample": [P(SampleDesc), VP, VP, VP, VP, VP, VP, VP, VP, VP, C.c_size_t, VP]}.items():
         getattr(lib, name).argtypes, getattr(lib, name).restype = args, I32
     lib.cascade_paged_attn_workspace_bytes.argtypes, lib.cascade_paged_attn_workspace_bytes.restype = [PC, P(PagedAttnDesc)], C.c_size_t
     lib.cascade_pages_workspace_bytes.argtypes, lib.cascade_pages_workspace_bytes.restype = [PC], C.c_size_t
+    lib.cascade_w4_bytes.argtypes, lib.cascade_w4_bytes.restype = [P(W4Weights)], C.c_size_t
+    lib.cascade_w4_gemm_workspace_bytes.argtypes = [P(W4Weights), P(W4GemmDesc)]
+    lib.cascade_w4_gemm_workspace_bytes.restype = C.c_size_t
+    lib.cascade_sample_workspace_bytes.argtypes, lib.cascade_sample_workspace_bytes.restype = [P(SampleDesc)], C.c_size_t
     _lib = lib
     return lib
 
@@ -763,6 +796,129 @@ def cascade_pages_copy(cache, src, dst, stream=None):
     _checked("cascade_pages_copy", torch.int32, src, dst)
     _counted("cascade_pages_copy", (src.numel() == dst.numel(), "src, dst [n]"))
     _check(lib.cascade_pages_copy(C.byref(cache), src.numel(), _at(src), _at(dst), _on(stream, cache.tensors[0], src, dst)), "cascade_pages_copy")
+
+
+# ------------------------------------------------------------------ a token's step around its attention
+def _dense_rows(t, where, what):
+    """Row stride of a [rows, columns] tensor on the GPU whose rows do not overlap (None: 0)."""
+    if t is None:
+        return 0
+    if t.dim() == 2:
+        (rows, cols), (sr, sc) = t.shape, t.stride()
+        if t.is_cuda and (sc == 1 or cols == 1) and (rows < 2 or sr >= cols):
+            return sr if rows > 1 else cols
+    raise CascadeError(ESHAPE, f"{where}: {what} [rows, columns], columns dense, rows that do not overlap, on the GPU")
+
+
+def _q8_format(t):
+    import torch
+    return {torch.int8: Q8_INT8, torch.float8_e4m3fn: Q8_E4M3}.get(t.dtype, Q8_NONE)
+
+
+def cascade_add_norm(x, gain, norm_kind, eps, delta=None, bias=None, sum=None, y=None, q=None, q_scale=None, stream=None):
+    """x, delta, sum, y [rows, D] of one type, gain, bias [D]; q [rows, D] int8 or float8_e4m3fn with q_scale fp32 [rows] or
+    [rows, D / group] (group 32, 64, 128 or 256).  One of sum, y, q is wanted; sum and y may be x or delta."""
+    import torch
+    lib = load_library()
+    where = "cascade_add_norm"
+    _checked(where, x.dtype, gain, bias)
+    _checked(where, torch.float32, q_scale)
+    strides = [_dense_rows(t, where, n) for t, n in ((x, "x"), (delta, "delta"), (sum, "sum"), (y, "y"), (q, "q"))]
+    rows, D = x.shape
+    _counted(where, (all(t is None or (t.shape == x.shape and t.dtype == x.dtype) for t in (delta, sum, y)), "delta, sum and y like x"),
+             (gain.numel() == D and (bias is None or bias.numel() == D), "gain, bias [D]"), ((q is None) == (q_scale is None), "q with q_scale"))
+    fmt = group = 0
+    if q is not None:
+        fmt, groups = _q8_format(q), q_scale.numel() // max(rows, 1)
+        _counted(where, (fmt != Q8_NONE and q.shape == x.shape, "q int8 or float8_e4m3fn, like x"),
+                 (rows == 0 or (q_scale.numel() == rows * groups and groups > 0 and D % groups == 0), "q_scale [rows, D / group]"))
+        group = D // groups if groups > 1 else 0
+    desc = AddNormDesc(_dtype_code(x), rows, D, norm_kind, eps, fmt, group, *strides)
+    st = lib.cascade_add_norm(C.byref(desc), _at(x), _at(delta), _at(gain), _at(bias), _at(sum), _at(y), _at(q), _at(q_scale),
+                              _on(stream, x, delta, gain, bias, sum, y, q, q_scale))
+    _check(st, where)
+
+
+def make_w4_weights(codes, scales, zeros=None):
+    """W4Weights of codes uint8 [n_out, k] (0 .. 15), scales [n_out, k / group] (bf16 or fp32: the product's type) and zeros uint8
+    like scales (None: 8), packed on the current stream into a tensor that the handle keeps alive."""
+    import torch
+    lib = load_library()
+    where = "make_w4_weights"
+    _checked(where, torch.uint8, codes, zeros)
+    _checked(where, scales.dtype, scales)
+    _counted(where, (codes.dim() == 2 and scales.dim() == 2 and scales.shape[0] == codes.shape[0], "codes [n_out, k], scales [n_out, k / group]"),
+             (zeros is None or zeros.shape == scales.shape, "zeros like scales"),
+             (scales.numel() > 0 and codes.shape[1] % scales.shape[1] == 0, "whole groups"))
+    n, k = codes.shape
+    w = W4Weights(_dtype_code(scales), n, k, k // scales.shape[1], 0 if zeros is None else 1, 0, None)
+    handle = _on(None, codes, scales, zeros)
+    size = lib.cascade_w4_bytes(C.byref(w))
+    packed = torch.empty(max(size, 256), dtype=torch.uint8, device=codes.device)
+    w.packed = packed.data_ptr()
+    w.tensors = (packed,)
+    _check(lib.cascade_w4_pack(C.byref(w), _at(codes), _at(scales), _at(zeros), handle), where)
+    return w
+
+
+def _w4_gemm_desc(weights, x, x_scale, epilogue, strides):
+    fmt = _q8_format(x)
+    if fmt == Q8_NONE:
+        _counted("cascade_w4_gemm", (_dtype_code(x) == weights.dtype, "x in the weights' type, int8 or float8_e4m3fn"))
+    groups = 1 if x_scale is None else x_scale.numel() // max(x.shape[0], 1)
+    _counted("cascade_w4_gemm", (x.dim() == 2 and x.shape[1] == weights.k, "x [rows, k]"), ((x_scale is None) == (fmt == Q8_NONE), "x_scale with 8-bit x"),
+             (x_scale is None or (x_scale.numel() == x.shape[0] * groups and groups > 0 and weights.k % groups == 0) or x.shape[0] == 0, "x_scale [rows, k / group]"))
+    return W4GemmDesc(x.shape[0], fmt, weights.k // groups if groups > 1 else 0, epilogue, *strides)
+
+
+def cascade_w4_gemm_workspace_bytes(weights, x, weights_up=None):
+    """For x as it will be given; weights_up: with EPI_SWIGLU."""
+    desc = W4GemmDesc(x.shape[0], _q8_format(x), 0, EPI_SWIGLU if weights_up is not None else 0, 0, 0, 0)
+    return load_library().cascade_w4_gemm_workspace_bytes(C.byref(weights), C.byref(desc))
+
+
+def cascade_w4_gemm(weights, x, y, x_scale=None, weights_up=None, bias=None, residual=None, epilogue=0, workspace=None, stream=None):
+    """y, residual [rows, n_out] and bias [n_out] in the weights' type; x [rows, k] likewise, or int8 / float8_e4m3fn with x_scale
+    fp32 [rows] or [rows, k / group]."""
+    import torch
+    lib = load_library()
+    where = "cascade_w4_gemm"
+    strides = [_dense_rows(t, where, n) for t, n in ((x, "x"), (residual, "residual"), (y, "y"))]
+    desc = _w4_gemm_desc(weights, x, x_scale, epilogue, strides)
+    _checked(where, torch.float32, x_scale)
+    _checked(where, y.dtype, bias)
+    _counted(where, (_dtype_code(y) == weights.dtype and y.shape == (x.shape[0], weights.n_out), "y [rows, n_out] in the weights' type"),
+             (residual is None or (residual.shape == y.shape and residual.dtype == y.dtype), "residual like y"),
+             (bias is None or bias.numel() == weights.n_out, "bias [n_out]"))
+    ws, ws_bytes = _room(workspace, where)
+    st = lib.cascade_w4_gemm(C.byref(weights), None if weights_up is None else C.byref(weights_up), C.byref(desc), _at(x), _at(x_scale),
+                             _at(bias), _at(residual), _at(y), ws, ws_bytes,
+                             _on(stream, x, y, x_scale, bias, residual, workspace, weights.tensors[0], weights_up and weights_up.tensors[0]))
+    _check(st, where)
+
+
+def cascade_sample_workspace_bytes(rows, vocab, dtype):
+    """dtype: the logits' (torch)."""
+    import torch
+    desc = SampleDesc(F32 if dtype == torch.float32 else BF16, rows, vocab, 0, 0)
+    return load_library().cascade_sample_workspace_bytes(C.byref(desc))
+
+
+def cascade_sample(logits, uniform, token, temperature=None, top_k=None, top_p=None, min_p=None, prob=None, workspace=None, stream=None):
+    """logits [rows, vocab]; uniform, temperature, top_p, min_p, prob fp32 [rows], top_k, token int32 [rows] (None: off, or not wanted)."""
+    import torch
+    lib = load_library()
+    where = "cascade_sample"
+    stride = _dense_rows(logits, where, "logits")
+    _checked(where, torch.float32, uniform, temperature, top_p, min_p, prob)
+    _checked(where, torch.int32, token, top_k)
+    rows, vocab = logits.shape
+    _counted(where, (all(t is None or t.numel() == rows for t in (uniform, token, temperature, top_k, top_p, min_p, prob)), "one value a row"))
+    desc = SampleDesc(_dtype_code(logits), rows, vocab, 0, stride)
+    ws, ws_bytes = _room(workspace, where)
+    st = lib.cascade_sample(C.byref(desc), _at(logits), _at(temperature), _at(top_k), _at(top_p), _at(min_p), _at(uniform), _at(token), _at(prob),
+                            ws, ws_bytes, _on(stream, logits, uniform, token, temperature, top_k, top_p, min_p, prob, workspace))
+    _check(st, where)
 
 
 def cascade_mfma_ceiling(lds_operands, iters=200000, stream=None):
