@@ -1,16 +1,17 @@
 // Products of few rows with 4-bit weights (cascade_w4_gemm), and the layout of the weights (cascade_w4_pack).
 //
 // What bounds it: every weight is used for a handful of rows, so a launch is as long as streaming the codes from HBM, half a byte
-// each.  A workgroup owns 16 or 32 output columns, its 8 wavefronts split the reduction and read the codes straight into matrix
-// operands, a ring of pieces ahead of their use; the partial sums meet in LDS in a fixed order.
+// each.  The 8 wavefronts of a workgroup are column groups by parts of the reduction; each reads the codes of its columns straight
+// into matrix operands, a ring of pieces ahead of their use.  X, which all of them need, comes through LDS in the
+// order of the operands: whole where it fits, in two halves in turn where not.
 //
 // Packed layout.  Codes: blocks of 16 columns by 128 reduction elements, 1 KB each, blocks of a column side by side along the
 // reduction.  In a block, lane (column l, quarter g) of a wavefront finds its 16 bytes at (16 g + l) * 16: word s holds elements
 // 32 s + 8 g .. + 7, which is the operand of one 16x16x32 product, and in a word nibble p < 4 holds element 2p, nibble p + 4
 // element 2p + 1.  So two nibbles 16 bits apart become a pair of bf16 numbers by a shift, a mask and an or: 0x4180 | code << 3 is
-// 16 + code.  A second product with -(16 + zero) in every element takes that back, exactly but for the fp32 sums.  INT8 rows
-// take codes as bytes (three operations for 8) and -zero, all in whole numbers.  Behind the codes: scales and zeros, [column
-// blocks][groups][16].
+// 16 + code.  What that adds, and the zero points, come off once per group: scale * (sum x (16 + code) - (16 + zero) * sum x), with
+// the sums of X formed where it enters LDS.  INT8 rows take codes as bytes (three operations for 8), all in whole numbers
+// up to the scales.  Behind the codes: scales and zeros, [column blocks][groups][16].
 #include <algorithm>
 #include <type_traits>
 #include "common.h"
@@ -33,70 +34,72 @@ struct W4Params {
     const float *x_scale;
     const void *bias, *residual;
     void *Y;
+    float *planes;                                         // [slices][matrices][M][N] sums, where the reduction is cut
     int64_t ldx, ldres, ldy;                               // elements
     int32_t M, N, K;
     int32_t blocks, groups;                                // of the reduction
     int32_t fold;                                          // 32-element steps that share all scales: 1, 2 or 4
     int32_t group_shift, x_group_shift, x_groups;          // log2 of the elements of a scale (x_group_shift 31: the row)
     int32_t has_zeros, flags;
+    int32_t cols_log2;                                     // column groups of a workgroup; 8 >> cols_log2 parts of the reduction
+    int32_t slices, slice_blocks;                          // parts of the reduction over workgroups
+    int32_t chunk, chunks_held;                            // blocks of X that enter LDS at once; how many chunks LDS has room for
 };
 
-// fp32 columns of a row as three bf16 numbers each, which add up to it exactly (8 bits of 24 each)
-__device__ __forceinline__ void limbs(const f32x4 &a, const f32x4 &b, bf16x8 (&out)[3]) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        float v = e < 4 ? a[e] : b[e - 4];
-#pragma unroll
-        for (int i = 0; i < 3; ++i) {
-            out[i][e] = (bf16_t)v;
-            v -= (float)out[i][e];
-        }
-    }
-}
-
-template <int XT> struct XPiece;                           // what a lane holds of a row's 128 columns, as it came
-template <> struct XPiece<X_BF16> { u32x4 v[4]; };
-template <> struct XPiece<X_F32> { u32x4 v[8]; };
-template <> struct XPiece<X_E4M3> { u32x2 v[4]; };
-template <> struct XPiece<X_INT8> { u32x2 v[4]; };
 template <int XT> constexpr int x_bytes() { return XT == X_BF16 ? 2 : XT == X_F32 ? 4 : 1; }
+template <int XT> constexpr int unit_bytes() { return XT == X_F32 ? 48 : XT == X_INT8 ? 8 : 16; }   // 8 columns of a row in LDS
+constexpr int MAX_UNITS = 4;                               // of a thread and chunk: chunk * rows * 16 / 512
 
+// 8 columns of X as they came, and in LDS: bf16 numbers (three sets of them for fp32, which add up to it exactly), or bytes in the
+// order of the codes' bytes.  Returns their sum.
+template <int XT> struct XRaw { u32x4 v; };
+template <> struct XRaw<X_F32> { u32x4 v, w; };
+template <> struct XRaw<X_E4M3> { u32x2 v; };
+template <> struct XRaw<X_INT8> { u32x2 v; };
 template <int XT>
-__device__ __forceinline__ void request_x(XPiece<XT> &x, __amdgpu_buffer_rsrc_t r, uint32_t off, int left) {
-    // columns 32 s + 8 g .. + 7 of the piece; `left`: columns from the lane's first one to the row's end
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-        const uint32_t o = 32 * s < left ? off + 32 * s * x_bytes<XT>() : OUT_OF_RANGE;
-        if constexpr (XT == X_BF16) x.v[s] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, o, 0, 0));
-        else if constexpr (XT == X_F32) {
-            x.v[2 * s] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, o, 0, 0));
-            x.v[2 * s + 1] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, o, 16, 0));
-        } else x.v[s] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, o, 0, 0));
-    }
+__device__ __forceinline__ XRaw<XT> load_x(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+    XRaw<XT> x;
+    if constexpr (XT == X_E4M3 || XT == X_INT8) x.v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0));
+    else x.v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+    if constexpr (XT == X_F32) x.w = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 16, 0));
+    return x;
 }
-
-// The operand of step s: bf16 numbers (three sets of them for fp32), or bytes in the order of the codes' bytes
-template <int XT> struct XOperand { bf16x8 v[XT == X_F32 ? 3 : 1]; };
-template <> struct XOperand<X_INT8> { int64_t v; };
 template <int XT>
-__device__ __forceinline__ XOperand<XT> x_operand(const XPiece<XT> &x, int s) {
-    XOperand<XT> o;
-    if constexpr (XT == X_BF16) o.v[0] = __builtin_bit_cast(bf16x8, x.v[s]);
-    else if constexpr (XT == X_F32) limbs(__builtin_bit_cast(f32x4, x.v[2 * s]), __builtin_bit_cast(f32x4, x.v[2 * s + 1]), o.v);
-    else if constexpr (XT == X_E4M3) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(x.v[s][h], false), b = __builtin_amdgcn_cvt_pk_f32_fp8(x.v[s][h], true);
-            o.v[0][4 * h] = (bf16_t)a[0];
-            o.v[0][4 * h + 1] = (bf16_t)a[1];
-            o.v[0][4 * h + 2] = (bf16_t)b[0];
-            o.v[0][4 * h + 3] = (bf16_t)b[1];
-        }
+__device__ __forceinline__ float store_x(const XRaw<XT> &x, char *to) {
+    if constexpr (XT == X_INT8) {
+        *(u32x2 *)to = u32x2{__builtin_amdgcn_perm(x.v[1], x.v[0], 0x05010400u), __builtin_amdgcn_perm(x.v[1], x.v[0], 0x07030602u)};
+        return (float)__builtin_amdgcn_sdot4(x.v[0], 0x01010101, __builtin_amdgcn_sdot4(x.v[1], 0x01010101, 0, false), false);
     } else {
-        const u32x2 b = {__builtin_amdgcn_perm(x.v[s][1], x.v[s][0], 0x05010400u), __builtin_amdgcn_perm(x.v[s][1], x.v[s][0], 0x07030602u)};
-        o.v = __builtin_bit_cast(int64_t, b);
+        float f[8];
+        if constexpr (XT == X_F32) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = __builtin_bit_cast(float, e < 4 ? x.v[e] : x.w[e - 4]);
+        } else if constexpr (XT == X_E4M3) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(x.v[h], false), b = __builtin_amdgcn_cvt_pk_f32_fp8(x.v[h], true);
+                f[4 * h] = a[0]; f[4 * h + 1] = a[1]; f[4 * h + 2] = b[0]; f[4 * h + 3] = b[1];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = __builtin_bit_cast(float, e & 1 ? x.v[e >> 1] & 0xffff0000u : x.v[e >> 1] << 16);
+        }
+        const float sum = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+        if constexpr (XT == X_BF16) *(u32x4 *)to = x.v;
+        else {
+#pragma unroll
+            for (int i = 0; i < (XT == X_F32 ? 3 : 1); ++i) {
+                bf16x8 v;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    v[e] = (bf16_t)f[e];
+                    f[e] -= (float)v[e];
+                }
+                *(bf16x8 *)(to + 16 * i) = v;
+            }
+        }
+        return sum;
     }
-    return o;
 }
 
 // 8 codes of a word as 16 + code
@@ -111,22 +114,6 @@ __device__ __forceinline__ int64_t codes_int8(uint32_t w) {
 }
 
 template <int XT> using Sum = typename std::conditional<XT == X_INT8, i32x4, f32x4>::type;
-template <int XT>
-__device__ __forceinline__ void step(Sum<XT> &acc, const XOperand<XT> &x, uint32_t w, uint32_t minus_zero) {
-    if constexpr (XT == X_INT8) {
-        const u32x2 z = {minus_zero, minus_zero};
-        acc = __builtin_amdgcn_mfma_i32_16x16x32_i8(x.v, codes_int8(w), acc, 0, 0, 0);
-        acc = __builtin_amdgcn_mfma_i32_16x16x32_i8(x.v, __builtin_bit_cast(int64_t, z), acc, 0, 0, 0);
-    } else {
-        const u32x4 z = {minus_zero, minus_zero, minus_zero, minus_zero};
-        const bf16x8 c = codes_bf16(w);
-#pragma unroll
-        for (int i = 0; i < (XT == X_F32 ? 3 : 1); ++i) {
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.v[i], c, acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.v[i], __builtin_bit_cast(bf16x8, z), acc, 0, 0, 0);
-        }
-    }
-}
 
 // One output from the formula, term by term.  The products above give NaN where a row holds an infinity (16 + code and
 // 16 + zero meet it with opposite signs), and fp32 values next to the largest leave the range of the first of their parts.
@@ -156,194 +143,356 @@ __device__ __forceinline__ float plain_output(const W4Params &p, int which, int 
     return sum;
 }
 
-// TM: 16-row blocks.  TN: 16-column blocks (SWIGLU: gate and up of the same columns).  D: pieces in flight per wavefront.
+// Behind the sums: scales of whole rows, the formula where a sum is no number, bias, activation, residual
+template <int XT, bool F32, bool SWIGLU>
+__device__ __forceinline__ void finish(const W4Params &p, float (&v)[2], int row, int n) {
+    typedef typename std::conditional<F32, float, bf16_t>::type T;
+#pragma unroll
+    for (int u = 0; u < (SWIGLU ? 2 : 1); ++u) {
+        if ((XT == X_E4M3 || XT == X_INT8) && p.x_groups == 1) v[u] *= p.x_scale[row];
+        if (!(fabsf(v[u]) < __builtin_inff())) v[u] = plain_output<XT, F32>(p, u, row, n);
+    }
+    float y = v[0];
+    if (p.flags & CASCADE_EPI_BIAS) y += (float)((const T *)p.bias)[n];
+    if (SWIGLU) y = silu_f(y) * v[1];
+    else y = F32 ? apply_act(y, p.flags) : apply_act_bf16(y, p.flags);
+    if (p.flags & CASCADE_EPI_RESIDUAL) y += (float)((const T *)p.residual)[row * p.ldres + n];
+    ((T *)p.Y)[row * p.ldy + n] = (T)y;
+}
+
+// TM: 16-row blocks.  TN: 16-column blocks of a wavefront (SWIGLU: gate and up of the same columns).
+// WHOLE: the slice's X fits into LDS and enters it once; else it comes in chunks of two pieces a wavefront, into halves in turn.
 // F32: scales, bias, residual and Y in fp32, else bf16.
-template <int XT, bool F32, int TM, int TN, int D, bool SWIGLU>
-__global__ __launch_bounds__(NW * 64) void w4_kernel(W4Params p) {
+template <int XT, bool F32, int TM, int TN, bool SWIGLU, bool WHOLE>
+__global__ __launch_bounds__(NW * 64, TM == 1 && WHOLE ? 4 : 2) void w4_kernel(W4Params p) {
     static_assert(!SWIGLU || TN == 2, "gate and up");
     typedef typename std::conditional<F32, float, bf16_t>::type T;
     constexpr bool X8 = XT == X_E4M3 || XT == X_INT8;
-    constexpr int TNO = SWIGLU ? 1 : TN, OUT = TNO * 256, PER = (OUT + NW * 64 - 1) / (NW * 64);
-    __shared__ __attribute__((aligned(16))) float part[NW][TN][256];
+    constexpr int TNO = SWIGLU ? 1 : TN, D = 4, UB = unit_bytes<XT>(), MATS = SWIGLU ? 2 : 1;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
 
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int row0 = blockIdx.y * (TM * 16), rows = min(p.M - row0, TM * 16);
-    const int block0 = blockIdx.x * TNO, n_blocks = min((p.N + 15) / 16 - block0, TNO);
+    const int cols = 1 << p.cols_log2, parts = NW >> p.cols_log2, cg = wave & (cols - 1), part = wave >> p.cols_log2;
+    const int row0 = blockIdx.z * (TM * 16), rows = min(p.M - row0, TM * 16);
+    const int tile0 = blockIdx.x * cols * TNO, block0 = tile0 + cg * TNO;        // 16-column blocks: of the workgroup, of the wavefront
+    const int all_blocks = (p.N + 15) / 16, n_blocks = max(0, min(all_blocks - block0, TNO));
+    const int first = blockIdx.y * p.slice_blocks, n_pieces = min(p.blocks - first, p.slice_blocks);
 
-    __amdgpu_buffer_rsrc_t rw[SWIGLU ? 2 : 1], rs[SWIGLU ? 2 : 1], rz[SWIGLU ? 2 : 1];
+    // LDS: chunks of X, the sums and scales of its 32-column steps
+    const int row_units = rows | 1;                        // odd: neighbouring units of a row lie in different banks
+    const int chunk_bytes = p.chunk * 16 * row_units * UB, chunk_sums = p.chunk * 4 * TM * 16;
+    float *sums = (float *)(lds + p.chunks_held * chunk_bytes), *xscales = sums + p.chunks_held * chunk_sums;
+
+    __amdgpu_buffer_rsrc_t rw[MATS], rs[MATS], rz[MATS];
 #pragma unroll
-    for (int i = 0; i < (SWIGLU ? 2 : 1); ++i) {
-        const int64_t scales = (int64_t)block0 * p.groups * 16;
-        rw[i] = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p.codes[i]) + (int64_t)block0 * p.blocks * 1024, 0,
-                                                  (uint32_t)(n_blocks * p.blocks) * 1024u, 0x00020000);
-        rs[i] = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p.scales[i]) + scales * sizeof(T), 0,
-                                                  (uint32_t)(n_blocks * p.groups * 16 * sizeof(T)), 0x00020000);
-        rz[i] = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p.zeros[i]) + scales, 0, p.has_zeros ? (uint32_t)(n_blocks * p.groups * 16) : 0u,
-                                                  0x00020000);
+    for (int i = 0; i < MATS; ++i) {
+        const int64_t at = n_blocks ? block0 : 0, entries = at * p.groups * 16;
+        rw[i] = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p.codes[i]) + at * p.blocks * 1024, 0, (uint32_t)(n_blocks * p.blocks) * 1024u, 0x00020000);
+        rs[i] = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p.scales[i]) + entries * sizeof(T), 0, (uint32_t)(n_blocks * p.groups * 16 * sizeof(T)), 0x00020000);
+        rz[i] = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p.zeros[i]) + entries, 0, p.has_zeros ? (uint32_t)(n_blocks * p.groups * 16) : 0u, 0x00020000);
     }
     const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<char *>(p.X) + row0 * p.ldx * x_bytes<XT>(), 0, (uint32_t)(((rows - 1) * p.ldx + p.K) * x_bytes<XT>()), 0x00020000);
     const __amdgpu_buffer_rsrc_t rxs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(X8 ? p.x_scale + (int64_t)row0 * p.x_groups : nullptr), 0,
                                                                          X8 ? (uint32_t)(rows * p.x_groups * 4) : 0u, 0x00020000);
-    uint32_t x_off[TM];
+
+    // Unit u of a chunk: columns 8 sg .. of piece (u >> 4) / rows, row (u >> 4) % rows.  f(k, piece, row) for a thread's units, which
+    // are 32 rows apart.
+    const int sg = tid & 15, units = p.chunk * rows * 16, piece_step = 32 / rows, row_step = 32 % rows;
+    auto each_unit = [&](int u, int most, int &piece, int &row, auto f) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) x_off[i] = 16 * i + l16 < rows ? (uint32_t)((16 * i + l16) * p.ldx + 8 * g) * x_bytes<XT>() : OUT_OF_RANGE;
+        for (int k = 0; k < most; ++k, u += NW * 64) {
+            if (u - tid >= units) break;
+            f(k, piece, row, u < units);
+            piece += piece_step;
+            row += row_step;
+            if (row >= rows) {
+                row -= rows;
+                ++piece;
+            }
+        }
+    };
+    const int piece0 = (tid >> 4) / rows, row_0 = (tid >> 4) % rows;
+    auto request_x = [&](int chunk, int piece, int row, bool is) {
+        const int q = chunk * p.chunk + piece, col = (first + q) * BLOCK + 8 * sg;
+        return load_x<XT>(rx, is && q < n_pieces && col < p.K ? (uint32_t)(row * p.ldx + col) * x_bytes<XT>() : OUT_OF_RANGE);
+    };
+    auto store_unit = [&](int chunk, int held, int piece, int row, bool is, const XRaw<XT> &x) {
+        float sum = 0.f;
+        if (is) sum = store_x<XT>(x, lds + held * chunk_bytes + ((piece * 16 + sg) * row_units + row) * UB);
+        sum += dpp_row_move<0xB1>(sum);
+        sum += dpp_row_move<0x4E>(sum);
+        if (!is || (sg & 3)) return;
+        const int at = held * chunk_sums + (piece * 4 + (sg >> 2)) * (TM * 16) + row;
+        sums[at] = sum;
+        if (X8 && p.x_groups > 1) {
+            const int q = chunk * p.chunk + piece, col = (first + q) * BLOCK + 8 * sg;
+            const uint32_t o = q < n_pieces && col < p.K ? (uint32_t)(row * p.x_groups + (col >> p.x_group_shift)) * 4u : OUT_OF_RANGE;
+            xscales[at] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rxs, o, 0, 0));
+        }
+    };
 
     struct Piece {
         u32x4 w[TN];
         uint32_t scale[TN], zero[TN];                      // of the fold that this lane's quarter stands for
-        XPiece<XT> x[TM];
-        f32x4 xs[X8 ? TM : 1];
     } ring[D];
-    const int folds_shift = 2 - __builtin_ctz(p.fold), folds = 1 << folds_shift;      // folds of a piece
-    // Workgroups start 256 bytes of X apart and wrap around, as those of the bf16 kernel for few rows do (L2 channels)
-    const int rot = (int)((blockIdx.x >> 3) % (uint32_t)p.blocks);
-    auto request = [&](Piece &c, int piece) {
-        const int at = piece + rot - (piece + rot >= p.blocks ? p.blocks : 0);
-        const bool past = piece >= p.blocks;
-        const int first = (at << 2) + (g & (folds - 1)) * p.fold;                // 32-element step at which the lane's fold begins
-        const int group = (first << 5) >> p.group_shift;
+    const int fold_log2 = __builtin_ctz(p.fold), folds = 4 >> fold_log2;         // folds of a piece
+    const int my_pieces = (n_pieces - part + parts - 1) / parts;
+    auto request = [&](Piece &c, int j) {                  // the wavefront's j-th piece
+        const int at = first + part + parts * j;
+        const bool past = j >= my_pieces;
+        const int group = ((at << 2) + (g & (folds - 1)) * p.fold) * 32 >> p.group_shift;
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            const int i = SWIGLU ? j : 0, b = SWIGLU ? 0 : j;
-            const uint32_t o = past ? OUT_OF_RANGE : (uint32_t)(b * p.blocks + at) * 1024u + lane * 16;
-            c.w[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw[i], o, 0, 0));
+        for (int t = 0; t < TN; ++t) {
+            const int i = SWIGLU ? t : 0, b = SWIGLU ? 0 : t;
+            c.w[t] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw[i], past ? OUT_OF_RANGE : (uint32_t)(b * p.blocks + at) * 1024u + lane * 16, 0, 0));
             const uint32_t so = past || group >= p.groups ? OUT_OF_RANGE : (uint32_t)((b * p.groups + group) * 16 + l16);
-            if constexpr (F32) c.scale[j] = __builtin_amdgcn_raw_buffer_load_b32(rs[i], so * 4 | (so & OUT_OF_RANGE), 0, 0);
-            else c.scale[j] = __builtin_amdgcn_raw_buffer_load_b16(rs[i], so * 2 | (so & OUT_OF_RANGE), 0, 0);
-            c.zero[j] = __builtin_amdgcn_raw_buffer_load_b8(rz[i], so, 0, 0);
+            if constexpr (F32) c.scale[t] = __builtin_amdgcn_raw_buffer_load_b32(rs[i], so * 4 | (so & OUT_OF_RANGE), 0, 0);
+            else c.scale[t] = __builtin_amdgcn_raw_buffer_load_b16(rs[i], so * 2 | (so & OUT_OF_RANGE), 0, 0);
+            c.zero[t] = __builtin_amdgcn_raw_buffer_load_b8(rz[i], so, 0, 0);
         }
-        const int left = past ? 0 : p.K - at * BLOCK - 8 * g;
-#pragma unroll
-        for (int i = 0; i < TM; ++i) request_x<XT>(c.x[i], rx, x_off[i] + (past ? 0u : (uint32_t)at * BLOCK * x_bytes<XT>()), x_off[i] & OUT_OF_RANGE ? 0 : left);
     };
 
-    f32x4 total[TM][TN];                                   // row 16 i + 4 g + r, column 16 j + l16
+    f32x4 total[TM][TN];                                   // row 16 i + 4 g + r, column 16 t + l16
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; ++j) total[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < TN; ++t) total[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    auto use = [&](const Piece &c, int piece) {
-        const int at = piece + rot - (piece + rot >= p.blocks ? p.blocks : 0);
+    int x_row[TM];                                         // rows behind the last one read it again, and are not stored
+#pragma unroll
+    for (int i = 0; i < TM; ++i) x_row[i] = min(16 * i + l16, rows - 1) * UB;
+    auto use = [&](const Piece &c, int held, int piece) {  // piece of the chunk
+        const char *x = lds + held * chunk_bytes + piece * 16 * row_units * UB;
+        const int at_sums = held * chunk_sums + piece * 4 * (TM * 16) + 4 * g;
         Sum<XT> acc[TM][TN];
-        uint32_t minus_zero[TN];
-        float scale[TN];
+        f32x4 xsum[TM];
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            if ((s & (p.fold - 1)) == 0) {                 // a fold begins
-                const int from = folds == 1 ? lane : (s >> __builtin_ctz(p.fold)) * 16 + l16;
+            const bool begins = (s & (p.fold - 1)) == 0, ends = ((s + 1) & (p.fold - 1)) == 0;
+            if (begins) {
 #pragma unroll
-                for (int j = 0; j < TN; ++j) {
-                    uint32_t sc = c.scale[j], z = c.zero[j];
+                for (int i = 0; i < TM; ++i) {
+                    xsum[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int t = 0; t < TN; ++t) acc[i][t] = Sum<XT>{0, 0, 0, 0};
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                const char *u = x + (4 * s + g) * row_units * UB + x_row[i];
+                if constexpr (XT == X_INT8) {
+                    const int64_t a = *(const int64_t *)u;
+#pragma unroll
+                    for (int t = 0; t < TN; ++t) acc[i][t] = __builtin_amdgcn_mfma_i32_16x16x32_i8(a, codes_int8(c.w[t][s]), acc[i][t], 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int l = 0; l < (XT == X_F32 ? 3 : 1); ++l) {
+                        const bf16x8 a = *(const bf16x8 *)(u + 16 * l);
+#pragma unroll
+                        for (int t = 0; t < TN; ++t) acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, codes_bf16(c.w[t][s]), acc[i][t], 0, 0, 0);
+                    }
+                }
+                xsum[i] += *(const f32x4 *)(sums + at_sums + s * (TM * 16) + 16 * i);
+            }
+            if (ends) {
+                const int from = (s >> fold_log2) * 16 + l16;
+#pragma unroll
+                for (int t = 0; t < TN; ++t) {
+                    uint32_t sc = c.scale[t], z = c.zero[t];
                     if (folds > 1) {
                         sc = __shfl((int)sc, from, WAVE);
                         z = __shfl((int)z, from, WAVE);
                     }
-                    scale[j] = F32 ? __builtin_bit_cast(float, sc) : __builtin_bit_cast(float, sc << 16);
-                    if (!p.has_zeros) z = 8;
-                    minus_zero[j] = XT == X_INT8 ? ((0u - z) & 255u) * 0x01010101u : (0xc180u | z << 3) * 0x00010001u;
-                }
+                    const float scale = __builtin_bit_cast(float, F32 ? sc : sc << 16);
+                    const float zero = (XT == X_INT8 ? 0.f : 16.f) + (p.has_zeros ? (float)z : 8.f);
 #pragma unroll
-                for (int i = 0; i < TM; ++i)
+                    for (int i = 0; i < TM; ++i) {
+                        f32x4 xs = {scale, scale, scale, scale};
+                        if (X8 && p.x_groups > 1) xs *= *(const f32x4 *)(xscales + at_sums + s * (TM * 16) + 16 * i);
 #pragma unroll
-                    for (int j = 0; j < TN; ++j) acc[i][j] = Sum<XT>{0, 0, 0, 0};
-            }
-#pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                const XOperand<XT> x = x_operand<XT>(c.x[i], s);
-#pragma unroll
-                for (int j = 0; j < TN; ++j) step<XT>(acc[i][j], x, c.w[j][s], minus_zero[j]);
-            }
-            if (((s + 1) & (p.fold - 1)) == 0) {           // and ends
-#pragma unroll
-                for (int i = 0; i < TM; ++i) {
-                    f32x4 xs = {1.f, 1.f, 1.f, 1.f};
-                    if (X8 && p.x_groups > 1) {
-                        const int k = at * BLOCK + (s + 1 - p.fold) * 32;
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const int m = 16 * i + 4 * g + r;
-                            const uint32_t o = m < rows && k < p.K ? (uint32_t)(m * p.x_groups + (k >> p.x_group_shift)) * 4u : OUT_OF_RANGE;
-                            xs[r] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rxs, o, 0, 0));
-                        }
+                        for (int r = 0; r < 4; ++r) total[i][t][r] = fmaf(fmaf(-zero, xsum[i][r], (float)acc[i][t][r]), xs[r], total[i][t][r]);
                     }
-#pragma unroll
-                    for (int j = 0; j < TN; ++j)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) total[i][j][r] = fmaf((float)acc[i][j][r], X8 ? xs[r] * scale[j] : scale[j], total[i][j][r]);
                 }
             }
         }
     };
 
 #pragma unroll
-    for (int d = 0; d < D; ++d) request(ring[d], wave + NW * d);
-    for (int piece = wave; piece < p.blocks; piece += NW * D) {
+    for (int d = 0; d < D; ++d) request(ring[d], d);
+    if constexpr (WHOLE) {
+        constexpr int BATCH = XT == X_F32 ? 2 : 4;         // requests of a thread under way
+        int piece = piece0, row = row_0;
+        for (int u = tid; u - tid < units; u += BATCH * NW * 64) {
+            XRaw<XT> x[BATCH];
+            int piece_too = piece, row_too = row;
+            each_unit(u, BATCH, piece, row, [&](int k, int q, int r, bool is) { x[k] = request_x(0, q, r, is); });
+            each_unit(u, BATCH, piece_too, row_too, [&](int k, int q, int r, bool is) { store_unit(0, 0, q, r, is, x[k]); });
+        }
+        __syncthreads();
+        for (int j0 = 0; j0 < my_pieces; j0 += D) {
 #pragma unroll
-        for (int d = 0; d < D; ++d) {
-            if (piece + NW * d < p.blocks) use(ring[d], piece + NW * d);
-            request(ring[d], piece + NW * (D + d));
+            for (int d = 0; d < D; ++d) {
+                if (j0 + d < my_pieces) use(ring[d], 0, (j0 + d) * parts + part);
+                request(ring[d], j0 + d + D);
+            }
+        }
+    } else {
+        static_assert(D == 4, "two chunks of two pieces");
+        const int chunks = (n_pieces + p.chunk - 1) / p.chunk;
+        XRaw<XT> ahead[MAX_UNITS];
+        auto request_chunk = [&](int chunk) {
+            int piece = piece0, row = row_0;
+            each_unit(tid, MAX_UNITS, piece, row, [&](int k, int q, int r, bool is) { ahead[k] = request_x(chunk, q, r, is); });
+        };
+        auto store_chunk = [&](int chunk, int held) {
+            int piece = piece0, row = row_0;
+            each_unit(tid, MAX_UNITS, piece, row, [&](int k, int q, int r, bool is) { store_unit(chunk, held, q, r, is, ahead[k]); });
+        };
+        request_chunk(0);
+        store_chunk(0, 0);
+        request_chunk(1);
+        __syncthreads();
+        for (int c0 = 0; c0 < chunks; c0 += 2) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const int j = 2 * (c0 + h) + t;
+                    if (j < my_pieces) use(ring[2 * h + t], h, t * parts + part);
+                    request(ring[2 * h + t], j + D);
+                }
+                if (c0 + h + 1 < chunks) {                 // the other half has been read before the barrier in front of this one
+                    store_chunk(c0 + h + 1, 1 - h);
+                    request_chunk(c0 + h + 2);
+                    __syncthreads();
+                }
+            }
         }
     }
 
-    const bool has_res = p.flags & CASCADE_EPI_RESIDUAL, has_bias = p.flags & CASCADE_EPI_BIAS;
+    float (*meet)[TN][256] = (float (*)[TN][256])lds;      // [wavefront][block][r * 64 + lane]
+    const int outs = cols * TNO * 256;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         if (16 * i >= rows) break;
-        if (i) __syncthreads();                            // the sums of the block before have been read
+        __syncthreads();                                   // X, or the sums of the block before, have been read
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
+        for (int t = 0; t < TN; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) part[wave][j][r * 64 + lane] = total[i][j][r];
+            for (int r = 0; r < 4; ++r) meet[wave][t][r * 64 + lane] = total[i][t][r];
         __syncthreads();
-#pragma unroll
-        for (int o = 0; o < PER; ++o) {
-            const int at = tid + o * NW * 64, j = at >> 8, m = (at >> 4) & 15, c = at & 15, n = (block0 + j) * 16 + c;
-            if (at >= OUT || 16 * i + m >= rows || n >= p.N) continue;
-            const int64_t row = row0 + 16 * i + m;
-            const int slot = (m & 3) * 64 + (m >> 2) * 16 + c;
+        for (int o = tid; o < outs; o += NW * 64) {        // row by row: neighbouring threads have neighbouring columns
+            const int col = o % (cols * TNO * 16), m = o / (cols * TNO * 16), b = col >> 4;
+            const int n = tile0 * 16 + col, row = row0 + 16 * i + m;
+            if (16 * i + m >= rows || n >= p.N) continue;
+            const int slot = (m & 3) * 64 + (m >> 2) * 16 + (col & 15), w0 = b / TNO, t0 = b % TNO;
             float v[2] = {0.f, 0.f};
-#pragma unroll
-            for (int w = 0; w < NW; ++w) {
-                v[0] += part[w][j][slot];
-                if (SWIGLU) v[1] += part[w][TN - 1][slot];
+            for (int w = 0; w < parts; ++w) {
+                v[0] += meet[w0 + w * cols][t0][slot];
+                if (SWIGLU) v[1] += meet[w0 + w * cols][TN - 1][slot];
             }
+            if (p.slices > 1) {
 #pragma unroll
-            for (int u = 0; u < (SWIGLU ? 2 : 1); ++u) {
-                if (X8 && p.x_groups == 1) v[u] *= p.x_scale[row];
-                if (!(fabsf(v[u]) < __builtin_inff())) v[u] = plain_output<XT, F32>(p, u, (int)row, n);
-            }
-            float y = v[0];
-            if (has_bias) y += (float)((const T *)p.bias)[n];
-            if (SWIGLU) y = silu_f(y) * v[1];
-            else y = F32 ? apply_act(y, p.flags) : apply_act_bf16(y, p.flags);
-            if (has_res) y += (float)((const T *)p.residual)[row * p.ldres + n];
-            ((T *)p.Y)[row * p.ldy + n] = (T)y;
+                for (int u = 0; u < MATS; ++u) p.planes[((int64_t)(blockIdx.y * MATS + u) * p.M + row) * p.N + n] = v[u];
+            } else finish<XT, F32, SWIGLU>(p, v, row, n);
         }
     }
 }
 
-template <int XT, bool F32, int TM, int TN, bool SWIGLU>
-void launch(const W4Params &p, hipStream_t s) {
-    constexpr int D = TM == 1 ? 4 : 2;
-    const unsigned cols = ((p.N + 15) / 16 + (SWIGLU ? 1 : TN) - 1) / (SWIGLU ? 1 : TN), rows = (p.M + TM * 16 - 1) / (TM * 16);
-    hipLaunchKernelGGL((w4_kernel<XT, F32, TM, TN, D, SWIGLU>), dim3(cols, rows), dim3(NW * 64), 0, s, p);
+// Adds the slices' sums in their order
+template <int XT, bool F32, bool SWIGLU>
+__global__ __launch_bounds__(256) void w4_finish_kernel(W4Params p) {
+    constexpr int MATS = SWIGLU ? 2 : 1;
+    const int64_t size = (int64_t)p.M * p.N;
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < size; e += (int64_t)gridDim.x * 256) {
+        float v[2] = {0.f, 0.f};
+#pragma unroll 4
+        for (int s = 0; s < p.slices; ++s)
+#pragma unroll
+            for (int u = 0; u < MATS; ++u) v[u] += p.planes[(s * MATS + u) * size + e];
+        finish<XT, F32, SWIGLU>(p, v, (int)(e / p.N), (int)(e % p.N));
+    }
 }
-template <int XT, bool F32, int TM>
-void launch_rows(const W4Params &p, hipStream_t s) {
-    if (p.flags & CASCADE_EPI_SWIGLU) launch<XT, F32, TM, 2, true>(p, s);
-    else if ((p.N + 15) / 16 >= 2 * 256) launch<XT, F32, TM, 2, false>(p, s);
-    else launch<XT, F32, TM, 1, false>(p, s);
+
+// How a product is cut.  One choice for the workspace and the launch.
+struct Cut {
+    int tm, tn, cols_log2, slices, slice_blocks, chunk, held;
+    size_t lds;
+};
+constexpr size_t LDS_MOST = 160 * 1024;
+
+Cut cut_of(const cascade_w4_weights *w, const cascade_w4_gemm_desc *d) {
+    const bool swiglu = d->epilogue & CASCADE_EPI_SWIGLU, x32 = !d->x_format && w->dtype == CASCADE_F32;
+    Cut c;
+    const int most_tm = x32 ? 2 : 4;
+    c.tm = d->rows <= 16 ? 1 : d->rows <= 32 ? 2 : most_tm;
+    const int rows = std::min(d->rows, c.tm * 16), unit = x32 ? 48 : d->x_format == CASCADE_Q8_INT8 ? 8 : 16;
+    const int blocks = (w->k + BLOCK - 1) / BLOCK, col_blocks = (w->n_out + 15) / 16;
+    c.tn = swiglu || c.tm > 1 || col_blocks > 256 ? 2 : 1;
+    const int units = (col_blocks + (swiglu ? 1 : c.tn) - 1) / (swiglu ? 1 : c.tn);      // of a wavefront's columns
+    auto lds_of = [&](int chunk, int held) { return (size_t)held * chunk * (16 * (rows | 1) * unit + 4 * c.tm * 16 * 4 * (d->x_format ? 2 : 1)); };
+    double best = 1e30;
+    for (int lg = 0; lg <= 3; ++lg) {
+        const int parts = NW >> lg, chunk = 2 * parts;
+        const int64_t tiles = (units + (1 << lg) - 1) >> lg;
+        for (int slices = 1; slices <= 32; ++slices) {
+            const int per = ((blocks + slices - 1) / slices + parts - 1) / parts * parts;
+            if (slices > 1 && ((int64_t)per * (slices - 1) >= blocks || per < 2 * parts)) continue;
+            const bool whole = lds_of(std::min(per, blocks), 1) <= LDS_MOST;
+            if (!whole && chunk * rows * 16 > MAX_UNITS * NW * 64) continue;
+            const size_t lds = std::max(whole ? lds_of(std::min(per, blocks), 1) : lds_of(chunk, 2), (size_t)NW * c.tn * 1024);
+            if (lds > LDS_MOST) continue;
+            const int resident = c.tm == 1 && whole && lds <= LDS_MOST / 2 ? 2 : 1;
+            // microseconds: rounds of workgroups, each a start and its pieces at the rate that the resident ones share
+            const int64_t groups = tiles * slices * ((d->rows + c.tm * 16 - 1) / (c.tm * 16));
+            const int64_t full = groups / (256 * resident), rest = groups - full * 256 * resident;
+            const double piece = c.tn * 1.024 / 20.0 * 8;  // eight wavefronts' pieces at 20 KB a microsecond and CU
+            const double turns = (double)((per + parts - 1) / parts);
+            const double bytes = (full * resident + (rest + 255) / 256) * turns * piece, start = 2.5 * (full + (rest ? 1 : 0));
+            const double planes = slices > 1 ? 3.0 + 2.0 * slices * d->rows * (double)w->n_out * 4 * (swiglu ? 2 : 1) / 4e6 : 0.0;
+            const double cost = bytes + start + planes;
+            if (cost < best) {
+                best = cost;
+                c.cols_log2 = lg; c.slices = slices; c.slice_blocks = per; c.chunk = whole ? std::min(per, blocks) : chunk;
+                c.held = whole ? 1 : 2; c.lds = lds;
+            }
+        }
+    }
+    return c;
 }
-template <int XT, bool F32>
-int32_t launch_x(const W4Params &p, hipStream_t s) {
-    if (p.M <= 16) launch_rows<XT, F32, 1>(p, s);
-    else if (p.M <= 32) launch_rows<XT, F32, 2>(p, s);
-    else launch_rows<XT, F32, 4>(p, s);
+
+template <int XT, bool F32, int TM, int TN, bool SWIGLU, bool WHOLE>
+int32_t launch(const W4Params &p, const Cut &c, hipStream_t s) {
+    static std::atomic<uint64_t> done{0};
+    const void *kernel = (const void *)w4_kernel<XT, F32, TM, TN, SWIGLU, WHOLE>;
+    CASCADE_HIP_TRY(ensure_dynamic_lds(kernel, (int)LDS_MOST, done));
+    const int cols = (SWIGLU ? 1 : TN) << c.cols_log2;
+    const dim3 grid((unsigned)(((p.N + 15) / 16 + cols - 1) / cols), (unsigned)p.slices, (unsigned)((p.M + TM * 16 - 1) / (TM * 16)));
+    hipLaunchKernelGGL((w4_kernel<XT, F32, TM, TN, SWIGLU, WHOLE>), grid, dim3(NW * 64), c.lds, s, p);
+    if (p.slices > 1)
+        hipLaunchKernelGGL((w4_finish_kernel<XT, F32, SWIGLU>), dim3((unsigned)std::min<int64_t>(((int64_t)p.M * p.N + 255) / 256, 1 << 16)), dim3(256), 0, s, p);
     CASCADE_HIP_TRY(hipGetLastError());
     return CASCADE_OK;
+}
+template <int XT, bool F32, int TM, int TN, bool SWIGLU>
+int32_t launch_held(const W4Params &p, const Cut &c, hipStream_t s) {
+    return c.held == 1 ? launch<XT, F32, TM, TN, SWIGLU, true>(p, c, s) : launch<XT, F32, TM, TN, SWIGLU, false>(p, c, s);
+}
+template <int XT, bool F32, int TM>
+int32_t launch_rows(const W4Params &p, const Cut &c, hipStream_t s) {
+    if (p.flags & CASCADE_EPI_SWIGLU) return launch_held<XT, F32, TM, 2, true>(p, c, s);
+    if constexpr (TM == 1)
+        if (c.tn == 1) return launch_held<XT, F32, 1, 1, false>(p, c, s);
+    return launch_held<XT, F32, TM, 2, false>(p, c, s);
+}
+template <int XT, bool F32>
+int32_t launch_x(const W4Params &p, const Cut &c, hipStream_t s) {
+    if (c.tm == 1) return launch_rows<XT, F32, 1>(p, c, s);
+    if constexpr (XT != X_F32)
+        if (c.tm == 4) return launch_rows<XT, F32, 4>(p, c, s);
+    return launch_rows<XT, F32, 2>(p, c, s);
 }
 
 // ---------------------------------------------------------------------------- layout
@@ -443,14 +592,14 @@ extern "C" int32_t cascade_w4_pack(const cascade_w4_weights *w, const void *code
 }
 
 extern "C" size_t cascade_w4_gemm_workspace_bytes(const cascade_w4_weights *w, const cascade_w4_gemm_desc *d) {
-    if (check_gemm(w, d) != CASCADE_OK) return 0;
-    return 0;
+    if (check_gemm(w, d) != CASCADE_OK || d->rows == 0) return 0;
+    const Cut c = cut_of(w, d);
+    return c.slices > 1 ? (size_t)c.slices * d->rows * w->n_out * 4 * (d->epilogue & CASCADE_EPI_SWIGLU ? 2 : 1) : 0;
 }
 
 extern "C" int32_t cascade_w4_gemm(const cascade_w4_weights *w, const cascade_w4_weights *up, const cascade_w4_gemm_desc *d, const void *X,
                                    const float *x_scale, const void *bias, const void *residual, void *Y, void *workspace,
                                    size_t workspace_bytes, void *stream) {
-    (void)workspace; (void)workspace_bytes;
     const int32_t st = check_gemm(w, d);
     if (st != CASCADE_OK) return st;
     const bool swiglu = d->epilogue & CASCADE_EPI_SWIGLU;
@@ -487,8 +636,12 @@ extern "C" int32_t cascade_w4_gemm(const cascade_w4_weights *w, const cascade_w4
     p.x_group_shift = x_group ? __builtin_ctz((unsigned)x_group) : 31;
     p.x_groups = x_group ? p.K / x_group : 1;
     p.has_zeros = w->zero_points; p.flags = d->epilogue;
+    const Cut c = cut_of(w, d);
+    if (c.slices > 1 && (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < cascade_w4_gemm_workspace_bytes(w, d))) return CASCADE_EWORKSPACE;
+    p.planes = (float *)workspace;
+    p.cols_log2 = c.cols_log2; p.slices = c.slices; p.slice_blocks = c.slice_blocks; p.chunk = c.chunk; p.chunks_held = c.held;
     hipStream_t s = (hipStream_t)stream;
-    if (d->x_format == CASCADE_Q8_E4M3) return f32 ? launch_x<X_E4M3, true>(p, s) : launch_x<X_E4M3, false>(p, s);
-    if (d->x_format == CASCADE_Q8_INT8) return f32 ? launch_x<X_INT8, true>(p, s) : launch_x<X_INT8, false>(p, s);
-    return f32 ? launch_x<X_F32, true>(p, s) : launch_x<X_BF16, false>(p, s);
+    if (d->x_format == CASCADE_Q8_E4M3) return f32 ? launch_x<X_E4M3, true>(p, c, s) : launch_x<X_E4M3, false>(p, c, s);
+    if (d->x_format == CASCADE_Q8_INT8) return f32 ? launch_x<X_INT8, true>(p, c, s) : launch_x<X_INT8, false>(p, c, s);
+    return f32 ? launch_x<X_F32, true>(p, c, s) : launch_x<X_BF16, false>(p, c, s);
 }
