@@ -4,26 +4,39 @@
 // sum of the weights passes a target, so everything asked of a row is "at which place does the running count, or the running sum,
 // reach this".  Pass 1 (a workgroup per chunk of a row) puts every logit into one of 704 bins of 1/16 in the exponent, on a grid
 // that does not depend on the row's maximum, so that the chunks' bins add up; a bin holds how many and the sum of their weights
-// relative to the bin's edge.  Pass 2 (a workgroup per row) adds the chunks, scans the bins, and looks closer where a border falls
+// relative to the bin's middle.  Pass 2 (a workgroup per row) adds the chunks, scans the bins, and looks closer where a border falls
 // inside a bin: the bin's elements are gathered from the row and sorted (up to 1024), or counted again in 1024 finer bins of the
 // numbers' own bit patterns until they are few or all alike.  Where all that can be kept has at most 1024 elements, one
-// gathering answers everything.
+// gathering answers everything; the chunks keep their largest elements (64, or a bin's end more) beside their bins, which
+// usually hold all that is to be gathered, because a second look at a row takes one CU 6 us for a quarter of a megabyte.
 //
-// Weights are exp(z / 16), z = 16 l / temperature in 64 bits; relative to the bin's edge, which lies within a sixteenth, they are whole
+// One token is the latency of a chain of short steps that each run once: the second pass is written for little code (rolled loops,
+// lane moves, one copy of a step), which its wavefronts fetch from cold caches.
+//
+// Weights are exp(z / 16), z = 16 l / temperature in 64 bits; relative to the middle of the bin, at most a 32nd away, they are whole
 // numbers of 2^-29, so that sums within a bin are exact and do not depend on any order; the rounding (2^-30 of a weight, either
 // way) is what the result is exact to.  Elements of weight below e^-43 of the largest are left out: 2^20 of them are 2e-13 of the sum.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 #include "common.h"
 #include "device_utils.h"
+
+// Pass 1 and pass 2 have to place an element alike: products are rounded before anything is added, fma() where one is meant
+#pragma clang fp contract(off)
 
 namespace {
 
 constexpr int BINS = 704;                                  // 44 in the exponent
 constexpr int COUNT_SHIFT = 46;                            // of a bin's word: sum below (2^13 .. 2^15 elements of less than 2^30)
-constexpr int CHUNK_WORDS = BINS + 2;                      // of 8 bytes: grid place of the maximum; maximum and where; bins
 constexpr int LIST = 1024;                                 // elements that are sorted, and threads of the second pass
 constexpr double UNIT = 0x1p-29;                           // of a weight within its bin
+
+// What the first pass leaves of a chunk, in words of 8 bytes: where its bins begin; its maximum, and where that is (greedy rows);
+// the last bin whose elements it kept all (-1: none) and how many it kept; the bins; the elements kept (~key, index)
+enum { HEAD_BASE, HEAD_MOST, HEAD_KEPT, HEADS };
+constexpr int KEEP = 64, ROOM = 128;                       // largest elements kept, and up to so many where a bin ends later
+constexpr int CHUNK_WORDS = HEADS + BINS + ROOM;
 
 struct SampleParams {
     const void *logits;
@@ -44,29 +57,39 @@ __device__ __forceinline__ uint32_t key_of(float v) {
 __device__ __forceinline__ float value_of(uint32_t k) {
     return __builtin_bit_cast(float, k ^ ((uint32_t)((int32_t)~k >> 31) | 0x80000000u));
 }
+// Largest value of a window of keys that ends at k: -0, which no element has, would let 0 in
+__device__ __forceinline__ float end_of(uint32_t k) { return value_of(k == 0x7fffffffu ? k - 1 : k); }
 constexpr uint32_t KEY_MIN = 0x00800000u, KEY_INF = 0xff800000u;                 // smallest finite value's key, +inf's
 
-// Where a value lies on the grid; c = 16 / temperature.  With an infinity in the row, only infinities count, at 0.
-__device__ __forceinline__ double grid(float v, double c, bool inf) { return inf ? (v == INFINITY ? 0.0 : -0x1p1000) : (double)v * c; }
-// exp(d / 16) in units of 2^-29, 0 <= d < 1: power series around the middle, remainder 1.3e-12
+// Where a value lies on the grid; c = 16 / temperature.  Its bin is the nearest whole number.  Beside an infinite maximum, or one so
+// far out on the grid that fp32 numbers are more than all bins apart, nothing else counts: then the maximum lies at 0.
+__device__ __forceinline__ bool stands_alone(float most, double c) { return most == INFINITY || fabs((double)most * c) >= 0x1p40; }
+__device__ __forceinline__ double grid(float v, double c, bool alone, float most) { return alone ? (v >= most ? 0.0 : -0x1p1000) : (double)v * c; }
+// exp(d / 16) in units of 2^-29, |d| <= 1/2: power series (remainder 2.5e-10 at the ends, an eighth of a unit); the last step adds
+// 1.5 * 2^52, which leaves the rounded whole number in the low word
+constexpr double TO_WHOLE = 0x1.8p52;
+__device__ __forceinline__ uint32_t low_word(double x) { return (uint32_t)__builtin_bit_cast(uint64_t, x); }
 __device__ __forceinline__ uint32_t weight(double d) {
-    const double x = fma(d, 0.0625, -0.03125);
-    double e = fma(x, 1.0 / 120, 1.0 / 24);
-    e = fma(e, x, 1.0 / 6);
-    e = fma(e, x, 0.5);
-    e = fma(e, x, 1.0);
-    e = fma(e, x, 1.0);
-    return (uint32_t)fma(e, 1.0317434074991026710 / UNIT, 0.5);                  // e^(1/32)
+    constexpr double U = 1.0 / UNIT;
+    double e = fma(d, U / (24.0 * 65536), U / (6.0 * 4096));
+    e = fma(e, d, U / (2.0 * 256));
+    e = fma(e, d, U / 16.0);
+    return low_word(fma(e, d, U + TO_WHOLE));
 }
-
 template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Piece { uint32_t w[4]; };
 template <typename T> constexpr int PER = 16 / (int)sizeof(T);                   // logits of a request
 
-// NaN to -inf, -0 to 0
-__device__ __forceinline__ float clean(float v) { return fmaxf(v, -INFINITY) + 0.f; }
 template <typename T> __device__ __forceinline__ float logit(const Piece<T> &p, int e) {
-    if constexpr (sizeof(T) == 4) return clean(__builtin_bit_cast(float, p.w[e]));
-    else return clean(__builtin_bit_cast(float, e & 1 ? p.w[e >> 1] & 0xffff0000u : p.w[e >> 1] << 16));
+    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, p.w[e]);
+    else return __builtin_bit_cast(float, e & 1 ? p.w[e >> 1] & 0xffff0000u : p.w[e >> 1] << 16);
+}
+// Moves the logits of a piece up by one
+template <typename T> __device__ __forceinline__ void next(Piece<T> &p) {
+    if constexpr (sizeof(T) == 4) {
+        p.w[0] = p.w[1]; p.w[1] = p.w[2]; p.w[2] = p.w[3];
+    } else {
+        p.w[0] = p.w[0] >> 16 | p.w[1] << 16; p.w[1] = p.w[1] >> 16 | p.w[2] << 16; p.w[2] = p.w[2] >> 16 | p.w[3] << 16; p.w[3] >>= 16;
+    }
 }
 // Logits i .. i + PER - 1 of a row of V; past its end -inf.  Whole pieces are requested without a branch.
 template <typename T>
@@ -78,14 +101,29 @@ __device__ __forceinline__ Piece<T> request(const T *row, int64_t i, int V) {
 template <typename T>
 __device__ __forceinline__ void mend(const T *row, int64_t i, int V, Piece<T> &p) {
     if (V - i >= PER<T>) return;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) p.w[j] = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
-#pragma unroll
-    for (int e = 0; e < PER<T>; ++e)
-        if (i + e < V) {
-            if constexpr (sizeof(T) == 4) p.w[e] = __builtin_bit_cast(uint32_t, row[i + e]);
-            else p.w[e >> 1] = (p.w[e >> 1] & (e & 1 ? 0xffffu : 0xffff0000u)) | (uint32_t)__builtin_bit_cast(uint16_t, row[i + e]) << (e & 1 ? 16 : 0);
+    typedef typename std::conditional<sizeof(T) == 4, uint32_t, uint16_t>::type bits;
+    for (int e = PER<T> - 1; e >= 0; --e) {                // each behind those before it
+        const uint32_t x = i + e < V ? (uint32_t)__builtin_bit_cast(bits, row[i + e]) : sizeof(T) == 4 ? 0xff800000u : 0xff80u;
+        if constexpr (sizeof(T) == 4) {
+            p.w[3] = p.w[2]; p.w[2] = p.w[1]; p.w[1] = p.w[0]; p.w[0] = x;
+        } else {
+            p.w[3] = p.w[3] << 16 | p.w[2] >> 16; p.w[2] = p.w[2] << 16 | p.w[1] >> 16; p.w[1] = p.w[1] << 16 | p.w[0] >> 16;
+            p.w[0] = p.w[0] << 16 | x;
         }
+    }
+}
+
+// Whether a piece may hold a value of at least lo > 0: positive numbers order as whole numbers of their bits, negative ones lie below
+template <typename T>
+__device__ __forceinline__ bool may_reach(const Piece<T> &p, float lo) {
+    if constexpr (sizeof(T) == 4) {
+        return max(max((int32_t)p.w[0], (int32_t)p.w[1]), max((int32_t)p.w[2], (int32_t)p.w[3])) >= __builtin_bit_cast(int32_t, lo);
+    } else {
+        typedef __attribute__((ext_vector_type(2))) int16_t i16x2;
+        const auto h = [&](int i) { return __builtin_bit_cast(i16x2, p.w[i]); };
+        const i16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(h(0), h(1)), __builtin_elementwise_max(h(2), h(3)));
+        return max(m[0], m[1]) >= (int16_t)(__builtin_bit_cast(int32_t, lo) >> 16);
+    }
 }
 
 __device__ __forceinline__ double grid_scale(const SampleParams &p, int row, bool &greedy) {
@@ -94,16 +132,50 @@ __device__ __forceinline__ double grid_scale(const SampleParams &p, int row, boo
     return greedy ? 0.0 : 16.0 / (double)t;
 }
 
+// Running sums over a wavefront by lane moves: inside rows of 16, then the rows' sums
+template <int CTRL, int ROWS, typename V>
+__device__ __forceinline__ V moved(V v) {                  // 0 where no lane gives
+    if constexpr (sizeof(V) == 4) return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+    else {
+        const u32x2 w = __builtin_bit_cast(u32x2, v);
+        const u32x2 r = {(uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[0], CTRL, ROWS, 0xf, false), (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[1], CTRL, ROWS, 0xf, false)};
+        return __builtin_bit_cast(V, r);
+    }
+}
+template <typename V>
+__device__ __forceinline__ V row_running_sum(V v) {
+    v += moved<0x111, 0xf>(v);                             // from 1, 2, 4 and 8 lanes before
+    v += moved<0x112, 0xf>(v);
+    v += moved<0x114, 0xf>(v);
+    return v + moved<0x118, 0xf>(v);
+}
+template <typename V>
+__device__ __forceinline__ V wave_running_sum(V v) {
+    v = row_running_sum(v);
+    v += moved<0x142, 0xa>(v);                             // the last lane of a row to the next one, of the first two to the others
+    return v + moved<0x143, 0xc>(v);
+}
+template <typename V>
+__device__ __forceinline__ V of_lane(V v, int lane) {      // the same for all lanes
+    if constexpr (sizeof(V) == 4) return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+    else {
+        const u32x2 w = __builtin_bit_cast(u32x2, v);
+        return __builtin_bit_cast(V, u32x2{(uint32_t)__builtin_amdgcn_readlane((int)w[0], lane), (uint32_t)__builtin_amdgcn_readlane((int)w[1], lane)});
+    }
+}
+
 // ---------------------------------------------------------------------------- pass 1: the bins of a chunk
 constexpr int chunk_of(int threads) { return threads * 32; }
 
 template <typename T, int NT>
-__global__ __launch_bounds__(NT) void sample_bins_kernel(SampleParams p) {
-    constexpr int N = 32 / PER<T>, WAVES = NT / 64;        // pieces of a thread
-    __shared__ unsigned long long bins[BINS];
+__global__ __launch_bounds__(NT, sizeof(T) == 2 ? 8 : 4) void sample_bins_kernel(SampleParams p) {
+    constexpr int N = 32 / PER<T>, WAVES = NT / 64, MINE = (BINS + NT - 1) / NT;
+    __shared__ unsigned long long bins[MINE * NT];
     __shared__ float wave_most[WAVES];
     __shared__ int wave_first[WAVES];
-    const int row = blockIdx.x / p.n_chunks, chunk = blockIdx.x - row * p.n_chunks, tid = threadIdx.x;
+    __shared__ uint32_t wave_count[WAVES], kept;
+    __shared__ int last_kept;
+    const int row = blockIdx.x / p.n_chunks, chunk = blockIdx.x - row * p.n_chunks, tid = threadIdx.x, wave = tid >> 6;
     const T *logits = (const T *)p.logits + row * p.stride;
     const int64_t i0 = (int64_t)chunk * chunk_of(NT) + tid * PER<T>;
     Piece<T> v[N];
@@ -111,7 +183,24 @@ __global__ __launch_bounds__(NT) void sample_bins_kernel(SampleParams p) {
     for (int j = 0; j < N; ++j) v[j] = request(logits, i0 + j * NT * PER<T>, p.vocab);
     bool greedy;
     const double c = grid_scale(p, row, greedy);
-    for (int b = tid; b < BINS; b += NT) bins[b] = 0;
+#pragma unroll
+    for (int b = 0; b < MINE; ++b) bins[tid + b * NT] = 0;
+    if (tid == 0) {
+        kept = 0;
+        last_kept = BINS - 1;
+    }
+    // f(logit, index) for all of the thread's, one copy of the code for its pieces, which move up
+    auto each = [&](auto f) {
+#pragma unroll 1
+        for (int j = 0; j < N; ++j) {
+            const Piece<T> now = v[0];
+#pragma unroll
+            for (int k = 0; k + 1 < N; ++k) v[k] = v[k + 1];
+            v[N - 1] = now;
+#pragma unroll
+            for (int e = 0; e < PER<T>; ++e) f(logit(now, e), (int)(i0 + j * NT * PER<T> + e));
+        }
+    };
     float most = -INFINITY;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
@@ -120,118 +209,164 @@ __global__ __launch_bounds__(NT) void sample_bins_kernel(SampleParams p) {
         for (int e = 0; e < PER<T>; ++e) most = fmaxf(most, logit(v[j], e));
     }
     most = wave_max(most);
-    if ((tid & 63) == 0) wave_most[tid >> 6] = most;
+    if ((tid & 63) == 0) wave_most[wave] = most;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) most = fmaxf(most, wave_most[w]);
     uint64_t *out = p.chunks + (int64_t)blockIdx.x * CHUNK_WORDS;
-    const bool inf = most == INFINITY;
-    const double top = most == -INFINITY ? 0.0 : floor(grid(most, c, inf));
-    int first = INT32_MAX;
+    const bool alone = most > -INFINITY && stands_alone(most, c);
+    const double base = most == -INFINITY || most == INFINITY ? 0.0 : rint((double)most * c);
+    // Values below `least` are out of the bins' reach; the few others that are, too, are kept back by the bin's number
+    const float least = alone ? most : fmaxf((float)((base - BINS - 2 - fabs(base) * 0x1p-20) / c), -0x1.fffffep127f);
+    const uint32_t zero = low_word(base + TO_WHOLE);
     if (greedy) {
-#pragma unroll
-        for (int j = N - 1; j >= 0; --j)
-#pragma unroll
-            for (int e = PER<T> - 1; e >= 0; --e)
-                if (logit(v[j], e) == most) first = (int)(i0 + j * NT * PER<T> + e);
+        int first = INT32_MAX;
+        each([&](float l, int i) { first = l == most ? min(first, i) : first; });
         for (int o = 32; o; o >>= 1) first = min(first, __shfl_xor(first, o, WAVE));
-        if ((tid & 63) == 0) wave_first[tid >> 6] = first;
+        if ((tid & 63) == 0) wave_first[wave] = first;
         __syncthreads();
+        if (tid == 0) {
+            for (int w = 1; w < WAVES; ++w) first = min(first, wave_first[w]);
+            out[HEAD_MOST] = (uint64_t)__builtin_bit_cast(uint32_t, most) << 32 | (uint32_t)first;
+        }
+        return;
+    }
+    if (alone) each([&](float l, int) { if (l >= least) atomicAdd(&bins[0], (1ull << COUNT_SHIFT) | weight(0.0)); });
+    else each([&](float l, int) {
+        const double z = (double)l * c, t = z + TO_WHOLE;
+        const uint32_t b = zero - low_word(t);
+        if (l >= least && b < (uint32_t)BINS) atomicAdd(&bins[b], (1ull << COUNT_SHIFT) | weight(z - (t - TO_WHOLE)));     // (no NaN)
+    });
+    __syncthreads();
+
+    // the bin down to which elements are kept: the first ones that hold KEEP, without the last if they are more than there is room for
+    uint32_t mine[MINE], sum = 0;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) first = min(first, wave_first[w]);
-    } else if (most > -INFINITY) {
+    for (int b = 0; b < MINE; ++b) {
+        const uint64_t w = bins[tid * MINE + b];
+        mine[b] = (uint32_t)(w >> COUNT_SHIFT);
+        sum += mine[b];
+    }
+    const uint32_t upto = wave_running_sum(sum);
+    if ((tid & 63) == 63) wave_count[wave] = upto;
+    __syncthreads();
+    uint32_t run = upto - sum;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) run += w < wave ? wave_count[w] : 0u;
+#pragma unroll
+    for (int b = 0; b < MINE; ++b) {
+        if (run < (uint32_t)KEEP && run + mine[b] >= (uint32_t)KEEP) last_kept = run + mine[b] <= (uint32_t)ROOM ? tid * MINE + b : tid * MINE + b - 1;
+        run += mine[b];
+    }
+    for (int b = tid; b < BINS; b += NT) out[HEADS + b] = bins[b];
+    __syncthreads();
+    // (rows that no filter cuts are not asked for their largest)
+    const bool cut = (p.top_k && p.top_k[row] > 0) || (p.top_p && p.top_p[row] < 1.f) || (p.min_p && p.min_p[row] > 0.f);
+    const int last = cut ? last_kept : -1;
+    if (cut) {
+        const float lowest = alone ? least : fmaxf((float)((base - last - 2 - fabs(base) * 0x1p-20) / c), least);
+        uint32_t candidates = 0;                           // few of the 32, which are then read again
 #pragma unroll
         for (int j = 0; j < N; ++j)
 #pragma unroll
-            for (int e = 0; e < PER<T>; ++e) {
-                const float l = logit(v[j], e);
-                const double z = grid(l, c, inf), f = floor(z), down = top - f;  // (-inf: down is infinite, or NaN where c is 0)
-                if (l > -INFINITY && down < (double)BINS)
-                    atomicAdd(&bins[(int)down], (1ull << COUNT_SHIFT) | weight(z - f));
-            }
+            for (int e = 0; e < PER<T>; ++e) candidates |= logit(v[j], e) >= lowest ? 1u << (j * PER<T> + e) : 0u;
+        for (; candidates; candidates &= candidates - 1) {
+            const int which = __builtin_ctz(candidates), i = (int)i0 + which / PER<T> * (NT * PER<T>) + which % PER<T>;
+            const float l = (float)logits[i];
+            if (!alone && (int)(zero - low_word((double)l * c + TO_WHOLE)) > last) continue;
+            const uint32_t at = atomicAdd(&kept, 1u);
+            if (at < (uint32_t)ROOM) out[HEADS + BINS + at] = (uint64_t)~key_of(l + 0.f) << 32 | (uint32_t)i;
+        }
     }
-    if (tid == 0) {
-        out[0] = __builtin_bit_cast(uint64_t, top);
-        out[1] = (uint64_t)__builtin_bit_cast(uint32_t, most) << 32 | (uint32_t)first;
-    }
-    if (greedy) return;
     __syncthreads();
-    for (int b = tid; b < BINS; b += NT) out[2 + b] = bins[b];
+    if (tid == 0) {
+        out[HEAD_BASE] = __builtin_bit_cast(uint64_t, base);
+        out[HEAD_MOST] = (uint64_t)__builtin_bit_cast(uint32_t, most) << 32;
+        out[HEAD_KEPT] = (uint64_t)(uint32_t)last << 32 | min(kept, (uint32_t)ROOM);
+    }
 }
 
 // ---------------------------------------------------------------------------- pass 2: the row
-// Whole-workgroup steps, LIST threads; every one ends behind a barrier, so that they follow each other freely.
-struct Scratch {
-    double d[LIST / 64];
-    uint64_t u[LIST / 64];
-    uint32_t n[LIST / 64];
+// Steps of the whole workgroup (LIST threads) in which each wavefront leaves a value and reads all of them behind one barrier.  Two
+// sets of places in turn: whoever writes a set has passed the barrier of the other one, behind which nobody reads it any more.
+constexpr int WAVES = LIST / 64;
+struct Meet {
+    uint64_t at[2][WAVES];
 };
-template <typename V>
-__device__ __forceinline__ V running_sum(V v, V *waves) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const V up = __shfl_up(v, o, WAVE);
-        if (lane >= o) v += up;
-    }
-    if (lane == 63) waves[wave] = v;
-    __syncthreads();
-    V before = 0;
-    for (int w = 0; w < wave; ++w) before += waves[w];
-    __syncthreads();
-    return before + v;
-}
-// first thread for which `is` holds; LIST: none
-__device__ __forceinline__ int first_thread(bool is, uint32_t *waves) {
-    const uint64_t b = __ballot(is);
-    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = b ? (threadIdx.x & ~63u) + __builtin_ctzll(b) : LIST;
-    __syncthreads();
-    uint32_t m = LIST;
-    for (int w = 0; w < LIST / 64; ++w) m = min(m, waves[w]);
-    __syncthreads();
-    return (int)m;
-}
-__device__ __forceinline__ uint32_t total_count(uint32_t v, uint32_t *waves) {
-    for (int o = 32; o; o >>= 1) v += __shfl_xor((int)v, o, WAVE);
-    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = v;
-    __syncthreads();
-    uint32_t s = 0;
-    for (int w = 0; w < LIST / 64; ++w) s += waves[w];
-    __syncthreads();
-    return s;
-}
+struct Steps {
+    Meet &meet;
+    int turn;
 
+    template <typename V> __device__ __forceinline__ V *places() {
+        turn ^= 1;
+        return (V *)meet.at[turn];
+    }
+    template <typename V> __device__ __forceinline__ V running_sum(V v) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        V *waves = places<V>();
+        v = wave_running_sum(v);
+        if (lane == 63) waves[wave] = v;
+        __syncthreads();
+        const V before = row_running_sum(lane < wave ? waves[lane & (WAVES - 1)] : (V)0);
+        return of_lane(before, 15) + v;
+    }
+    // first thread for which `is` holds; LIST: none
+    __device__ __forceinline__ int first_thread(bool is) {
+        const uint64_t b = __ballot(is);
+        uint32_t *waves = places<uint32_t>();
+        const int lane = threadIdx.x & 63;
+        if (lane == 0) waves[threadIdx.x >> 6] = b ? (threadIdx.x & ~63u) + __builtin_ctzll(b) : LIST;
+        __syncthreads();
+        const uint32_t first = waves[lane & (WAVES - 1)];
+        const uint64_t any = __ballot(first < (uint32_t)LIST);
+        return any ? of_lane((int)first, __builtin_ctzll(any) & 63) : LIST;
+    }
+    __device__ __forceinline__ uint32_t total(uint32_t v) { return of_last(running_sum(v)); }
+    template <typename V> __device__ __forceinline__ V of_last(V v) {            // the last thread's
+        V *waves = places<V>();
+        if (threadIdx.x == LIST - 1) waves[0] = v;
+        __syncthreads();
+        return waves[0];
+    }
+};
+
+enum { AT_PLACE, AT_BIN, ABOVE_BIN };
 template <typename T>
 struct Row {
     const T *logits;
     int32_t V;
     double c;
-    bool inf;
+    bool alone;
+    float most;
 
-    // f(value, index) for every logit, pieces of a thread requested four at a time
-    template <typename F> __device__ __forceinline__ void each(F f) const {
-        constexpr int STEP = LIST * PER<T>;
-        for (int64_t i0 = (int64_t)threadIdx.x * PER<T>; i0 < V; i0 += 4 * STEP) {
-            Piece<T> v[4];
+    __device__ __forceinline__ double place(float v) const { return grid(v, c, alone, most); }
+
+    // f(value, index) for every logit of at least lo (and some below), pieces of a thread requested eight at a time
+    template <typename F> __device__ __forceinline__ void each(float lo, F f) const {
+        constexpr int STEP = LIST * PER<T>, N = 8;
+        for (int64_t i0 = (int64_t)threadIdx.x * PER<T>; i0 < V; i0 += N * STEP) {
+            Piece<T> v[N];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = request(logits, i0 + j * STEP, V);
+            for (int j = 0; j < N; ++j) v[j] = request(logits, i0 + j * STEP, V);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                mend(logits, i0 + j * STEP, V, v[j]);
-#pragma unroll
-                for (int e = 0; e < PER<T>; ++e) f(logit(v[j], e), (int)(i0 + j * STEP + e));
+            for (int j = 0; j < N; ++j) {
+                const int64_t i = i0 + j * STEP;
+                if (i >= V || (lo > 0.f && V - i >= PER<T> && !may_reach(v[j], lo))) continue;
+                mend(logits, i, V, v[j]);
+#pragma unroll 1
+                for (int e = 0; e < PER<T>; ++e, next(v[j])) f(logit(v[j], 0), (int)(i + e));
             }
         }
     }
-    // smallest key whose place on the grid is at least z (ABOVE: beyond the bin that begins at z; KEY_INF + 1: none), found by
-    // every wavefront for itself
-    template <bool ABOVE = false>
+    // smallest key whose place on the grid is at least z (AT_BIN: whose bin is at least z, ABOVE_BIN: above z; KEY_INF + 1: none),
+    // found by every wavefront for itself
+    template <int WHAT>
     __device__ __forceinline__ uint32_t first_key(double z) const {
         uint32_t lo = KEY_MIN, n = KEY_INF + 1 - KEY_MIN;  // the answer is lo .. lo + n
         while (n) {
             const uint32_t step = (n + 63) >> 6, at = (threadIdx.x & 63) * step;
-            const double place = grid(value_of(lo + (at < n ? at : 0)), c, inf);
-            const bool is = at >= n || (ABOVE ? floor(place) > z : place >= z);
+            const double place = this->place(value_of(lo + (at < n ? at : 0)));
+            const bool is = at >= n || (WHAT == ABOVE_BIN ? rint(place) > z : WHAT == AT_BIN ? rint(place) >= z : place >= z);
             const uint64_t b = __ballot(is);
             if (!b) {                                      // behind the last one asked
                 lo += 63 * step + 1;
@@ -248,35 +383,32 @@ struct Row {
     }
 };
 
+constexpr int MOST_CHUNKS = 128;                           // 2^20 logits in chunks of 8192
+
 struct Shared {
+    int32_t down[MOST_CHUNKS];                             // bins by which a chunk's begin below the row's; BINS: none of it counts
+    uint32_t kept[MOST_CHUNKS];                            // elements that the chunk kept
     double mass[BINS];                                     // running sums of the bins
     uint32_t count[BINS];
     uint64_t list[LIST];                                   // sorted elements (~key, index), or the sums of finer bins
     uint32_t fine[LIST];                                   // their counts
     uint32_t n;
     int32_t at;
-    Scratch s;
+    double found[2];
+    uint64_t sum;
+    Meet meet;
 };
 
-// Gathers the elements of keys klo .. khi (n of them, at most LIST), sorts them and returns the caller's, or ~0
-template <typename T>
-__device__ uint64_t gather(const Row<T> &row, uint32_t klo, uint32_t khi, uint32_t n, Shared &sh) {
-    const float lo = value_of(klo), hi = value_of(khi);
+// Sorts the n <= LIST elements of the list (the others ~0) and returns the caller's
+__device__ __forceinline__ uint64_t sorted(uint32_t n, Shared &sh) {
     const int tid = threadIdx.x;
-    if (tid == 0) sh.n = 0;
-    sh.list[tid] = ~0ull;
-    __syncthreads();
-    row.each([&](float v, int i) {
-        if (v >= lo && v <= hi) {
-            const uint32_t at = atomicAdd(&sh.n, 1u);
-            if (at < LIST) sh.list[at] = (uint64_t)~key_of(v) << 32 | (uint32_t)i;
-        }
-    });
     __syncthreads();
     uint64_t mine = sh.list[tid];
     uint32_t width = 64;
     while (width < n) width <<= 1;
+#pragma unroll 1
     for (uint32_t k = 2; k <= width; k <<= 1)              // bitonic; exchanges inside a wavefront by lane
+#pragma unroll 1
         for (uint32_t o = k >> 1; o; o >>= 1) {
             uint64_t other;
             if (o < 64) other = __shfl_xor((unsigned long long)mine, (int)o, WAVE);
@@ -292,6 +424,32 @@ __device__ uint64_t gather(const Row<T> &row, uint32_t klo, uint32_t khi, uint32
     __syncthreads();
     return mine;
 }
+__device__ __forceinline__ void start_list(Shared &sh) {
+    if (threadIdx.x == 0) sh.n = 0;
+    sh.list[threadIdx.x] = ~0ull;
+    __syncthreads();
+}
+__device__ __forceinline__ void put(uint64_t element, Shared &sh) {
+    const uint32_t at = atomicAdd(&sh.n, 1u);
+    if (at < LIST) sh.list[at] = element;
+}
+// Gathers the row's elements of keys klo .. khi (at most LIST) into the list
+template <typename T>
+__device__ __attribute__((noinline)) void gather(const Row<T> &row, uint32_t klo, uint32_t khi, Shared &sh) {
+    const float lo = value_of(klo), hi = end_of(khi);
+    start_list(sh);
+    row.each(lo, [&](float v, int i) {
+        if (v >= lo && v <= hi) put((uint64_t)~key_of(v + 0.f) << 32 | (uint32_t)i, sh);
+    });
+}
+// exp(-b / 16), b >= 0 a whole number: 2 to the whole and the rest, the rest by its power series (1e-15)
+__device__ __forceinline__ double bin_weight(double b) {
+    const double y = b * (-1.4426950408889634074 / 16), i = rint(y), f = (y - i) * 0.693147180559945309417;
+    double e = 1.0;
+#pragma unroll
+    for (int k = 13; k; --k) e = fma(e * f, 1.0 / k, 1.0);
+    return ldexp(e, (int)i);
+}
 
 struct Place {
     uint32_t count;                                        // elements up to and with this one
@@ -302,83 +460,84 @@ struct Place {
 // The first place in descending order at which the running count reaches k (by_count), or the running sum reaches t
 // (over: exceeds it).  One that does not exist is the last place.  `index`: whether the element itself is wanted.
 template <typename T>
-__device__ Place search(const Row<T> &row, double top, Shared &sh, bool by_count, uint32_t k, double t, bool over, bool index) {
+__device__ __attribute__((noinline)) Place search(const Row<T> &row, double base, Shared &sh, Steps &steps, bool by_count, uint32_t k, double t, bool over, bool index) {
     const int tid = threadIdx.x;
     auto reached = [&](uint32_t n, double m) { return by_count ? n >= k : over ? m > t : m >= t; };
     const int bin = min(tid, BINS - 1);
     const bool holds = tid < BINS && sh.count[bin] > (bin ? sh.count[bin - 1] : 0);
-    int b = first_thread(holds && reached(sh.count[bin], sh.mass[bin]), sh.s.n);
+    int b = steps.first_thread(holds && reached(sh.count[bin], sh.mass[bin]));
     if (b >= BINS) {                                       // the last place
         by_count = true;
         k = sh.count[BINS - 1];
-        b = first_thread(holds && sh.count[bin] >= k, sh.s.n);
+        b = steps.first_thread(holds && sh.count[bin] >= k);
     }
     uint32_t before = b ? sh.count[b - 1] : 0, n = sh.count[b] - before;
     if (by_count && !index && sh.count[b] == k) return Place{k, sh.mass[b], 0.0, -1};
-    const double base = b ? sh.mass[b - 1] : 0.0, unit = exp(-0.0625 * b) * UNIT;
-    uint32_t klo = row.first_key(top - b), khi = row.template first_key<true>(top - b) - 1;
+    const double below = b ? sh.mass[b - 1] : 0.0, unit = bin_weight(b) * UNIT;
+    uint32_t klo = row.template first_key<AT_BIN>(base - b), khi = row.template first_key<ABOVE_BIN>(base - b) - 1;
     uint64_t sum = 0;                                      // of the bin's elements in front of klo .. khi
     while (n > LIST && klo < khi) {
         const uint32_t span = khi - klo, shift = max(0, 22 - (int)__builtin_clz(span)), fine = (span >> shift) + 1;
-        const float lo = value_of(klo), hi = value_of(khi);
+        const float lo = value_of(klo), hi = end_of(khi);
         sh.list[tid] = 0;
         sh.fine[tid] = 0;
         __syncthreads();
-        row.each([&](float v, int) {
+        row.each(lo, [&](float v, int) {
             if (v >= lo && v <= hi) {
-                const uint32_t at = fine - 1 - ((key_of(v) - klo) >> shift);
-                const double z = grid(v, row.c, row.inf);
+                const uint32_t at = fine - 1 - ((key_of(v + 0.f) - klo) >> shift);
+                const double z = row.place(v);
                 atomicAdd(&sh.fine[at], 1u);
-                atomicAdd((unsigned long long *)&sh.list[at], (unsigned long long)weight(z - floor(z)));
+                atomicAdd((unsigned long long *)&sh.list[at], (unsigned long long)weight(z - rint(z)));
             }
         });
         __syncthreads();
         const uint32_t c = sh.fine[tid];
         const uint64_t m = sh.list[tid];
-        const uint32_t cs = before + running_sum(c, sh.s.n);
-        const uint64_t ms = sum + running_sum(m, sh.s.u);
-        int f = first_thread(c && reached(cs, base + unit * (double)ms), sh.s.n);
+        const uint32_t cs = before + steps.running_sum(c);
+        const uint64_t ms = sum + steps.running_sum(m);
+        int f = steps.first_thread(c && reached(cs, below + unit * (double)ms));
         if (f >= LIST) {                                   // sums of the bins and of their parts differ in the last bits
             by_count = true;
             k = before + n;
-            f = first_thread(c && cs >= k, sh.s.n);
+            f = steps.first_thread(c && cs >= k);
         }
         if (tid == f) {
             sh.n = c;
-            sh.s.n[0] = cs - c;
-            sh.s.u[0] = ms - m;
+            sh.at = (int32_t)(cs - c);
+            sh.sum = ms - m;
         }
         __syncthreads();
         n = sh.n;
-        before = sh.s.n[0];
-        sum = sh.s.u[0];
+        before = (uint32_t)sh.at;
+        sum = sh.sum;
         __syncthreads();
         const uint32_t from = klo + ((fine - 1 - (uint32_t)f) << shift);
         khi = min(khi, from + ((1u << shift) - 1));
         klo = from;
     }
     if (n <= LIST) {
-        const uint64_t mine = gather(row, klo, khi, n, sh);
+        gather(row, klo, khi, sh);
+        const uint64_t mine = sorted(n, sh);
         const bool is = (uint32_t)tid < n;
-        const double z = is ? grid(value_of(~(uint32_t)(mine >> 32)), row.c, row.inf) : 0.0;
-        const uint32_t w = is ? weight(z - floor(z)) : 0;
-        const double mass = base + unit * (double)(sum + running_sum((uint64_t)w, sh.s.u));
-        int f = first_thread(is && reached(before + tid + 1, mass), sh.s.n);
+        const double z = is ? row.place(value_of(~(uint32_t)(mine >> 32))) : 0.0;
+        const uint32_t w = is ? weight(z - rint(z)) : 0;
+        const double mass = below + unit * (double)(sum + steps.running_sum((uint64_t)w));
+        int f = steps.first_thread(is && reached(before + tid + 1, mass));
         f = f < LIST ? f : (int)n - 1;
         if (tid == f) {
-            sh.s.d[0] = mass;
-            sh.s.d[1] = unit * w;
+            sh.found[0] = mass;
+            sh.found[1] = unit * w;
             sh.at = (int32_t)(uint32_t)mine;
         }
         __syncthreads();
-        const Place r = {before + (uint32_t)f + 1, sh.s.d[0], sh.s.d[1], sh.at};
+        const Place r = {before + (uint32_t)f + 1, sh.found[0], sh.found[1], sh.at};
         __syncthreads();
         return r;
     }
     // all alike: the place by arithmetic, its index by counting in the order of the row
-    const double z = grid(value_of(klo), row.c, row.inf);
-    const uint32_t w = weight(z - floor(z));
-    auto mass_at = [&](uint32_t i) { return base + unit * (double)(sum + (uint64_t)w * i); };
+    const double z = row.place(value_of(klo));
+    const uint32_t w = weight(z - rint(z));
+    auto mass_at = [&](uint32_t i) { return below + unit * (double)(sum + (uint64_t)w * i); };
     uint32_t lo = 1, hi = n;                               // first i <= n that reaches it, or n
     while (lo < hi) {
         const uint32_t mid = lo + (hi - lo) / 2;
@@ -396,7 +555,7 @@ __device__ Place search(const Row<T> &row, double top, Shared &sh, bool by_count
         uint32_t mine = 0;
 #pragma unroll
         for (int e = 0; e < PER<T>; ++e) mine += logit(v, e) == value;
-        const uint32_t upto = passed + running_sum(mine, sh.s.n);
+        const uint32_t upto = passed + steps.running_sum(mine);
         if (upto >= lo && upto - mine < lo) {
             uint32_t left = lo - (upto - mine);
 #pragma unroll
@@ -417,20 +576,36 @@ __device__ Place search(const Row<T> &row, double top, Shared &sh, bool by_count
 template <typename T>
 __global__ __launch_bounds__(LIST) void sample_row_kernel(SampleParams p) {
     __shared__ Shared sh;
+    Steps steps{sh.meet, 0};
     const int r = blockIdx.x, tid = threadIdx.x;
     bool greedy;
-    Row<T> row = {(const T *)p.logits + r * p.stride, p.vocab, grid_scale(p, r, greedy), false};
+    Row<T> row = {(const T *)p.logits + r * p.stride, p.vocab, grid_scale(p, r, greedy), false, 0.f};
     const uint64_t *chunks = p.chunks + (int64_t)r * p.n_chunks * CHUNK_WORDS;
-    float most = -INFINITY;
-    double top = 0.0;
+    // every wavefront looks at all chunks: the row's maximum, the first chunk that has it, where its bins begin
+    const int lane = tid & 63;
+    uint64_t heads[MOST_CHUNKS / 64][HEADS];
+    float most = -INFINITY, mosts[MOST_CHUNKS / 64];
+#pragma unroll
+    for (int h = 0; h < MOST_CHUNKS / 64; ++h) {
+        const int c = lane + 64 * h;
+        mosts[h] = -INFINITY;
+        for (int k = 0; k < HEADS; ++k) heads[h][k] = 0;
+        if (c < p.n_chunks) {
+            for (int k = 0; k < HEADS; ++k) heads[h][k] = chunks[(int64_t)c * CHUNK_WORDS + k];
+            mosts[h] = __builtin_bit_cast(float, (uint32_t)(heads[h][HEAD_MOST] >> 32));
+        }
+        most = fmaxf(most, mosts[h]);
+    }
+    most = wave_max(most);
+    double base = 0.0;
     int first = 0;
-    for (int c = 0; c < p.n_chunks; ++c) {                 // the first chunk that has the maximum
-        const uint64_t w = chunks[(int64_t)c * CHUNK_WORDS + 1];
-        const float m = __builtin_bit_cast(float, (uint32_t)(w >> 32));
-        if (m > most) {
-            most = m;
-            first = (int)(uint32_t)w;
-            top = __builtin_bit_cast(double, chunks[(int64_t)c * CHUNK_WORDS]);
+#pragma unroll
+    for (int h = MOST_CHUNKS / 64 - 1; h >= 0; --h) {
+        const uint64_t b = __ballot(mosts[h] == most);
+        if (b) {
+            const int from = __builtin_ctzll(b);
+            first = of_lane((int)(uint32_t)heads[h][HEAD_MOST], from);
+            base = of_lane(__builtin_bit_cast(double, heads[h][HEAD_BASE]), from);
         }
     }
     if (greedy || most == -INFINITY) {
@@ -440,25 +615,44 @@ __global__ __launch_bounds__(LIST) void sample_row_kernel(SampleParams p) {
         }
         return;
     }
-    row.inf = most == INFINITY;
+    row.alone = stands_alone(most, row.c);
+    row.most = most;
+    if (row.alone) base = 0.0;
 
     // the chunks' bins, each from its own place on the grid on
+    int downs[MOST_CHUNKS / 64];
+#pragma unroll
+    for (int h = 0; h < MOST_CHUNKS / 64; ++h) {
+        const double down = row.alone ? 0.0 : base - __builtin_bit_cast(double, heads[h][HEAD_BASE]);
+        downs[h] = mosts[h] == -INFINITY || (row.alone && mosts[h] < most) || !(down < (double)BINS) ? BINS : (int)down;
+        if (tid < 64) {
+            sh.down[lane + 64 * h] = downs[h];
+            sh.kept[lane + 64 * h] = downs[h] < BINS ? (uint32_t)heads[h][HEAD_KEPT] : 0u;
+        }
+    }
+    __syncthreads();
     uint32_t count = 0;
     uint64_t mass = 0;
-    if (tid < BINS)
-        for (int c = 0; c < p.n_chunks; ++c) {
-            const uint64_t *w = chunks + (int64_t)c * CHUNK_WORDS;
-            const float m = __builtin_bit_cast(float, (uint32_t)(w[1] >> 32));
-            if (m == -INFINITY || (row.inf && m < INFINITY)) continue;
-            const double down = top - __builtin_bit_cast(double, w[0]);
-            if (!(down <= (double)tid)) continue;
-            const uint64_t bin = w[2 + tid - (int)down];
-            count += (uint32_t)(bin >> COUNT_SHIFT);
-            mass += bin & ((1ull << COUNT_SHIFT) - 1);
+    if (tid < BINS) {
+#pragma unroll 1
+        for (int c0 = 0; c0 < p.n_chunks; c0 += 16) {      // sixteen requests at a time, those that count nothing to a place that exists
+            uint64_t bin[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const int at = tid - sh.down[min(c0 + j, MOST_CHUNKS - 1)];
+                const bool is = c0 + j < p.n_chunks && at >= 0;
+                bin[j] = is ? chunks[(c0 + j) * CHUNK_WORDS + HEADS + at] : 0;
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                count += (uint32_t)(bin[j] >> COUNT_SHIFT);
+                mass += bin[j] & ((1ull << COUNT_SHIFT) - 1);
+            }
         }
-    const double unit = exp(-0.0625 * tid) * UNIT;
-    const uint32_t counts = running_sum(count, sh.s.n);
-    const double masses = running_sum((double)mass * unit, sh.s.d);
+    }
+    const double unit = bin_weight(tid) * UNIT;
+    const uint32_t counts = steps.running_sum(count);
+    const double masses = steps.running_sum((double)mass * unit);
     if (tid < BINS) {
         sh.count[tid] = counts;
         sh.mass[tid] = masses;
@@ -469,7 +663,7 @@ __global__ __launch_bounds__(LIST) void sample_row_kernel(SampleParams p) {
     const int32_t top_k = p.top_k ? p.top_k[r] : 0;
     const float top_p = p.top_p ? p.top_p[r] : 1.f, min_p = p.min_p ? p.min_p[r] : 0.f, u = p.uniform[r];
     const uint32_t k = top_k > 0 ? min((uint32_t)top_k, all) : all;
-    const double least = min_p > 0.f ? grid(most, row.c, row.inf) + 16.0 * log((double)min_p) : -INFINITY;
+    const double least = min_p > 0.f ? row.place(most) + 16.0 * log((double)min_p) : -INFINITY;
     const double uniform = u >= 0.f ? (double)u : 0.0;
 
     uint32_t kept = k;
@@ -478,31 +672,44 @@ __global__ __launch_bounds__(LIST) void sample_row_kernel(SampleParams p) {
         const uint32_t n = tid < BINS ? sh.count[tid] : all;
         const double m = tid < BINS ? sh.mass[tid] : 0.0;
         const bool known = left >= 0.0 || !(top_p < 1.f);  // else all that top_k leaves is needed, for its mass
-        return min(first_thread(n >= kept || (known && ((top_p < 1.f && n && m >= (double)top_p * left) || top - tid <= least)), sh.s.n), BINS - 1);
+        return min(steps.first_thread(n >= kept || (known && ((top_p < 1.f && n && m >= (double)top_p * left) || base - tid - 0.5 < least))), BINS - 1);
     };
     int b = last_bin();
     if (sh.count[b] > LIST && left < 0.0 && top_p < 1.f) {
-        left = search(row, top, sh, true, k, 0.0, false, false).mass;
+        left = search(row, base, sh, steps, true, k, 0.0, false, false).mass;
         b = last_bin();
     }
     const uint32_t n = sh.count[b];
     if (n <= LIST) {
-        const uint64_t mine = gather(row, row.first_key(top - b), KEY_INF, n, sh);
+        bool have = true;                                  // whether the chunks kept all of bins 0 .. b
+#pragma unroll
+        for (int h = 0; h < MOST_CHUNKS / 64; ++h) have &= b - downs[h] <= (int32_t)(heads[h][HEAD_KEPT] >> 32) || b < downs[h];
+        if (__all(have)) {
+            start_list(sh);
+#pragma unroll 1
+            for (int c = tid >> 6; c < p.n_chunks; c += WAVES)
+#pragma unroll 1
+                for (uint32_t e = lane; e < sh.kept[c]; e += 64) {
+                    const uint64_t element = chunks[c * CHUNK_WORDS + HEADS + BINS + e];
+                    if (base - rint(row.place(value_of(~(uint32_t)(element >> 32)))) <= (double)b) put(element, sh);
+                }
+        } else gather(row, row.template first_key<AT_BIN>(base - b), KEY_INF, sh);
+        const uint64_t mine = sorted(n, sh);
         const bool is = (uint32_t)tid < n;
-        const double z = is ? grid(value_of(~(uint32_t)(mine >> 32)), row.c, row.inf) : 0.0, f = floor(z);
-        const double own = is ? exp(-0.0625 * (top - f)) * UNIT * weight(z - f) : 0.0;
-        const double upto = running_sum(own, sh.s.d);
+        const double z = is ? row.place(value_of(~(uint32_t)(mine >> 32))) : 0.0, f = rint(z);
+        const double own = is ? bin_weight(base - f) * UNIT * weight(z - f) : 0.0;
+        const double upto = steps.running_sum(own);
         double *sums = (double *)sh.list;                  // (the list is in registers now)
         sums[tid] = upto;
         __syncthreads();
         kept = min(kept, n);
         if (top_p < 1.f) {
             if (left < 0.0) left = sums[kept - 1];
-            kept = min(kept, (uint32_t)first_thread(is && upto >= (double)top_p * left, sh.s.n) + 1u);
+            kept = min(kept, (uint32_t)steps.first_thread(is && upto >= (double)top_p * left) + 1u);
         }
-        kept = min(kept, max(1u, total_count(is && z >= least, sh.s.n)));
+        kept = min(kept, max(1u, steps.total(is && z >= least)));
         const double mass_kept = sums[kept - 1];
-        const uint32_t at = min((uint32_t)first_thread(is && upto > uniform * mass_kept, sh.s.n), kept - 1);
+        const uint32_t at = min((uint32_t)steps.first_thread(is && upto > uniform * mass_kept), kept - 1);
         if ((uint32_t)tid == at) {
             p.token[r] = (int32_t)(uint32_t)mine;
             if (p.prob) p.prob[r] = (float)(own / mass_kept);
@@ -510,27 +717,27 @@ __global__ __launch_bounds__(LIST) void sample_row_kernel(SampleParams p) {
         return;
     }
     double mass_kept = left;
-    if (k < all && top_p >= 1.f) mass_kept = search(row, top, sh, true, k, 0.0, false, false).mass;
+    if (k < all && top_p >= 1.f) mass_kept = search(row, base, sh, steps, true, k, 0.0, false, false).mass;
     if (top_p < 1.f) {
-        const Place q = search(row, top, sh, false, 0, (double)top_p * left, false, false);
+        const Place q = search(row, base, sh, steps, false, 0, (double)top_p * left, false, false);
         if (q.count < kept) {
             kept = q.count;
             mass_kept = q.mass;
         }
     }
     if (min_p > 0.f) {
-        const float lowest = value_of(min(row.first_key(least), KEY_INF));
+        const float lowest = value_of(min(row.template first_key<AT_PLACE>(least), KEY_INF));
         uint32_t mine = 0;
-        if (least <= grid(most, row.c, row.inf)) row.each([&](float v, int) { mine += v >= lowest; });
-        const uint32_t q = max(1u, total_count(mine, sh.s.n));
+        if (least <= row.place(most)) row.each(lowest, [&](float v, int) { mine += v >= lowest; });
+        const uint32_t q = max(1u, steps.total(mine));
         if (q < kept) {
             kept = q;
-            mass_kept = search(row, top, sh, true, kept, 0.0, false, false).mass;
+            mass_kept = search(row, base, sh, steps, true, kept, 0.0, false, false).mass;
         }
     }
     const double target = uniform * mass_kept;
-    Place q = search(row, top, sh, !(target < mass_kept), kept, target, true, true);
-    if (q.count > kept) q = search(row, top, sh, true, kept, 0.0, false, true);
+    Place q = search(row, base, sh, steps, !(target < mass_kept), kept, target, true, true);
+    if (q.count > kept) q = search(row, base, sh, steps, true, kept, 0.0, false, true);
     if (tid == 0) {
         p.token[r] = q.index;
         if (p.prob) p.prob[r] = (float)(q.own / mass_kept);
@@ -540,10 +747,7 @@ __global__ __launch_bounds__(LIST) void sample_row_kernel(SampleParams p) {
 // Threads of a workgroup of the first pass: small chunks while they are few (latency), larger ones where the bins they write would
 // otherwise weigh as much as the logits
 int bins_threads(int32_t rows, int32_t vocab) { return (int64_t)rows * ((vocab + 8191) / 8192) <= 1024 ? 256 : 1024; }
-int chunks_of(const cascade_sample_desc *d) {
-    const int chunk = chunk_of(bins_threads(d->rows, d->vocab));
-    return (d->vocab + chunk - 1) / chunk;
-}
+int chunks_of(int threads, int32_t vocab) { return (vocab + chunk_of(threads) - 1) / chunk_of(threads); }
 
 int32_t check(const cascade_sample_desc *d) {
     if (!d || d->rows < 0 || d->vocab <= 0 || d->stride < 0 || d->reserved) return CASCADE_EINVAL;
@@ -567,7 +771,8 @@ int32_t launch(const SampleParams &p, int32_t rows, int threads, hipStream_t s) 
 
 extern "C" size_t cascade_sample_workspace_bytes(const cascade_sample_desc *d) {
     if (check(d) != CASCADE_OK) return 0;
-    return (size_t)d->rows * chunks_of(d) * CHUNK_WORDS * 8;
+    const int threads = bins_threads(d->rows, d->vocab);
+    return (size_t)d->rows * chunks_of(threads, d->vocab) * CHUNK_WORDS * 8;
 }
 
 extern "C" int32_t cascade_sample(const cascade_sample_desc *d, const void *logits, const float *temperature, const int32_t *top_k,
@@ -582,8 +787,8 @@ extern "C" int32_t cascade_sample(const cascade_sample_desc *d, const void *logi
     p.logits = logits; p.temperature = temperature; p.top_k = top_k; p.top_p = top_p; p.min_p = min_p; p.uniform = uniform;
     p.token = token; p.prob = prob; p.chunks = (uint64_t *)workspace;
     p.stride = d->stride ? d->stride : d->vocab;
-    p.vocab = d->vocab; p.n_chunks = chunks_of(d);
     const int threads = bins_threads(d->rows, d->vocab);
+    p.vocab = d->vocab; p.n_chunks = chunks_of(threads, d->vocab);
     return d->dtype == CASCADE_BF16 ? launch<bf16_t>(p, d->rows, threads, (hipStream_t)stream)
                                     : launch<float>(p, d->rows, threads, (hipStream_t)stream);
 }

@@ -128,6 +128,21 @@ def test_minus_zero_ties_with_zero(cas):
     run(cas, logits, 0.7, k=2)
 
 
+def test_values_next_to_zero_on_either_side(cas):
+    """Windows of finer bins that end right below zero."""
+    import torch
+    for least in (-1e-40, -1e-45, 1e-45):
+        logits = torch.full((6, 2600), -5.0, device="cuda")
+        logits[:, 100:1300:2] = 0.0
+        logits[:, 101:1301:2] = least
+        logits[3:, 1300:2500] = least
+        logits[:, 120] = -0.0
+        for u in (0.05, 0.2, 0.3, 0.45, 0.6, 0.9):
+            run(cas, logits, u, t=float("inf"))
+            run(cas, logits, u, t=float("inf"), k=700)
+            run(cas, logits, u, t=1e30, p=0.3)
+
+
 @pytest.mark.parametrize("t", [1e-30, 1e-6, 1e-3, 1e30, 1.4e-45, float("nan"), -1.0, 0.0, float("inf")])
 def test_temperatures(cas, t):
     import torch
