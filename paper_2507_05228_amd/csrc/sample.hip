@@ -2,7 +2,7 @@
 //
 // No row is sorted.  All three filters keep a prefix of the row in descending order, and the token is the place where the running
 // sum of the weights passes a target, so everything asked of a row is "at which place does the running count, or the running sum,
-// reach this".  Pass 1 (a workgroup per chunk of a row) puts every logit into one of 704 bins of 1/16 in the exponent, on a grid
+// reach this".  Pass 1 (a workgroup per chunk of a row) puts every logit into one of 1024 bins of 1/24 in the exponent, on a grid
 // that does not depend on the row's maximum, so that the chunks' bins add up; a bin holds how many and the sum of their weights
 // relative to the bin's middle.  Pass 2 (a workgroup per row) adds the chunks, scans the bins, and looks closer where a border falls
 // inside a bin: the bin's elements are gathered from the row and sorted (up to 1024), or counted again in 1024 finer bins of the
@@ -13,9 +13,9 @@
 // One token is the latency of a chain of short steps that each run once: the second pass is written for little code (rolled loops,
 // lane moves, one copy of a step), which its wavefronts fetch from cold caches.
 //
-// Weights are exp(z / 16), z = 16 l / temperature in 64 bits; relative to the middle of the bin, at most a 32nd away, they are whole
+// Weights are exp(z / 24), z = 24 l / temperature in 64 bits; relative to the middle of the bin, at most a 48th away, they are whole
 // numbers of 2^-29, so that sums within a bin are exact and do not depend on any order; the rounding (2^-30 of a weight, either
-// way) is what the result is exact to.  Elements of weight below e^-43 of the largest are left out: 2^20 of them are 2e-13 of the sum.
+// way) is what the result is exact to.  Elements of weight below e^-42 of the largest are left out: 2^20 of them are 6e-13 of the sum.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -27,7 +27,7 @@
 
 namespace {
 
-constexpr int BINS = 704;                                  // 44 in the exponent
+constexpr int BINS = 1024, SCALE = 24;                     // 42.7 in the exponent; one to a thread of the second pass
 constexpr int COUNT_SHIFT = 46;                            // of a bin's word: sum below (2^13 .. 2^15 elements of less than 2^30)
 constexpr int LIST = 1024;                                 // elements that are sorted, and threads of the second pass
 constexpr double UNIT = 0x1p-29;                           // of a weight within its bin
@@ -61,19 +61,20 @@ __device__ __forceinline__ float value_of(uint32_t k) {
 __device__ __forceinline__ float end_of(uint32_t k) { return value_of(k == 0x7fffffffu ? k - 1 : k); }
 constexpr uint32_t KEY_MIN = 0x00800000u, KEY_INF = 0xff800000u;                 // smallest finite value's key, +inf's
 
-// Where a value lies on the grid; c = 16 / temperature.  Its bin is the nearest whole number.  Beside an infinite maximum, or one so
+// Where a value lies on the grid; c = 24 / temperature.  Its bin is the nearest whole number.  Beside an infinite maximum, or one so
 // far out on the grid that fp32 numbers are more than all bins apart, nothing else counts: then the maximum lies at 0.
 __device__ __forceinline__ bool stands_alone(float most, double c) { return most == INFINITY || fabs((double)most * c) >= 0x1p40; }
 __device__ __forceinline__ double grid(float v, double c, bool alone, float most) { return alone ? (v >= most ? 0.0 : -0x1p1000) : (double)v * c; }
-// exp(d / 16) in units of 2^-29, |d| <= 1/2: power series (remainder 2.5e-10 at the ends, an eighth of a unit); the last step adds
+// exp(d / 24) in units of 2^-29, |d| <= 1/2: power series (remainder 3.3e-11 at the ends, a 50th of a unit); the last step adds
 // 1.5 * 2^52, which leaves the rounded whole number in the low word
 constexpr double TO_WHOLE = 0x1.8p52;
 __device__ __forceinline__ uint32_t low_word(double x) { return (uint32_t)__builtin_bit_cast(uint64_t, x); }
 __device__ __forceinline__ uint32_t weight(double d) {
     constexpr double U = 1.0 / UNIT;
-    double e = fma(d, U / (24.0 * 65536), U / (6.0 * 4096));
-    e = fma(e, d, U / (2.0 * 256));
-    e = fma(e, d, U / 16.0);
+    constexpr double S = SCALE;
+    double e = fma(d, U / (24 * S * S * S * S), U / (6 * S * S * S));
+    e = fma(e, d, U / (2 * S * S));
+    e = fma(e, d, U / S);
     return low_word(fma(e, d, U + TO_WHOLE));
 }
 template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Piece { uint32_t w[4]; };
@@ -82,14 +83,6 @@ template <typename T> constexpr int PER = 16 / (int)sizeof(T);                  
 template <typename T> __device__ __forceinline__ float logit(const Piece<T> &p, int e) {
     if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, p.w[e]);
     else return __builtin_bit_cast(float, e & 1 ? p.w[e >> 1] & 0xffff0000u : p.w[e >> 1] << 16);
-}
-// Moves the logits of a piece up by one
-template <typename T> __device__ __forceinline__ void next(Piece<T> &p) {
-    if constexpr (sizeof(T) == 4) {
-        p.w[0] = p.w[1]; p.w[1] = p.w[2]; p.w[2] = p.w[3];
-    } else {
-        p.w[0] = p.w[0] >> 16 | p.w[1] << 16; p.w[1] = p.w[1] >> 16 | p.w[2] << 16; p.w[2] = p.w[2] >> 16 | p.w[3] << 16; p.w[3] >>= 16;
-    }
 }
 // Logits i .. i + PER - 1 of a row of V; past its end -inf.  Whole pieces are requested without a branch.
 template <typename T>
@@ -113,23 +106,10 @@ __device__ __forceinline__ void mend(const T *row, int64_t i, int V, Piece<T> &p
     }
 }
 
-// Whether a piece may hold a value of at least lo > 0: positive numbers order as whole numbers of their bits, negative ones lie below
-template <typename T>
-__device__ __forceinline__ bool may_reach(const Piece<T> &p, float lo) {
-    if constexpr (sizeof(T) == 4) {
-        return max(max((int32_t)p.w[0], (int32_t)p.w[1]), max((int32_t)p.w[2], (int32_t)p.w[3])) >= __builtin_bit_cast(int32_t, lo);
-    } else {
-        typedef __attribute__((ext_vector_type(2))) int16_t i16x2;
-        const auto h = [&](int i) { return __builtin_bit_cast(i16x2, p.w[i]); };
-        const i16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(h(0), h(1)), __builtin_elementwise_max(h(2), h(3)));
-        return max(m[0], m[1]) >= (int16_t)(__builtin_bit_cast(int32_t, lo) >> 16);
-    }
-}
-
 __device__ __forceinline__ double grid_scale(const SampleParams &p, int row, bool &greedy) {
     const float t = p.temperature ? p.temperature[row] : 1.f;
     greedy = !(t > 0.f);
-    return greedy ? 0.0 : 16.0 / (double)t;
+    return greedy ? 0.0 : SCALE / (double)t;
 }
 
 // Running sums over a wavefront by lane moves: inside rows of 16, then the rows' sums
@@ -168,7 +148,7 @@ __device__ __forceinline__ V of_lane(V v, int lane) {      // the same for all l
 constexpr int chunk_of(int threads) { return threads * 32; }
 
 template <typename T, int NT>
-__global__ __launch_bounds__(NT, sizeof(T) == 2 ? 8 : 4) void sample_bins_kernel(SampleParams p) {
+__global__ __launch_bounds__(NT) void sample_bins_kernel(SampleParams p) {
     constexpr int N = 32 / PER<T>, WAVES = NT / 64, MINE = (BINS + NT - 1) / NT;
     __shared__ unsigned long long bins[MINE * NT];
     __shared__ float wave_most[WAVES];
@@ -331,6 +311,9 @@ struct Steps {
 };
 
 enum { AT_PLACE, AT_BIN, ABOVE_BIN };
+struct Run {
+    float lo, hi;
+};
 template <typename T>
 struct Row {
     const T *logits;
@@ -341,32 +324,70 @@ struct Row {
 
     __device__ __forceinline__ double place(float v) const { return grid(v, c, alone, most); }
 
-    // f(value, index) for every logit of at least lo (and some below), pieces of a thread requested eight at a time
-    template <typename F> __device__ __forceinline__ void each(float lo, F f) const {
+    // The thread's pieces, eight requested at a time: f(pieces, index of the first logit, indices from one piece to the next)
+    template <typename F> __device__ __forceinline__ void each_batch(F f) const {
         constexpr int STEP = LIST * PER<T>, N = 8;
         for (int64_t i0 = (int64_t)threadIdx.x * PER<T>; i0 < V; i0 += N * STEP) {
             Piece<T> v[N];
 #pragma unroll
             for (int j = 0; j < N; ++j) v[j] = request(logits, i0 + j * STEP, V);
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const int64_t i = i0 + j * STEP;
-                if (i >= V || (lo > 0.f && V - i >= PER<T> && !may_reach(v[j], lo))) continue;
-                mend(logits, i, V, v[j]);
-#pragma unroll 1
-                for (int e = 0; e < PER<T>; ++e, next(v[j])) f(logit(v[j], 0), (int)(i + e));
-            }
+            for (int j = 0; j < N; ++j) mend(logits, i0 + j * STEP, V, v[j]);
+            f(v, (int)i0, STEP);
         }
+    }
+    // f(value, index) for the logits in any of n runs, which are few: a bit for each one that is, those are then read again
+    template <typename F> __device__ __forceinline__ void each_in(const Run *runs, int n, F f) const {
+        each_batch([&](const Piece<T> (&v)[8], int i0, int step) {
+            uint32_t in[8 * PER<T> / 32] = {};
+#pragma unroll 1
+            for (int r = 0; r < n; ++r) {
+                const float lo = runs[r].lo, hi = runs[r].hi;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int e = 0; e < PER<T>; ++e) {
+                        const float l = logit(v[j], e);
+                        const int bit = j * PER<T> + e;
+                        in[bit >> 5] |= l >= lo && l <= hi ? 1u << (bit & 31) : 0u;
+                    }
+            }
+#pragma unroll
+            for (int w = 0; w < 8 * PER<T> / 32; ++w)
+#pragma unroll 1
+                for (; in[w]; in[w] &= in[w] - 1) {
+                    const int bit = 32 * w + __builtin_ctz(in[w]), i = i0 + bit / PER<T> * step + bit % PER<T>;
+                    f((float)logits[i], i);
+                }
+        });
+    }
+    // f(value, index) for every logit
+    template <typename F> __device__ __forceinline__ void each(F f) const {
+        each_batch([&](const Piece<T> (&v)[8], int i0, int step) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int e = 0; e < PER<T>; ++e) f(logit(v[j], e), i0 + j * step + e);
+        });
+    }
+    template <int WHAT> __device__ __forceinline__ bool reaches(uint32_t key, double z) const {
+        const double at = place(value_of(key));
+        return WHAT == ABOVE_BIN ? rint(at) > z : WHAT == AT_BIN ? rint(at) >= z : at >= z;
     }
     // smallest key whose place on the grid is at least z (AT_BIN: whose bin is at least z, ABOVE_BIN: above z; KEY_INF + 1: none),
     // found by every wavefront for itself
     template <int WHAT>
     __device__ __forceinline__ uint32_t first_key(double z) const {
         uint32_t lo = KEY_MIN, n = KEY_INF + 1 - KEY_MIN;  // the answer is lo .. lo + n
+        const float near = (float)((WHAT == AT_PLACE ? z : WHAT == AT_BIN ? z - 0.5 : z + 0.5) / c);
+        const uint32_t guess = key_of(near);               // usually within a few keys of it: one question instead of six
+        if (!alone && guess > KEY_MIN + 32 && guess < KEY_INF - 32) {
+            const uint64_t b = __ballot(reaches<WHAT>(guess - 32 + (threadIdx.x & 63), z));
+            if (b && !(b & 1)) return guess - 32 + __builtin_ctzll(b);
+        }
         while (n) {
             const uint32_t step = (n + 63) >> 6, at = (threadIdx.x & 63) * step;
-            const double place = this->place(value_of(lo + (at < n ? at : 0)));
-            const bool is = at >= n || (WHAT == ABOVE_BIN ? rint(place) > z : WHAT == AT_BIN ? rint(place) >= z : place >= z);
+            const bool is = at >= n || reaches<WHAT>(lo + (at < n ? at : 0), z);
             const uint64_t b = __ballot(is);
             if (!b) {                                      // behind the last one asked
                 lo += 63 * step + 1;
@@ -383,6 +404,7 @@ struct Row {
     }
 };
 
+constexpr int MOST_RUNS = 4;
 constexpr int MOST_CHUNKS = 128;                           // 2^20 logits in chunks of 8192
 
 struct Shared {
@@ -392,6 +414,16 @@ struct Shared {
     uint32_t count[BINS];
     uint64_t list[LIST];                                   // sorted elements (~key, index), or the sums of finer bins
     uint32_t fine[LIST];                                   // their counts
+    // elements of whole bins, gathered together because borders are expected in them: element, bin, and the running count and sum
+    uint32_t known;                                        // how many
+    bool wanted[BINS];                                     // whose
+    uint64_t known_element[LIST];
+    int32_t known_bin[LIST];
+    uint32_t known_count[LIST];
+    double known_mass[LIST];
+    uint64_t before_sum[BINS];                             // sum and number of the known elements in front of a bin's
+    uint32_t before_count[BINS];
+    Run runs[MOST_RUNS];
     uint32_t n;
     int32_t at;
     double found[2];
@@ -399,28 +431,54 @@ struct Shared {
     Meet meet;
 };
 
+// One exchange of a bitonic sort between lanes O apart
+template <int O>
+__device__ __forceinline__ void exchange(uint64_t &mine, bool keep_low) {
+    uint64_t other;
+    if constexpr (O == 1) other = moved<0xB1, 0xf>(mine);
+    else if constexpr (O == 2) other = moved<0x4E, 0xf>(mine);
+    else if constexpr (O == 4) other = moved<0x1B, 0xf>(moved<0x141, 0xf>(mine));          // 7 - i, then 3 - i
+    else if constexpr (O == 8) other = moved<0x128, 0xf>(mine);
+    else if constexpr (O == 16) {
+        const u32x2 w = __builtin_bit_cast(u32x2, mine);
+        other = __builtin_bit_cast(uint64_t, u32x2{(uint32_t)__builtin_amdgcn_ds_swizzle((int)w[0], 0x401f), (uint32_t)__builtin_amdgcn_ds_swizzle((int)w[1], 0x401f)});
+    } else other = __shfl_xor((unsigned long long)mine, O, WAVE);
+    mine = (mine < other) == keep_low ? mine : other;
+}
+// Exchanges between lanes O, O / 2, .. 1 apart; up: the sequence is to ascend
+template <int O>
+__device__ __forceinline__ void exchanges(uint64_t &mine, bool up) {
+    exchange<O>(mine, ((threadIdx.x & O) == 0) == up);
+    if constexpr (O > 1) exchanges<O / 2>(mine, up);
+}
 // Sorts the n <= LIST elements of the list (the others ~0) and returns the caller's
-__device__ __forceinline__ uint64_t sorted(uint32_t n, Shared &sh) {
+__device__ __attribute__((noinline)) uint64_t sorted(uint32_t n, Shared &sh) {
     const int tid = threadIdx.x;
     __syncthreads();
     uint64_t mine = sh.list[tid];
     uint32_t width = 64;
     while (width < n) width <<= 1;
+    const bool in = (uint32_t)tid < width;                 // of whole wavefronts
+    if (in) {
+        exchanges<1>(mine, !(tid & 2));
+        exchanges<2>(mine, !(tid & 4));
+        exchanges<4>(mine, !(tid & 8));
+        exchanges<8>(mine, !(tid & 16));
+        exchanges<16>(mine, !(tid & 32));
+        exchanges<32>(mine, !(tid & 64));
+    }
 #pragma unroll 1
-    for (uint32_t k = 2; k <= width; k <<= 1)              // bitonic; exchanges inside a wavefront by lane
+    for (uint32_t k = 128; k <= width; k <<= 1) {
 #pragma unroll 1
-        for (uint32_t o = k >> 1; o; o >>= 1) {
-            uint64_t other;
-            if (o < 64) other = __shfl_xor((unsigned long long)mine, (int)o, WAVE);
-            else {
-                __syncthreads();
-                sh.list[tid] = mine;
-                __syncthreads();
-                other = sh.list[tid ^ o];
-            }
-            const bool keep_low = ((tid & o) == 0) == ((tid & k) == 0);
-            mine = (mine < other) == keep_low ? mine : other;
+        for (uint32_t o = k >> 1; o >= 64; o >>= 1) {
+            __syncthreads();
+            sh.list[tid] = mine;
+            __syncthreads();
+            const uint64_t other = sh.list[tid ^ o];
+            mine = (mine < other) == (((tid & o) == 0) == ((tid & k) == 0)) ? mine : other;
         }
+        if (in) exchanges<32>(mine, !(tid & k));
+    }
     __syncthreads();
     return mine;
 }
@@ -436,15 +494,13 @@ __device__ __forceinline__ void put(uint64_t element, Shared &sh) {
 // Gathers the row's elements of keys klo .. khi (at most LIST) into the list
 template <typename T>
 __device__ __attribute__((noinline)) void gather(const Row<T> &row, uint32_t klo, uint32_t khi, Shared &sh) {
-    const float lo = value_of(klo), hi = end_of(khi);
+    if (threadIdx.x == 0) sh.runs[0] = {value_of(klo), end_of(khi)};
     start_list(sh);
-    row.each(lo, [&](float v, int i) {
-        if (v >= lo && v <= hi) put((uint64_t)~key_of(v + 0.f) << 32 | (uint32_t)i, sh);
-    });
+    row.each_in(sh.runs, 1, [&](float v, int i) { put((uint64_t)~key_of(v + 0.f) << 32 | (uint32_t)i, sh); });
 }
-// exp(-b / 16), b >= 0 a whole number: 2 to the whole and the rest, the rest by its power series (1e-15)
+// exp(-b / 24), b >= 0 a whole number: 2 to the whole and the rest, the rest by its power series (1e-15)
 __device__ __forceinline__ double bin_weight(double b) {
-    const double y = b * (-1.4426950408889634074 / 16), i = rint(y), f = (y - i) * 0.693147180559945309417;
+    const double y = b * (-1.4426950408889634074 / SCALE), i = rint(y), f = (y - i) * 0.693147180559945309417;
     double e = 1.0;
 #pragma unroll
     for (int k = 13; k; --k) e = fma(e * f, 1.0 / k, 1.0);
@@ -474,6 +530,14 @@ __device__ __attribute__((noinline)) Place search(const Row<T> &row, double base
     uint32_t before = b ? sh.count[b - 1] : 0, n = sh.count[b] - before;
     if (by_count && !index && sh.count[b] == k) return Place{k, sh.mass[b], 0.0, -1};
     const double below = b ? sh.mass[b - 1] : 0.0, unit = bin_weight(b) * UNIT;
+    if (sh.known && sh.wanted[b]) {
+        const bool mine = (uint32_t)tid < sh.known && sh.known_bin[tid] == b;
+        int f = steps.first_thread(mine && reached(sh.known_count[tid], sh.known_mass[tid]));
+        if (f >= LIST) f = steps.first_thread(mine && sh.known_count[tid] == before + n);
+        const uint64_t e = sh.known_element[f];
+        const double z = row.place(value_of(~(uint32_t)(e >> 32)));
+        return Place{sh.known_count[f], sh.known_mass[f], unit * weight(z - rint(z)), (int32_t)(uint32_t)e};
+    }
     uint32_t klo = row.template first_key<AT_BIN>(base - b), khi = row.template first_key<ABOVE_BIN>(base - b) - 1;
     uint64_t sum = 0;                                      // of the bin's elements in front of klo .. khi
     while (n > LIST && klo < khi) {
@@ -481,15 +545,16 @@ __device__ __attribute__((noinline)) Place search(const Row<T> &row, double base
         const float lo = value_of(klo), hi = end_of(khi);
         sh.list[tid] = 0;
         sh.fine[tid] = 0;
+        if (tid == 0) sh.runs[0] = {lo, hi};
         __syncthreads();
-        row.each(lo, [&](float v, int) {
-            if (v >= lo && v <= hi) {
-                const uint32_t at = fine - 1 - ((key_of(v + 0.f) - klo) >> shift);
-                const double z = row.place(v);
-                atomicAdd(&sh.fine[at], 1u);
-                atomicAdd((unsigned long long *)&sh.list[at], (unsigned long long)weight(z - rint(z)));
-            }
-        });
+        auto add = [&](float v, int) {
+            const uint32_t at = fine - 1 - ((key_of(v + 0.f) - klo) >> shift);
+            const double z = row.place(v);
+            atomicAdd(&sh.fine[at], 1u);
+            atomicAdd((unsigned long long *)&sh.list[at], (unsigned long long)weight(z - rint(z)));
+        };
+        if (n < (uint32_t)row.V / 16) row.each_in(sh.runs, 1, add);
+        else row.each([&](float v, int i) { if (v >= lo && v <= hi) add(v, i); });
         __syncthreads();
         const uint32_t c = sh.fine[tid];
         const uint64_t m = sh.list[tid];
@@ -571,6 +636,47 @@ __device__ __attribute__((noinline)) Place search(const Row<T> &row, double base
     r.index = sh.at;
     __syncthreads();
     return r;
+}
+
+// Gathers the elements of the bins that are wanted (n of them, at most LIST) in one look at the row
+template <typename T>
+__device__ __attribute__((noinline)) void gather_wanted(const Row<T> &row, double base, uint32_t n, Shared &sh, Steps &steps) {
+    const int tid = threadIdx.x;
+    // runs of wanted bins, each found by the wavefront of its number; what is left of them beyond four belongs to the last run
+    const bool is_wanted = tid < BINS && sh.wanted[min(tid, BINS - 1)];
+    const bool begins = is_wanted && (tid == 0 || !sh.wanted[tid - 1]), ends = is_wanted && (tid == BINS - 1 || !sh.wanted[tid + 1]);
+    const uint32_t run = steps.running_sum((uint32_t)begins), n_runs = min(steps.of_last(run), (uint32_t)MOST_RUNS);
+    if (begins && run <= (uint32_t)MOST_RUNS) sh.fine[run - 1] = tid;
+    if (ends) atomicMax(&sh.fine[MOST_RUNS + min(run, (uint32_t)MOST_RUNS) - 1], (uint32_t)tid);
+    __syncthreads();
+    if (const uint32_t w = tid >> 6; w < n_runs) {
+        const float hi = end_of(row.template first_key<ABOVE_BIN>(base - (double)sh.fine[w]) - 1);
+        const float lo = value_of(row.template first_key<AT_BIN>(base - (double)sh.fine[MOST_RUNS + w]));
+        if ((tid & 63) == 0) sh.runs[w] = {lo, hi};
+    }
+    start_list(sh);
+    row.each_in(sh.runs, (int)n_runs, [&](float v, int i) {
+        if (sh.wanted[(int)(base - rint(row.place(v)))]) put((uint64_t)~key_of(v + 0.f) << 32 | (uint32_t)i, sh);
+    });
+    const uint64_t e = sorted(n, sh);
+    const bool is = (uint32_t)tid < n;
+    const double z = is ? row.place(value_of(~(uint32_t)(e >> 32))) : base;
+    const int b = is ? (int)(base - rint(z)) : BINS;
+    const uint64_t w = is ? weight(z - rint(z)) : 0, sum = steps.running_sum(w);
+    sh.known_element[tid] = e;
+    sh.known_bin[tid] = b;
+    __syncthreads();
+    if (is && (tid == 0 || sh.known_bin[tid - 1] != b)) {
+        sh.before_sum[b] = sum - w;
+        sh.before_count[b] = tid;
+    }
+    __syncthreads();
+    if (is) {
+        sh.known_count[tid] = (b ? sh.count[b - 1] : 0) + tid - sh.before_count[b] + 1;
+        sh.known_mass[tid] = (b ? sh.mass[b - 1] : 0.0) + bin_weight(b) * UNIT * (double)(sum - sh.before_sum[b]);
+    }
+    if (tid == 0) sh.known = n;
+    __syncthreads();
 }
 
 template <typename T>
@@ -663,24 +769,55 @@ __global__ __launch_bounds__(LIST) void sample_row_kernel(SampleParams p) {
     const int32_t top_k = p.top_k ? p.top_k[r] : 0;
     const float top_p = p.top_p ? p.top_p[r] : 1.f, min_p = p.min_p ? p.min_p[r] : 0.f, u = p.uniform[r];
     const uint32_t k = top_k > 0 ? min((uint32_t)top_k, all) : all;
-    const double least = min_p > 0.f ? row.place(most) + 16.0 * log((double)min_p) : -INFINITY;
+    const double least = min_p > 0.f ? row.place(most) + SCALE * log((double)min_p) : -INFINITY;
     const double uniform = u >= 0.f ? (double)u : 0.0;
 
+    if (tid == 0) sh.known = 0;
+    const int bin = min(tid, BINS - 1);
+    const uint32_t own_count = tid < BINS ? sh.count[bin] - (bin ? sh.count[bin - 1] : 0) : 0;
+    auto bin_with = [&](bool is) { return min(steps.first_thread(own_count && is), BINS - 1); };     // the first one
+    auto mass_to = [&](int b) { return b ? sh.mass[b - 1] : 0.0; };                                  // of the bins in front
     uint32_t kept = k;
     double left = k < all ? -1.0 : sh.mass[BINS - 1];      // mass of what top_k leaves, as soon as it is known
-    auto last_bin = [&]() {                                // the bin in which the kept ones end at the latest
-        const uint32_t n = tid < BINS ? sh.count[tid] : all;
-        const double m = tid < BINS ? sh.mass[tid] : 0.0;
-        const bool known = left >= 0.0 || !(top_p < 1.f);  // else all that top_k leaves is needed, for its mass
-        return min(steps.first_thread(n >= kept || (known && ((top_p < 1.f && n && m >= (double)top_p * left) || base - tid - 0.5 < least))), BINS - 1);
-    };
-    int b = last_bin();
-    if (sh.count[b] > LIST && left < 0.0 && top_p < 1.f) {
-        left = search(row, base, sh, steps, true, k, 0.0, false, false).mass;
-        b = last_bin();
+    // the bin in which the kept ones end at the latest; as long as the mass that top_k leaves is wanted, all of that
+    const int k_bin = bin_with(sh.count[bin] >= kept);
+    const int least_bin = least > -INFINITY ? (int)fmin(fmax(base - rint(least), 0.0), (double)BINS) : BINS;
+    int b = k_bin;
+    if (left >= 0.0 && top_p < 1.f) b = min(b, bin_with(sh.mass[bin] >= (double)top_p * left));
+    if (left >= 0.0 || !(top_p < 1.f)) b = min(b, least_bin);
+    if (sh.count[b] > LIST) {
+        // The borders that will be looked for, as far as the bins tell: where top_k cuts, where top_p does, where min_p does, where the
+        // token is.  Each cut lies within one bin, so that the masses behind it are known up to that bin's.
+        bool wanted = false;
+        double lo = k < all ? mass_to(k_bin) : left, hi = k < all ? sh.mass[k_bin] : left;
+        int end = k_bin;
+        if (top_p < 1.f) {
+            const int from = bin_with(sh.mass[bin] >= (double)top_p * lo), to = bin_with(sh.mass[bin] >= (double)top_p * hi);
+            wanted |= tid >= from && tid <= to;
+            lo = fmin(lo, mass_to(from));
+            hi = fmin(hi, sh.mass[to]);
+            end = min(end, to);
+        }
+        if (least_bin < BINS) {
+            wanted |= tid == least_bin;
+            lo = fmin(lo, mass_to(least_bin));
+            hi = fmin(hi, sh.mass[least_bin]);
+            end = min(end, least_bin);
+        }
+        const int from = bin_with(sh.mass[bin] > uniform * lo), to = bin_with(sh.mass[bin] > uniform * hi);
+        wanted = (wanted || (tid >= from && tid <= to)) && tid <= end && own_count;
+        wanted |= k < all && sh.count[k_bin] != k && tid == k_bin && (top_p < 1.f || k_bin <= end);
+        if (tid < BINS) sh.wanted[bin] = wanted;
+        if (tid < 2 * MOST_RUNS) sh.fine[tid] = 0;
+        const uint32_t n = steps.total(wanted ? own_count : 0u);
+        if (n && n <= LIST) gather_wanted(row, base, n, sh, steps);
+        if (left < 0.0 && top_p < 1.f) {
+            left = search(row, base, sh, steps, true, k, 0.0, false, false).mass;
+            b = min(min(k_bin, least_bin), bin_with(sh.mass[bin] >= (double)top_p * left));
+        }
     }
     const uint32_t n = sh.count[b];
-    if (n <= LIST) {
+    if (n <= LIST && !sh.known) {
         bool have = true;                                  // whether the chunks kept all of bins 0 .. b
 #pragma unroll
         for (int h = 0; h < MOST_CHUNKS / 64; ++h) have &= b - downs[h] <= (int32_t)(heads[h][HEAD_KEPT] >> 32) || b < downs[h];
@@ -725,10 +862,15 @@ __global__ __launch_bounds__(LIST) void sample_row_kernel(SampleParams p) {
             mass_kept = q.mass;
         }
     }
-    if (min_p > 0.f) {
-        const float lowest = value_of(min(row.template first_key<AT_PLACE>(least), KEY_INF));
+    if (least_bin < BINS) {
         uint32_t mine = 0;
-        if (least <= row.place(most)) row.each(lowest, [&](float v, int) { mine += v >= lowest; });
+        if (sh.known && sh.wanted[least_bin]) {
+            mine = (uint32_t)tid < sh.known && sh.known_bin[tid] == least_bin && row.place(value_of(~(uint32_t)(sh.known_element[tid] >> 32))) >= least;
+            if (tid == 0 && least_bin) mine += sh.count[least_bin - 1];
+        } else if (least <= row.place(most)) {
+            const float lowest = value_of(min(row.template first_key<AT_PLACE>(least), KEY_INF));
+            row.each([&](float v, int) { mine += v >= lowest; });
+        }
         const uint32_t q = max(1u, steps.total(mine));
         if (q < kept) {
             kept = q;
@@ -746,7 +888,7 @@ __global__ __launch_bounds__(LIST) void sample_row_kernel(SampleParams p) {
 
 // Threads of a workgroup of the first pass: small chunks while they are few (latency), larger ones where the bins they write would
 // otherwise weigh as much as the logits
-int bins_threads(int32_t rows, int32_t vocab) { return (int64_t)rows * ((vocab + 8191) / 8192) <= 1024 ? 256 : 1024; }
+int bins_threads(int32_t rows, int32_t vocab) { return (int64_t)rows * ((vocab + 8191) / 8192) <= 1024 ? 256 : 512; }
 int chunks_of(int threads, int32_t vocab) { return (vocab + chunk_of(threads) - 1) / chunk_of(threads); }
 
 int32_t check(const cascade_sample_desc *d) {
@@ -761,7 +903,7 @@ template <typename T>
 int32_t launch(const SampleParams &p, int32_t rows, int threads, hipStream_t s) {
     const dim3 grid((unsigned)(rows * p.n_chunks));
     if (threads == 256) hipLaunchKernelGGL((sample_bins_kernel<T, 256>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((sample_bins_kernel<T, 1024>), grid, dim3(1024), 0, s, p);
+    else hipLaunchKernelGGL((sample_bins_kernel<T, 512>), grid, dim3(512), 0, s, p);
     hipLaunchKernelGGL(sample_row_kernel<T>, dim3(rows), dim3(LIST), 0, s, p);
     CASCADE_HIP_TRY(hipGetLastError());
     return CASCADE_OK;
