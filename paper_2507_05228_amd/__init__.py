@@ -128,15 +128,18 @@ class LayerWeights(C.Structure):
 
 
 _lib = None
+_torch, _Q8 = None, {}                                     # torch, and its 8-bit types' formats, as soon as the library is loaded
+_CODES = {}                                                # of torch's types
 
 
 def load_library():
     """dlopen libcascade.so and declare the signatures.  Raises if it was not built."""
-    global _lib
+    global _lib, _torch, _Q8
     if _lib is not None:
         return _lib
     try:
-        import torch  # noqa: F401  (its HIP runtime must be the one this process initialises first)
+        import torch              # (its HIP runtime must be the one this process initialises first)
+        _torch, _Q8 = torch, {torch.int8: Q8_INT8, torch.float8_e4m3fn: Q8_E4M3}
     except ImportError:
         pass
     if not os.path.exists(LIB_PATH):
@@ -250,12 +253,13 @@ def _stream(stream):
 
 
 def _dtype_code(t):
-    import torch
-    if t.dtype == torch.bfloat16:
-        return BF16
-    if t.dtype == torch.float32:
-        return F32
-    raise CascadeError(EUNSUPPORTED, f"dtype {t.dtype}")
+    if not _CODES:
+        import torch
+        _CODES.update({torch.bfloat16: BF16, torch.float32: F32})
+    code = _CODES.get(t.dtype)
+    if code is None:
+        raise CascadeError(EUNSUPPORTED, f"dtype {t.dtype}")
+    return code
 
 
 class Plan:
@@ -799,44 +803,86 @@ def cascade_pages_copy(cache, src, dst, stream=None):
 
 
 # ------------------------------------------------------------------ a token's step around its attention
-def _dense_rows(t, where, what):
-    """Row stride of a [rows, columns] tensor on the GPU whose rows do not overlap (None: 0)."""
+def _operand(t, shape, dtype, device, where, what):
+    """(address, row stride) of a [rows, columns] tensor of this shape and type on this device, its columns dense, its rows at any
+    stride that keeps them apart (0: dense).  None: (None, 0)."""
     if t is None:
-        return 0
-    if t.dim() == 2:
-        (rows, cols), (sr, sc) = t.shape, t.stride()
-        if t.is_cuda and (sc == 1 or cols == 1) and (rows < 2 or sr >= cols):
-            return sr if rows > 1 else cols
-    raise CascadeError(ESHAPE, f"{where}: {what} [rows, columns], columns dense, rows that do not overlap, on the GPU")
+        return None, 0
+    if t.dtype == dtype and t.shape == shape:
+        if t.get_device() != device:
+            raise CascadeError(EINVAL if t.is_cuda else ESHAPE, f"{where}: {what} on device {t.device}, the current device is {device}")
+        if t.is_contiguous():
+            return t.data_ptr(), 0
+        if t.stride(1) == 1 and (shape[0] < 2 or t.stride(0) >= shape[1]):
+            return t.data_ptr(), t.stride(0) if shape[0] > 1 else 0
+    raise CascadeError(ESHAPE, f"{where}: {what} {dtype} {tuple(shape)}, columns dense, rows that do not overlap; given {t.dtype} {tuple(t.shape)}")
 
 
-def _q8_format(t):
-    import torch
-    return {torch.int8: Q8_INT8, torch.float8_e4m3fn: Q8_E4M3}.get(t.dtype, Q8_NONE)
+def _vector(t, n, dtype, device, where, what):
+    """Address of a contiguous tensor of n values of this type on this device.  None: None."""
+    if t is None:
+        return None
+    if not (t.dtype == dtype and t.numel() == n and t.is_contiguous()):
+        raise CascadeError(ESHAPE, f"{where}: {what} {dtype}, {n} values, contiguous; given {t.dtype} {tuple(t.shape)}")
+    if t.get_device() != device:
+        raise CascadeError(EINVAL if t.is_cuda else ESHAPE, f"{where}: {what} on device {t.device}, the current device is {device}")
+    return t.data_ptr()
+
+
+def _device_of(x, where):
+    """The current device; x [rows, columns] decides whether there is one."""
+    if x.dim() != 2 or not x.is_cuda:
+        raise CascadeError(ESHAPE, f"{where}: [rows, columns] on the GPU")
+    return _torch.cuda.current_device()
+
+
+def _handle(stream, device):
+    if stream is None:
+        return _torch._C._cuda_getCurrentRawStream(device)
+    if getattr(stream, "device_index", device) != device:
+        raise CascadeError(EINVAL, f"a stream of device {stream.device_index}, the current device is {device}")
+    return stream.cuda_stream
+
+
+def _workspace(workspace, device, where):
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != device or not workspace.is_contiguous():
+        raise CascadeError(EWORKSPACE, f"{where}: a contiguous workspace on the current device")
+    return workspace.data_ptr(), workspace.nbytes
+
+
+def _scale_groups(scale, rows, columns, where):
+    """How many scales a row has: scale [rows] or [rows, groups]."""
+    groups = 1 if scale.dim() == 1 else scale.shape[1] if scale.dim() == 2 else 0
+    if groups <= 0 or columns % groups or scale.shape[0] != rows:
+        raise CascadeError(ESHAPE, f"{where}: scales [rows] or [rows, groups], whole groups")
+    return groups
 
 
 def cascade_add_norm(x, gain, norm_kind, eps, delta=None, bias=None, sum=None, y=None, q=None, q_scale=None, stream=None):
     """x, delta, sum, y [rows, D] of one type, gain, bias [D]; q [rows, D] int8 or float8_e4m3fn with q_scale fp32 [rows] or
     [rows, D / group] (group 32, 64, 128 or 256).  One of sum, y, q is wanted; sum and y may be x or delta."""
-    import torch
-    lib = load_library()
-    where = "cascade_add_norm"
-    _checked(where, x.dtype, gain, bias)
-    _checked(where, torch.float32, q_scale)
-    strides = [_dense_rows(t, where, n) for t, n in ((x, "x"), (delta, "delta"), (sum, "sum"), (y, "y"), (q, "q"))]
-    rows, D = x.shape
-    _counted(where, (all(t is None or (t.shape == x.shape and t.dtype == x.dtype) for t in (delta, sum, y)), "delta, sum and y like x"),
-             (gain.numel() == D and (bias is None or bias.numel() == D), "gain, bias [D]"), ((q is None) == (q_scale is None), "q with q_scale"))
+    lib, where = _lib or load_library(), "cascade_add_norm"
+    device, dtype, shape = _device_of(x, where), x.dtype, x.shape
+    rows, D = shape
     fmt = group = 0
-    if q is not None:
-        fmt, groups = _q8_format(q), q_scale.numel() // max(rows, 1)
-        _counted(where, (fmt != Q8_NONE and q.shape == x.shape, "q int8 or float8_e4m3fn, like x"),
-                 (rows == 0 or (q_scale.numel() == rows * groups and groups > 0 and D % groups == 0), "q_scale [rows, D / group]"))
+    if q is not None or q_scale is not None:
+        if q is None or q_scale is None or q.dtype not in _Q8:
+            raise CascadeError(ESHAPE, f"{where}: q int8 or float8_e4m3fn, with q_scale")
+        fmt, groups = _Q8[q.dtype], _scale_groups(q_scale, rows, D, where)
         group = D // groups if groups > 1 else 0
-    desc = AddNormDesc(_dtype_code(x), rows, D, norm_kind, eps, fmt, group, *strides)
-    st = lib.cascade_add_norm(C.byref(desc), _at(x), _at(delta), _at(gain), _at(bias), _at(sum), _at(y), _at(q), _at(q_scale),
-                              _on(stream, x, delta, gain, bias, sum, y, q, q_scale))
-    _check(st, where)
+    x_at, sx = _operand(x, shape, dtype, device, where, "x")
+    delta_at, sd = _operand(delta, shape, dtype, device, where, "delta")
+    sum_at, ss = _operand(sum, shape, dtype, device, where, "sum")
+    y_at, sy = _operand(y, shape, dtype, device, where, "y")
+    q_at, sq = _operand(q, shape, q.dtype, device, where, "q") if fmt else (None, 0)
+    desc = AddNormDesc(_dtype_code(x), rows, D, norm_kind, eps, fmt, group, sx, sd, ss, sy, sq)
+    st = lib.cascade_add_norm(C.byref(desc), x_at, delta_at, _vector(gain, D, dtype, device, where, "gain"), _vector(bias, D, dtype, device, where, "bias"),
+                              sum_at, y_at, q_at, _vector(q_scale, rows * groups, _torch.float32, device, where, "q_scale") if fmt else None,
+                              _handle(stream, device))
+    if st:
+        raise CascadeError(st, where)
 
 
 def make_w4_weights(codes, scales, zeros=None):
@@ -861,40 +907,35 @@ def make_w4_weights(codes, scales, zeros=None):
     return w
 
 
-def _w4_gemm_desc(weights, x, x_scale, epilogue, strides):
-    fmt = _q8_format(x)
-    if fmt == Q8_NONE:
-        _counted("cascade_w4_gemm", (_dtype_code(x) == weights.dtype, "x in the weights' type, int8 or float8_e4m3fn"))
-    groups = 1 if x_scale is None else x_scale.numel() // max(x.shape[0], 1)
-    _counted("cascade_w4_gemm", (x.dim() == 2 and x.shape[1] == weights.k, "x [rows, k]"), ((x_scale is None) == (fmt == Q8_NONE), "x_scale with 8-bit x"),
-             (x_scale is None or (x_scale.numel() == x.shape[0] * groups and groups > 0 and weights.k % groups == 0) or x.shape[0] == 0, "x_scale [rows, k / group]"))
-    return W4GemmDesc(x.shape[0], fmt, weights.k // groups if groups > 1 else 0, epilogue, *strides)
-
-
 def cascade_w4_gemm_workspace_bytes(weights, x, weights_up=None):
     """For x as it will be given; weights_up: with EPI_SWIGLU."""
-    desc = W4GemmDesc(x.shape[0], _q8_format(x), 0, EPI_SWIGLU if weights_up is not None else 0, 0, 0, 0)
+    desc = W4GemmDesc(x.shape[0], _Q8.get(x.dtype, Q8_NONE), 0, EPI_SWIGLU if weights_up is not None else 0, 0, 0, 0)
     return load_library().cascade_w4_gemm_workspace_bytes(C.byref(weights), C.byref(desc))
 
 
 def cascade_w4_gemm(weights, x, y, x_scale=None, weights_up=None, bias=None, residual=None, epilogue=0, workspace=None, stream=None):
     """y, residual [rows, n_out] and bias [n_out] in the weights' type; x [rows, k] likewise, or int8 / float8_e4m3fn with x_scale
     fp32 [rows] or [rows, k / group]."""
-    import torch
-    lib = load_library()
-    where = "cascade_w4_gemm"
-    strides = [_dense_rows(t, where, n) for t, n in ((x, "x"), (residual, "residual"), (y, "y"))]
-    desc = _w4_gemm_desc(weights, x, x_scale, epilogue, strides)
-    _checked(where, torch.float32, x_scale)
-    _checked(where, y.dtype, bias)
-    _counted(where, (_dtype_code(y) == weights.dtype and y.shape == (x.shape[0], weights.n_out), "y [rows, n_out] in the weights' type"),
-             (residual is None or (residual.shape == y.shape and residual.dtype == y.dtype), "residual like y"),
-             (bias is None or bias.numel() == weights.n_out, "bias [n_out]"))
-    ws, ws_bytes = _room(workspace, where)
-    st = lib.cascade_w4_gemm(C.byref(weights), None if weights_up is None else C.byref(weights_up), C.byref(desc), _at(x), _at(x_scale),
-                             _at(bias), _at(residual), _at(y), ws, ws_bytes,
-                             _on(stream, x, y, x_scale, bias, residual, workspace, weights.tensors[0], weights_up and weights_up.tensors[0]))
-    _check(st, where)
+    lib, where = _lib or load_library(), "cascade_w4_gemm"
+    device, dtype, n = _device_of(x, where), _torch.float32 if weights.dtype == F32 else _torch.bfloat16, weights.n_out
+    rows, fmt, groups, scale_at = x.shape[0], _Q8.get(x.dtype, Q8_NONE), 1, None
+    if x_scale is not None or fmt:
+        if x_scale is None or not fmt:
+            raise CascadeError(ESHAPE, f"{where}: x_scale with int8 or float8_e4m3fn x")
+        groups = _scale_groups(x_scale, rows, weights.k, where)
+        scale_at = _vector(x_scale, rows * groups, _torch.float32, device, where, "x_scale")
+    x_at, sx = _operand(x, (rows, weights.k), x.dtype if fmt else dtype, device, where, "x")
+    res_at, sr = _operand(residual, (rows, n), dtype, device, where, "residual")
+    y_at, sy = _operand(y, (rows, n), dtype, device, where, "y")
+    for w in (weights, weights_up):
+        if w is not None and w.tensors[0] is not None and w.tensors[0].get_device() != device:
+            raise CascadeError(EINVAL, f"{where}: weights on device {w.tensors[0].get_device()}, the current device is {device}")
+    ws, ws_bytes = _workspace(workspace, device, where)
+    desc = W4GemmDesc(rows, fmt, weights.k // groups if groups > 1 else 0, epilogue, sx, sr, sy)
+    st = lib.cascade_w4_gemm(C.byref(weights), None if weights_up is None else C.byref(weights_up), C.byref(desc), x_at, scale_at,
+                             _vector(bias, n, dtype, device, where, "bias"), res_at, y_at, ws, ws_bytes, _handle(stream, device))
+    if st:
+        raise CascadeError(st, where)
 
 
 def cascade_sample_workspace_bytes(rows, vocab, dtype):
@@ -906,19 +947,20 @@ def cascade_sample_workspace_bytes(rows, vocab, dtype):
 
 def cascade_sample(logits, uniform, token, temperature=None, top_k=None, top_p=None, min_p=None, prob=None, workspace=None, stream=None):
     """logits [rows, vocab]; uniform, temperature, top_p, min_p, prob fp32 [rows], top_k, token int32 [rows] (None: off, or not wanted)."""
-    import torch
-    lib = load_library()
-    where = "cascade_sample"
-    stride = _dense_rows(logits, where, "logits")
-    _checked(where, torch.float32, uniform, temperature, top_p, min_p, prob)
-    _checked(where, torch.int32, token, top_k)
+    lib, where = _lib or load_library(), "cascade_sample"
+    device = _device_of(logits, where)
     rows, vocab = logits.shape
-    _counted(where, (all(t is None or t.numel() == rows for t in (uniform, token, temperature, top_k, top_p, min_p, prob)), "one value a row"))
+    f32, i32 = _torch.float32, _torch.int32
+    l_at, stride = _operand(logits, logits.shape, logits.dtype, device, where, "logits")
+    ws, ws_bytes = _workspace(workspace, device, where)
     desc = SampleDesc(_dtype_code(logits), rows, vocab, 0, stride)
-    ws, ws_bytes = _room(workspace, where)
-    st = lib.cascade_sample(C.byref(desc), _at(logits), _at(temperature), _at(top_k), _at(top_p), _at(min_p), _at(uniform), _at(token), _at(prob),
-                            ws, ws_bytes, _on(stream, logits, uniform, token, temperature, top_k, top_p, min_p, prob, workspace))
-    _check(st, where)
+    st = lib.cascade_sample(C.byref(desc), l_at, _vector(temperature, rows, f32, device, where, "temperature"),
+                            _vector(top_k, rows, i32, device, where, "top_k"), _vector(top_p, rows, f32, device, where, "top_p"),
+                            _vector(min_p, rows, f32, device, where, "min_p"), _vector(uniform, rows, f32, device, where, "uniform"),
+                            _vector(token, rows, i32, device, where, "token"), _vector(prob, rows, f32, device, where, "prob"),
+                            ws, ws_bytes, _handle(stream, device))
+    if st:
+        raise CascadeError(st, where)
 
 
 def cascade_mfma_ceiling(lds_operands, iters=200000, stream=None):
