@@ -9,9 +9,9 @@
 // reduction.  In a block, lane (column l, quarter g) of a wavefront finds its 16 bytes at (16 g + l) * 16: word s holds elements
 // 32 s + 8 g .. + 7, which is the operand of one 16x16x32 product, and in a word nibble p < 4 holds element 2p, nibble p + 4
 // element 2p + 1.  So two nibbles 16 bits apart become a pair of bf16 numbers by a shift, a mask and an or: 0x4180 | code << 3 is
-// 16 + code.  What that adds, and the zero points, come off once per group: scale * (sum x (16 + code) - (16 + zero) * sum x), with
-// the sums of X formed where it enters LDS.  INT8 rows take codes as bytes (three operations for 8), all in whole numbers
-// up to the scales.  Behind the codes: scales and zeros, [column blocks][groups][16].
+// 16 + code.  What that adds, and the zero points, come off once per group: scale * (sum x (16 + code) - (16 + zero) * sum x), where
+// the sums of X come from one more product per step, with ones, for all columns of the wavefront.  INT8 rows take codes as bytes
+// (three operations for 8), all in whole numbers up to the scales.  Behind the codes: scales and zeros, [column blocks][groups][16].
 #include <algorithm>
 #include <type_traits>
 #include "common.h"
@@ -38,7 +38,6 @@ struct W4Params {
     int64_t ldx, ldres, ldy;                               // elements
     int32_t M, N, K;
     int32_t blocks, groups;                                // of the reduction
-    int32_t fold;                                          // 32-element steps that share all scales: 1, 2 or 4
     int32_t group_shift, x_group_shift, x_groups;          // log2 of the elements of a scale (x_group_shift 31: the row)
     int32_t has_zeros, flags;
     int32_t cols_log2;                                     // column groups of a workgroup; 8 >> cols_log2 parts of the reduction
@@ -51,7 +50,7 @@ template <int XT> constexpr int unit_bytes() { return XT == X_F32 ? 48 : XT == X
 constexpr int MAX_UNITS = 4;                               // of a thread and chunk: chunk * rows * 16 / 512
 
 // 8 columns of X as they came, and in LDS: bf16 numbers (three sets of them for fp32, which add up to it exactly), or bytes in the
-// order of the codes' bytes.  Returns their sum.
+// order of the codes' bytes
 template <int XT> struct XRaw { u32x4 v; };
 template <> struct XRaw<X_F32> { u32x4 v, w; };
 template <> struct XRaw<X_E4M3> { u32x2 v; };
@@ -65,40 +64,33 @@ __device__ __forceinline__ XRaw<XT> load_x(__amdgpu_buffer_rsrc_t r, uint32_t of
     return x;
 }
 template <int XT>
-__device__ __forceinline__ float store_x(const XRaw<XT> &x, char *to) {
+__device__ __forceinline__ void store_x(const XRaw<XT> &x, char *to) {
     if constexpr (XT == X_INT8) {
         *(u32x2 *)to = u32x2{__builtin_amdgcn_perm(x.v[1], x.v[0], 0x05010400u), __builtin_amdgcn_perm(x.v[1], x.v[0], 0x07030602u)};
-        return (float)__builtin_amdgcn_sdot4(x.v[0], 0x01010101, __builtin_amdgcn_sdot4(x.v[1], 0x01010101, 0, false), false);
+    } else if constexpr (XT == X_BF16) {
+        *(u32x4 *)to = x.v;
     } else {
         float f[8];
         if constexpr (XT == X_F32) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[e] = __builtin_bit_cast(float, e < 4 ? x.v[e] : x.w[e - 4]);
-        } else if constexpr (XT == X_E4M3) {
+        } else {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(x.v[h], false), b = __builtin_amdgcn_cvt_pk_f32_fp8(x.v[h], true);
                 f[4 * h] = a[0]; f[4 * h + 1] = a[1]; f[4 * h + 2] = b[0]; f[4 * h + 3] = b[1];
             }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = __builtin_bit_cast(float, e & 1 ? x.v[e >> 1] & 0xffff0000u : x.v[e >> 1] << 16);
         }
-        const float sum = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
-        if constexpr (XT == X_BF16) *(u32x4 *)to = x.v;
-        else {
 #pragma unroll
-            for (int i = 0; i < (XT == X_F32 ? 3 : 1); ++i) {
-                bf16x8 v;
+        for (int i = 0; i < (XT == X_F32 ? 3 : 1); ++i) {
+            bf16x8 v;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    v[e] = (bf16_t)f[e];
-                    f[e] -= (float)v[e];
-                }
-                *(bf16x8 *)(to + 16 * i) = v;
+            for (int e = 0; e < 8; ++e) {
+                v[e] = (bf16_t)f[e];
+                f[e] -= (float)v[e];
             }
+            *(bf16x8 *)(to + 16 * i) = v;
         }
-        return sum;
     }
 }
 
@@ -114,6 +106,51 @@ __device__ __forceinline__ int64_t codes_int8(uint32_t w) {
 }
 
 template <int XT> using Sum = typename std::conditional<XT == X_INT8, i32x4, f32x4>::type;
+// 8 columns of X as an operand (three of them for fp32)
+template <int XT> struct XOperand { bf16x8 v[XT == X_F32 ? 3 : 1]; };
+template <> struct XOperand<X_INT8> { int64_t v; };
+template <int XT>
+__device__ __forceinline__ XOperand<XT> operand(const char *x) {
+    XOperand<XT> o;
+    if constexpr (XT == X_INT8) o.v = *(const int64_t *)x;
+    else {
+#pragma unroll
+        for (int l = 0; l < (XT == X_F32 ? 3 : 1); ++l) o.v[l] = *(const bf16x8 *)(x + 16 * l);
+    }
+    return o;
+}
+// The operands of a step's codes, and of ones
+template <int XT> using WOperand = typename std::conditional<XT == X_INT8, int64_t, bf16x8>::type;
+template <int XT>
+__device__ __forceinline__ WOperand<XT> codes(uint32_t w) {
+    if constexpr (XT == X_INT8) return codes_int8(w);
+    else return codes_bf16(w);
+}
+template <int XT>
+__device__ __forceinline__ WOperand<XT> ones_operand() {
+    if constexpr (XT == X_INT8) return 0x0101010101010101ll;
+    else return __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+}
+// acc + x w over STEPS steps.  Two steps of bytes go into one 16x16x64 product, which has twice the rate of 16x16x32; in which order
+// a lane's 16 elements stand is free, as long as it is the same on both sides.
+template <int XT, int STEPS, int STRIDE>
+__device__ __forceinline__ Sum<XT> product(const XOperand<XT> *x, const WOperand<XT> *w, Sum<XT> acc) {
+    if constexpr (XT == X_INT8 && STEPS > 1) {
+        typedef __attribute__((ext_vector_type(2))) int64_t i64x2;
+#pragma unroll
+        for (int s = 0; s < STEPS; s += 2)
+            acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, i64x2{x[s * STRIDE].v, x[(s + 1) * STRIDE].v}),
+                                                        __builtin_bit_cast(i32x4, i64x2{w[s], w[s + 1]}), acc, 0, 0, 0);
+    } else if constexpr (XT == X_INT8) {
+        acc = __builtin_amdgcn_mfma_i32_16x16x32_i8(x[0].v, w[0], acc, 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+            for (int l = 0; l < (XT == X_F32 ? 3 : 1); ++l) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[s * STRIDE].v[l], w[s], acc, 0, 0, 0);
+    }
+    return acc;
+}
 
 // One output from the formula, term by term.  The products above give NaN where a row holds an infinity (16 + code and
 // 16 + zero meet it with opposite signs), and fp32 values next to the largest leave the range of the first of their parts.
@@ -161,9 +198,10 @@ __device__ __forceinline__ void finish(const W4Params &p, float (&v)[2], int row
 }
 
 // TM: 16-row blocks.  TN: 16-column blocks of a wavefront (SWIGLU: gate and up of the same columns).
+// FOLD: 32-element steps that share all scales, 1, 2 or 4.
 // WHOLE: the slice's X fits into LDS and enters it once; else it comes in chunks of two pieces a wavefront, into halves in turn.
 // F32: scales, bias, residual and Y in fp32, else bf16.
-template <int XT, bool F32, int TM, int TN, bool SWIGLU, bool WHOLE>
+template <int XT, bool F32, int TM, int TN, bool SWIGLU, int FOLD, bool WHOLE>
 __global__ __launch_bounds__(NW * 64, TM == 1 && WHOLE ? 4 : 2) void w4_kernel(W4Params p) {
     static_assert(!SWIGLU || TN == 2, "gate and up");
     typedef typename std::conditional<F32, float, bf16_t>::type T;
@@ -175,22 +213,25 @@ __global__ __launch_bounds__(NW * 64, TM == 1 && WHOLE ? 4 : 2) void w4_kernel(W
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int cols = 1 << p.cols_log2, parts = NW >> p.cols_log2, cg = wave & (cols - 1), part = wave >> p.cols_log2;
     const int row0 = blockIdx.z * (TM * 16), rows = min(p.M - row0, TM * 16);
-    const int tile0 = blockIdx.x * cols * TNO, block0 = tile0 + cg * TNO;        // 16-column blocks: of the workgroup, of the wavefront
-    const int all_blocks = (p.N + 15) / 16, n_blocks = max(0, min(all_blocks - block0, TNO));
+    const int tile0 = blockIdx.x * cols * TNO;             // 16-column blocks: of the workgroup,
+    // of the wavefront, and how many there are.  Those behind the last column read the first block, or the one beside them, instead, and are
+    // not stored: whatever a range check makes of scalar offsets, they stay inside the weights.
+    const int left_blocks = (p.N + 15) / 16 - tile0 - cg * TNO, block0 = __builtin_amdgcn_readfirstlane(left_blocks > 0 ? tile0 + cg * TNO : 0);
+    const int n_blocks = __builtin_amdgcn_readfirstlane(left_blocks > 0 ? min(left_blocks, TNO) : 1);
     const int first = blockIdx.y * p.slice_blocks, n_pieces = min(p.blocks - first, p.slice_blocks);
 
-    // LDS: chunks of X, the sums and scales of its 32-column steps
+    // LDS: chunks of X, and the scales of its 32-column steps where there are several
     const int row_units = rows | 1;                        // odd: neighbouring units of a row lie in different banks
-    const int chunk_bytes = p.chunk * 16 * row_units * UB, chunk_sums = p.chunk * 4 * TM * 16;
-    float *sums = (float *)(lds + p.chunks_held * chunk_bytes), *xscales = sums + p.chunks_held * chunk_sums;
+    const int chunk_bytes = p.chunk * 16 * row_units * UB, chunk_scales = p.chunk * 4 * TM * 16;
+    float *xscales = (float *)(lds + p.chunks_held * chunk_bytes);
 
     __amdgpu_buffer_rsrc_t rw[MATS], rs[MATS], rz[MATS];
 #pragma unroll
     for (int i = 0; i < MATS; ++i) {
-        const int64_t at = n_blocks ? block0 : 0, entries = at * p.groups * 16;
+        const int64_t at = block0, entries = at * p.groups * 16;
         rw[i] = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p.codes[i]) + at * p.blocks * 1024, 0, (uint32_t)(n_blocks * p.blocks) * 1024u, 0x00020000);
         rs[i] = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p.scales[i]) + entries * sizeof(T), 0, (uint32_t)(n_blocks * p.groups * 16 * sizeof(T)), 0x00020000);
-        rz[i] = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p.zeros[i]) + entries, 0, p.has_zeros ? (uint32_t)(n_blocks * p.groups * 16) : 0u, 0x00020000);
+        rz[i] = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p.zeros[i]) + entries, 0, (uint32_t)(n_blocks * p.groups * 16), 0x00020000);
     }
     const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<char *>(p.X) + row0 * p.ldx * x_bytes<XT>(), 0, (uint32_t)(((rows - 1) * p.ldx + p.K) * x_bytes<XT>()), 0x00020000);
@@ -219,17 +260,12 @@ __global__ __launch_bounds__(NW * 64, TM == 1 && WHOLE ? 4 : 2) void w4_kernel(W
         return load_x<XT>(rx, is && q < n_pieces && col < p.K ? (uint32_t)(row * p.ldx + col) * x_bytes<XT>() : OUT_OF_RANGE);
     };
     auto store_unit = [&](int chunk, int held, int piece, int row, bool is, const XRaw<XT> &x) {
-        float sum = 0.f;
-        if (is) sum = store_x<XT>(x, lds + held * chunk_bytes + ((piece * 16 + sg) * row_units + row) * UB);
-        sum += dpp_row_move<0xB1>(sum);
-        sum += dpp_row_move<0x4E>(sum);
-        if (!is || (sg & 3)) return;
-        const int at = held * chunk_sums + (piece * 4 + (sg >> 2)) * (TM * 16) + row;
-        sums[at] = sum;
-        if (X8 && p.x_groups > 1) {
+        if (!is) return;
+        store_x<XT>(x, lds + held * chunk_bytes + ((piece * 16 + sg) * row_units + row) * UB);
+        if (X8 && p.x_groups > 1 && (sg & 3) == 0) {
             const int q = chunk * p.chunk + piece, col = (first + q) * BLOCK + 8 * sg;
             const uint32_t o = q < n_pieces && col < p.K ? (uint32_t)(row * p.x_groups + (col >> p.x_group_shift)) * 4u : OUT_OF_RANGE;
-            xscales[at] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rxs, o, 0, 0));
+            xscales[held * chunk_scales + (piece * 4 + (sg >> 2)) * (TM * 16) + row] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rxs, o, 0, 0));
         }
     };
 
@@ -237,20 +273,23 @@ __global__ __launch_bounds__(NW * 64, TM == 1 && WHOLE ? 4 : 2) void w4_kernel(W
         u32x4 w[TN];
         uint32_t scale[TN], zero[TN];                      // of the fold that this lane's quarter stands for
     } ring[D];
-    const int fold_log2 = __builtin_ctz(p.fold), folds = 4 >> fold_log2;         // folds of a piece
+    constexpr int FOLDS = 4 / FOLD;                        // of a piece
     const int my_pieces = (n_pieces - part + parts - 1) / parts;
+    // Offsets of the lanes; those of a piece are scalars.  A lane whose fold lies behind the last group of a block that ends early
+    // reads out of range there.
+    const int group_log2 = p.group_shift, my_group = (g & (FOLDS - 1)) * FOLD * 32 >> group_log2, block_groups = BLOCK >> group_log2;
+    const uint32_t scale_off = (uint32_t)(my_group * 16 + l16), tail = (p.blocks - 1) * block_groups + my_group < p.groups ? 0u : OUT_OF_RANGE;
+    const uint32_t no_zeros = p.has_zeros ? 0u : OUT_OF_RANGE;
     auto request = [&](Piece &c, int j) {                  // the wavefront's j-th piece
-        const int at = first + part + parts * j;
-        const bool past = j >= my_pieces;
-        const int group = ((at << 2) + (g & (folds - 1)) * p.fold) * 32 >> p.group_shift;
+        const int at = min(first + part + parts * j, p.blocks - 1);
+        const uint32_t past = j < my_pieces ? 0u : OUT_OF_RANGE, late = past | (at == p.blocks - 1 ? tail : 0u);
 #pragma unroll
         for (int t = 0; t < TN; ++t) {
-            const int i = SWIGLU ? t : 0, b = SWIGLU ? 0 : t;
-            c.w[t] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw[i], past ? OUT_OF_RANGE : (uint32_t)(b * p.blocks + at) * 1024u + lane * 16, 0, 0));
-            const uint32_t so = past || group >= p.groups ? OUT_OF_RANGE : (uint32_t)((b * p.groups + group) * 16 + l16);
-            if constexpr (F32) c.scale[t] = __builtin_amdgcn_raw_buffer_load_b32(rs[i], so * 4 | (so & OUT_OF_RANGE), 0, 0);
-            else c.scale[t] = __builtin_amdgcn_raw_buffer_load_b16(rs[i], so * 2 | (so & OUT_OF_RANGE), 0, 0);
-            c.zero[t] = __builtin_amdgcn_raw_buffer_load_b8(rz[i], so, 0, 0);
+            const int i = SWIGLU ? t : 0, b = SWIGLU ? 0 : min(t, n_blocks - 1), entry = (b * p.groups + at * block_groups) * 16;
+            c.w[t] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw[i], (uint32_t)lane * 16 | past, (b * p.blocks + at) * 1024, 0));
+            if constexpr (F32) c.scale[t] = __builtin_amdgcn_raw_buffer_load_b32(rs[i], scale_off * 4 | late, entry * 4, 0);
+            else c.scale[t] = __builtin_amdgcn_raw_buffer_load_b16(rs[i], scale_off * 2 | late, entry * 2, 0);
+            c.zero[t] = __builtin_amdgcn_raw_buffer_load_b8(rz[i], scale_off | late | no_zeros, entry, 0);
         }
     };
 
@@ -264,57 +303,78 @@ __global__ __launch_bounds__(NW * 64, TM == 1 && WHOLE ? 4 : 2) void w4_kernel(W
 #pragma unroll
     for (int i = 0; i < TM; ++i) x_row[i] = min(16 * i + l16, rows - 1) * UB;
     auto use = [&](const Piece &c, int held, int piece) {  // piece of the chunk
-        const char *x = lds + held * chunk_bytes + piece * 16 * row_units * UB;
-        const int at_sums = held * chunk_sums + piece * 4 * (TM * 16) + 4 * g;
-        Sum<XT> acc[TM][TN];
-        f32x4 xsum[TM];
+        const char *x = lds + held * chunk_bytes + (piece * 16 + g) * row_units * UB;
+        const float *xsc = xscales + held * chunk_scales + piece * 4 * (TM * 16) + 4 * g;
+        // all of the piece's operands are under way before the first is waited for (left to itself, the compiler asks for one at a
+        // time), where there is room for them
+        constexpr bool AHEAD = XT != X_F32 && (TM <= 2 || (XT == X_INT8 && FOLD > 1));
+        XOperand<XT> xo[4][TM];
+        auto read_x = [&](int s) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const bool begins = (s & (p.fold - 1)) == 0, ends = ((s + 1) & (p.fold - 1)) == 0;
-            if (begins) {
+            for (int i = 0; i < TM; ++i) xo[s][i] = operand<XT>(x + 4 * s * row_units * UB + x_row[i]);
+        };
+        if constexpr (AHEAD) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) read_x(s);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int f = 0; f < FOLDS; ++f) {
+            Sum<XT> acc[TM][TN], ones[TM];
+            constexpr int STEPS = XT == X_INT8 && FOLD > 1 ? 2 : 1;
+#pragma unroll
+            for (int s = f * FOLD; s < (f + 1) * FOLD; s += STEPS) {
+                WOperand<XT> w[TN][STEPS], one[STEPS];
+#pragma unroll
+                for (int k = 0; k < STEPS; ++k) {
+                    if constexpr (!AHEAD) read_x(s + k);
+                    one[k] = ones_operand<XT>();
+#pragma unroll
+                    for (int t = 0; t < TN; ++t) w[t][k] = codes<XT>(c.w[t][s + k]);
+                }
 #pragma unroll
                 for (int i = 0; i < TM; ++i) {
-                    xsum[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    ones[i] = product<XT, STEPS, TM>(&xo[s][i], one, s == f * FOLD ? Sum<XT>{0, 0, 0, 0} : ones[i]);
 #pragma unroll
-                    for (int t = 0; t < TN; ++t) acc[i][t] = Sum<XT>{0, 0, 0, 0};
+                    for (int t = 0; t < TN; ++t) acc[i][t] = product<XT, STEPS, TM>(&xo[s][i], w[t], s == f * FOLD ? Sum<XT>{0, 0, 0, 0} : acc[i][t]);
                 }
             }
+            const int from = f * 16 + l16;
+            float scale[TN];
 #pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                const char *u = x + (4 * s + g) * row_units * UB + x_row[i];
-                if constexpr (XT == X_INT8) {
-                    const int64_t a = *(const int64_t *)u;
-#pragma unroll
-                    for (int t = 0; t < TN; ++t) acc[i][t] = __builtin_amdgcn_mfma_i32_16x16x32_i8(a, codes_int8(c.w[t][s]), acc[i][t], 0, 0, 0);
-                } else {
-#pragma unroll
-                    for (int l = 0; l < (XT == X_F32 ? 3 : 1); ++l) {
-                        const bf16x8 a = *(const bf16x8 *)(u + 16 * l);
-#pragma unroll
-                        for (int t = 0; t < TN; ++t) acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, codes_bf16(c.w[t][s]), acc[i][t], 0, 0, 0);
-                    }
+            for (int t = 0; t < TN; ++t) {
+                uint32_t sc = c.scale[t], z = c.zero[t];
+                if (FOLDS > 1) {
+                    sc = __shfl((int)sc, from, WAVE);
+                    z = __shfl((int)z, from, WAVE);
                 }
-                xsum[i] += *(const f32x4 *)(sums + at_sums + s * (TM * 16) + 16 * i);
+                if (!p.has_zeros) z = 8;
+                scale[t] = __builtin_bit_cast(float, F32 ? sc : sc << 16);
+                const float minus_zero = -(float)(z + 16);
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        if constexpr (XT == X_INT8) acc[i][t][r] -= __mul24((int)z, ones[i][r]);
+                        else acc[i][t][r] = fmaf(minus_zero, ones[i][r], acc[i][t][r]);
+                    }
             }
-            if (ends) {
-                const int from = (s >> fold_log2) * 16 + l16;
+            if (X8 && p.x_groups > 1) {
 #pragma unroll
-                for (int t = 0; t < TN; ++t) {
-                    uint32_t sc = c.scale[t], z = c.zero[t];
-                    if (folds > 1) {
-                        sc = __shfl((int)sc, from, WAVE);
-                        z = __shfl((int)z, from, WAVE);
-                    }
-                    const float scale = __builtin_bit_cast(float, F32 ? sc : sc << 16);
-                    const float zero = (XT == X_INT8 ? 0.f : 16.f) + (p.has_zeros ? (float)z : 8.f);
+                for (int i = 0; i < TM; ++i) {
+                    const f32x4 xs = *(const f32x4 *)(xsc + f * FOLD * (TM * 16) + 16 * i);
 #pragma unroll
-                    for (int i = 0; i < TM; ++i) {
-                        f32x4 xs = {scale, scale, scale, scale};
-                        if (X8 && p.x_groups > 1) xs *= *(const f32x4 *)(xscales + at_sums + s * (TM * 16) + 16 * i);
+                    for (int t = 0; t < TN; ++t)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) total[i][t][r] = fmaf(fmaf(-zero, xsum[i][r], (float)acc[i][t][r]), xs[r], total[i][t][r]);
-                    }
+                        for (int r = 0; r < 4; ++r) total[i][t][r] = fmaf((float)acc[i][t][r], xs[r] * scale[t], total[i][t][r]);
                 }
+            } else {
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int t = 0; t < TN; ++t)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) total[i][t][r] = fmaf((float)acc[i][t][r], scale[t], total[i][t][r]);
             }
         }
     };
@@ -322,7 +382,7 @@ __global__ __launch_bounds__(NW * 64, TM == 1 && WHOLE ? 4 : 2) void w4_kernel(W
 #pragma unroll
     for (int d = 0; d < D; ++d) request(ring[d], d);
     if constexpr (WHOLE) {
-        constexpr int BATCH = XT == X_F32 ? 2 : 4;         // requests of a thread under way
+        constexpr int BATCH = XT == X_F32 ? 2 : TM == 1 ? 4 : 8;     // requests of a thread under way
         int piece = piece0, row = row_0;
         for (int u = tid; u - tid < units; u += BATCH * NW * 64) {
             XRaw<XT> x[BATCH];
@@ -372,32 +432,33 @@ __global__ __launch_bounds__(NW * 64, TM == 1 && WHOLE ? 4 : 2) void w4_kernel(W
         }
     }
 
-    float (*meet)[TN][256] = (float (*)[TN][256])lds;      // [wavefront][block][r * 64 + lane]
-    const int outs = cols * TNO * 256;
+    float (*meet)[TM][TN][256] = (float (*)[TM][TN][256])lds;                    // [wavefront][row block][block][r * 64 + lane]
+    __syncthreads();                                       // X has been read
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        if (16 * i >= rows) break;
-        __syncthreads();                                   // X, or the sums of the block before, have been read
+    for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int t = 0; t < TN; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) meet[wave][t][r * 64 + lane] = total[i][t][r];
-        __syncthreads();
-        for (int o = tid; o < outs; o += NW * 64) {        // row by row: neighbouring threads have neighbouring columns
-            const int col = o % (cols * TNO * 16), m = o / (cols * TNO * 16), b = col >> 4;
-            const int n = tile0 * 16 + col, row = row0 + 16 * i + m;
-            if (16 * i + m >= rows || n >= p.N) continue;
-            const int slot = (m & 3) * 64 + (m >> 2) * 16 + (col & 15), w0 = b / TNO, t0 = b % TNO;
-            float v[2] = {0.f, 0.f};
-            for (int w = 0; w < parts; ++w) {
-                v[0] += meet[w0 + w * cols][t0][slot];
-                if (SWIGLU) v[1] += meet[w0 + w * cols][TN - 1][slot];
-            }
-            if (p.slices > 1) {
+            for (int r = 0; r < 4; ++r) meet[wave][i][t][r * 64 + lane] = total[i][t][r];
+    __syncthreads();
+    // row by row: neighbouring threads have neighbouring columns
+    constexpr int TNO_LOG2 = TNO == 2 ? 1 : 0;
+    const int width_log2 = p.cols_log2 + TNO_LOG2 + 4, width = 1 << width_log2;
+    for (int o = tid; o < rows << width_log2; o += NW * 64) {
+        const int col = o & (width - 1), row = o >> width_log2, n = tile0 * 16 + col;
+        if (n >= p.N) continue;
+        const int m = row & 15, b = col >> 4, slot = (m & 3) * 64 + (m >> 2) * 16 + (col & 15), w0 = b >> TNO_LOG2, t0 = b & (TNO - 1);
+        float v[2] = {0.f, 0.f};
 #pragma unroll
-                for (int u = 0; u < MATS; ++u) p.planes[((int64_t)(blockIdx.y * MATS + u) * p.M + row) * p.N + n] = v[u];
-            } else finish<XT, F32, SWIGLU>(p, v, row, n);
+        for (int w = 0; w < NW; ++w) {
+            if (w >= parts) break;
+            v[0] += meet[w0 + (w << p.cols_log2)][row >> 4][t0][slot];
+            if (SWIGLU) v[1] += meet[w0 + (w << p.cols_log2)][row >> 4][TN - 1][slot];
         }
+        if (p.slices > 1) {
+#pragma unroll
+            for (int u = 0; u < MATS; ++u) p.planes[((int64_t)(blockIdx.y * MATS + u) * p.M + row0 + row) * p.N + n] = v[u];
+        } else finish<XT, F32, SWIGLU>(p, v, row0 + row, n);
     }
 }
 
@@ -418,7 +479,7 @@ __global__ __launch_bounds__(256) void w4_finish_kernel(W4Params p) {
 
 // How a product is cut.  One choice for the workspace and the launch.
 struct Cut {
-    int tm, tn, cols_log2, slices, slice_blocks, chunk, held;
+    int tm, tn, fold, cols_log2, slices, slice_blocks, chunk, held;
     size_t lds;
 };
 constexpr size_t LDS_MOST = 160 * 1024;
@@ -432,7 +493,9 @@ Cut cut_of(const cascade_w4_weights *w, const cascade_w4_gemm_desc *d) {
     const int blocks = (w->k + BLOCK - 1) / BLOCK, col_blocks = (w->n_out + 15) / 16;
     c.tn = swiglu || c.tm > 1 || col_blocks > 256 ? 2 : 1;
     const int units = (col_blocks + (swiglu ? 1 : c.tn) - 1) / (swiglu ? 1 : c.tn);      // of a wavefront's columns
-    auto lds_of = [&](int chunk, int held) { return (size_t)held * chunk * (16 * (rows | 1) * unit + 4 * c.tm * 16 * 4 * (d->x_format ? 2 : 1)); };
+    const int x_group = d->x_format ? d->x_group : 0;
+    c.fold = w->dtype == CASCADE_F32 ? 1 : std::min(w->group, x_group ? std::min(x_group, BLOCK) : BLOCK) / 32;
+    auto lds_of = [&](int chunk, int held) { return (size_t)held * chunk * (16 * (rows | 1) * unit + (d->x_format ? 4 * c.tm * 16 * 4 : 0)); };
     double best = 1e30;
     for (int lg = 0; lg <= 3; ++lg) {
         const int parts = NW >> lg, chunk = 2 * parts;
@@ -442,7 +505,7 @@ Cut cut_of(const cascade_w4_weights *w, const cascade_w4_gemm_desc *d) {
             if (slices > 1 && ((int64_t)per * (slices - 1) >= blocks || per < 2 * parts)) continue;
             const bool whole = lds_of(std::min(per, blocks), 1) <= LDS_MOST;
             if (!whole && chunk * rows * 16 > MAX_UNITS * NW * 64) continue;
-            const size_t lds = std::max(whole ? lds_of(std::min(per, blocks), 1) : lds_of(chunk, 2), (size_t)NW * c.tn * 1024);
+            const size_t lds = std::max(whole ? lds_of(std::min(per, blocks), 1) : lds_of(chunk, 2), (size_t)NW * c.tm * c.tn * 1024);
             if (lds > LDS_MOST) continue;
             const int resident = c.tm == 1 && whole && lds <= LDS_MOST / 2 ? 2 : 1;
             // microseconds: rounds of workgroups, each a start and its pieces at the rate that the resident ones share
@@ -463,14 +526,14 @@ Cut cut_of(const cascade_w4_weights *w, const cascade_w4_gemm_desc *d) {
     return c;
 }
 
-template <int XT, bool F32, int TM, int TN, bool SWIGLU, bool WHOLE>
+template <int XT, bool F32, int TM, int TN, bool SWIGLU, int FOLD, bool WHOLE>
 int32_t launch(const W4Params &p, const Cut &c, hipStream_t s) {
     static std::atomic<uint64_t> done{0};
-    const void *kernel = (const void *)w4_kernel<XT, F32, TM, TN, SWIGLU, WHOLE>;
+    const void *kernel = (const void *)w4_kernel<XT, F32, TM, TN, SWIGLU, FOLD, WHOLE>;
     CASCADE_HIP_TRY(ensure_dynamic_lds(kernel, (int)LDS_MOST, done));
     const int cols = (SWIGLU ? 1 : TN) << c.cols_log2;
     const dim3 grid((unsigned)(((p.N + 15) / 16 + cols - 1) / cols), (unsigned)p.slices, (unsigned)((p.M + TM * 16 - 1) / (TM * 16)));
-    hipLaunchKernelGGL((w4_kernel<XT, F32, TM, TN, SWIGLU, WHOLE>), grid, dim3(NW * 64), c.lds, s, p);
+    hipLaunchKernelGGL((w4_kernel<XT, F32, TM, TN, SWIGLU, FOLD, WHOLE>), grid, dim3(NW * 64), c.lds, s, p);
     if (p.slices > 1)
         hipLaunchKernelGGL((w4_finish_kernel<XT, F32, SWIGLU>), dim3((unsigned)std::min<int64_t>(((int64_t)p.M * p.N + 255) / 256, 1 << 16)), dim3(256), 0, s, p);
     CASCADE_HIP_TRY(hipGetLastError());
@@ -478,7 +541,11 @@ int32_t launch(const W4Params &p, const Cut &c, hipStream_t s) {
 }
 template <int XT, bool F32, int TM, int TN, bool SWIGLU>
 int32_t launch_held(const W4Params &p, const Cut &c, hipStream_t s) {
-    return c.held == 1 ? launch<XT, F32, TM, TN, SWIGLU, true>(p, c, s) : launch<XT, F32, TM, TN, SWIGLU, false>(p, c, s);
+    if constexpr (!F32) {
+        if (c.fold == 4) return c.held == 1 ? launch<XT, F32, TM, TN, SWIGLU, 4, true>(p, c, s) : launch<XT, F32, TM, TN, SWIGLU, 4, false>(p, c, s);
+        if (c.fold == 2) return c.held == 1 ? launch<XT, F32, TM, TN, SWIGLU, 2, true>(p, c, s) : launch<XT, F32, TM, TN, SWIGLU, 2, false>(p, c, s);
+    }
+    return c.held == 1 ? launch<XT, F32, TM, TN, SWIGLU, 1, true>(p, c, s) : launch<XT, F32, TM, TN, SWIGLU, 1, false>(p, c, s);
 }
 template <int XT, bool F32, int TM>
 int32_t launch_rows(const W4Params &p, const Cut &c, hipStream_t s) {
@@ -626,12 +693,11 @@ extern "C" int32_t cascade_w4_gemm(const cascade_w4_weights *w, const cascade_w4
     for (int i = 0; i < (swiglu ? 2 : 1); ++i) {
         p.codes[i] = (const char *)(i ? up : w)->packed;
         p.scales[i] = p.codes[i] + l.scales;
-        p.zeros[i] = p.codes[i] + l.zeros;
+        p.zeros[i] = p.codes[i] + (w->zero_points ? l.zeros : l.scales);       // (not used without zero points)
     }
     p.X = (const char *)X; p.x_scale = x_scale; p.bias = bias; p.residual = residual; p.Y = Y;
     p.blocks = (p.K + BLOCK - 1) / BLOCK; p.groups = p.K / w->group;
     const int x_group = d->x_format ? d->x_group : 0;
-    p.fold = std::min(w->group, x_group ? std::min(x_group, BLOCK) : BLOCK) / 32;
     p.group_shift = __builtin_ctz((unsigned)w->group);
     p.x_group_shift = x_group ? __builtin_ctz((unsigned)x_group) : 31;
     p.x_groups = x_group ? p.K / x_group : 1;
