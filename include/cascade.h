@@ -673,7 +673,7 @@ CASCADE_API int32_t cascade_add_norm(const cascade_add_norm_desc *desc, const vo
  * scales and zeros too.                                                             */
 typedef struct cascade_w4_weights {
     int32_t dtype;        /* of the scales, and of the product's bias, residual and Y  */
-    int32_t n_out, k;     /* k: a multiple of group, at most 2^20                      */
+    int32_t n_out, k;     /* n_out: at most 2^26; k: a multiple of group, at most 2^20 */
     int32_t group;        /* reduction elements of a scale: 32, 64 or 128              */
     int32_t zero_points;  /* 0: zero is 8 everywhere                                   */
     int32_t reserved;     /* 0                                                         */
@@ -684,7 +684,7 @@ CASCADE_API size_t cascade_w4_bytes(const cascade_w4_weights *weights);
 
 /* codes [n_out, k] bytes, scales [n_out, k / group] in dtype, zeros [n_out, k / group] bytes (NULL
  * exactly where zero_points is 0); of codes and zeros the low 4 bits count.
- * Errors: EINVAL, ESHAPE (k % group), EUNSUPPORTED (dtype, group, k, alignment), EHIP. */
+ * Errors: EINVAL, ESHAPE (k % group), EUNSUPPORTED (dtype, group, n_out, k, alignment), EHIP. */
 CASCADE_API int32_t cascade_w4_pack(const cascade_w4_weights *weights, const void *codes, const void *scales, const void *zeros,
                         void *stream);
 
@@ -698,10 +698,10 @@ CASCADE_API int32_t cascade_w4_pack(const cascade_w4_weights *weights, const voi
  * overlap X.  Calls that may overlap in time need a workspace each (16-byte aligned; contents need
  * not be kept between calls).  A call with the same arguments gives the same bits each time; those of a row may depend on the
  * number of rows.
- * Errors: EINVAL, ESHAPE (strides, W_up), EUNSUPPORTED (dtype, group, x_format, alignment, an
+ * Errors: EINVAL, ESHAPE (strides, W_up), EUNSUPPORTED (dtype, group, sizes, alignment, an
  * epilogue other than these, BIAS with SWIGLU), EWORKSPACE, EHIP.                   */
 typedef struct cascade_w4_gemm_desc {
-    int32_t rows;
+    int32_t rows;         /* at most 2^20                                              */
     int32_t x_format;     /* CASCADE_Q8_*; NONE: X in the weights' dtype              */
     int32_t x_group;      /* 8-bit X: columns of a scale: 32, 64, 128 or 256, dividing k; 0: the row */
     int32_t epilogue;     /* CASCADE_EPI_BIAS | GELU_ERF | GELU_TANH | SWIGLU | RESIDUAL */
@@ -728,14 +728,14 @@ CASCADE_API int32_t cascade_w4_gemm(const cascade_w4_weights *weights, const cas
  * The same arguments give the same tokens each time, whatever the other rows.       */
 typedef struct cascade_sample_desc {
     int32_t dtype;        /* of the logits                                            */
-    int32_t rows, vocab;  /* vocab: at most 2^20                                       */
+    int32_t rows, vocab;  /* rows: at most 65536; vocab: at most 2^20                  */
     int32_t reserved;     /* 0                                                         */
     int64_t stride;       /* of rows, in elements; 0: dense                            */
 } cascade_sample_desc;
 
 /* uniform [rows] in [0, 1); token [rows] int32.  workspace: 16-byte aligned; calls that may overlap in time need one each, its contents
  * need not be kept between calls.
- * Errors: EINVAL, ESHAPE (stride), EUNSUPPORTED (dtype, vocab), EWORKSPACE, EHIP.   */
+ * Errors: EINVAL, ESHAPE (stride), EUNSUPPORTED (dtype, rows, vocab), EWORKSPACE, EHIP.   */
 CASCADE_API size_t cascade_sample_workspace_bytes(const cascade_sample_desc *desc);
 CASCADE_API int32_t cascade_sample(const cascade_sample_desc *desc, const void *logits, const float *temperature, const int32_t *top_k,
                        const float *top_p, const float *min_p, const float *uniform, int32_t *token, float *prob,

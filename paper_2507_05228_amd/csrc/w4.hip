@@ -34,10 +34,11 @@ struct W4Params {
     const float *x_scale;
     const void *bias, *residual;
     void *Y;
-    float *planes;                                         // [slices][matrices][M][N] sums, where the reduction is cut
+    float *planes;                                         // [slices][matrices][row blocks][col blocks][64][4] sums, where the reduction is cut
     int64_t ldx, ldres, ldy;                               // elements
     int32_t M, N, K;
     int32_t blocks, groups;                                // of the reduction
+    int32_t row_blocks, col_blocks;                        // of 16
     int32_t group_shift, x_group_shift, x_groups;          // log2 of the elements of a scale (x_group_shift 31: the row)
     int32_t has_zeros, flags;
     int32_t cols_log2;                                     // column groups of a workgroup; 8 >> cols_log2 parts of the reduction
@@ -216,7 +217,7 @@ __global__ __launch_bounds__(NW * 64, TM == 1 && WHOLE ? 4 : 2) void w4_kernel(W
     const int tile0 = blockIdx.x * cols * TNO;             // 16-column blocks: of the workgroup,
     // of the wavefront, and how many there are.  Those behind the last column read the first block, or the one beside them, instead, and are
     // not stored: whatever a range check makes of scalar offsets, they stay inside the weights.
-    const int left_blocks = (p.N + 15) / 16 - tile0 - cg * TNO, block0 = __builtin_amdgcn_readfirstlane(left_blocks > 0 ? tile0 + cg * TNO : 0);
+    const int left_blocks = p.col_blocks - tile0 - cg * TNO, block0 = __builtin_amdgcn_readfirstlane(left_blocks > 0 ? tile0 + cg * TNO : 0);
     const int n_blocks = __builtin_amdgcn_readfirstlane(left_blocks > 0 ? min(left_blocks, TNO) : 1);
     const int first = blockIdx.y * p.slice_blocks, n_pieces = min(p.blocks - first, p.slice_blocks);
 
@@ -255,18 +256,23 @@ __global__ __launch_bounds__(NW * 64, TM == 1 && WHOLE ? 4 : 2) void w4_kernel(W
         }
     };
     const int piece0 = (tid >> 4) / rows, row_0 = (tid >> 4) % rows;
+    const bool scaled_steps = X8 && p.x_groups > 1;
+    struct Unit {
+        XRaw<XT> x;
+        uint32_t scale;
+    };
     auto request_x = [&](int chunk, int piece, int row, bool is) {
         const int q = chunk * p.chunk + piece, col = (first + q) * BLOCK + 8 * sg;
-        return load_x<XT>(rx, is && q < n_pieces && col < p.K ? (uint32_t)(row * p.ldx + col) * x_bytes<XT>() : OUT_OF_RANGE);
+        is = is && q < n_pieces && col < p.K;
+        Unit u;
+        u.x = load_x<XT>(rx, is ? (uint32_t)(row * p.ldx + col) * x_bytes<XT>() : OUT_OF_RANGE);
+        if constexpr (X8) u.scale = __builtin_amdgcn_raw_buffer_load_b32(rxs, is && scaled_steps ? (uint32_t)(row * p.x_groups + (col >> p.x_group_shift)) * 4u : OUT_OF_RANGE, 0, 0);
+        return u;
     };
-    auto store_unit = [&](int chunk, int held, int piece, int row, bool is, const XRaw<XT> &x) {
+    auto store_unit = [&](int held, int piece, int row, bool is, const Unit &u) {
         if (!is) return;
-        store_x<XT>(x, lds + held * chunk_bytes + ((piece * 16 + sg) * row_units + row) * UB);
-        if (X8 && p.x_groups > 1 && (sg & 3) == 0) {
-            const int q = chunk * p.chunk + piece, col = (first + q) * BLOCK + 8 * sg;
-            const uint32_t o = q < n_pieces && col < p.K ? (uint32_t)(row * p.x_groups + (col >> p.x_group_shift)) * 4u : OUT_OF_RANGE;
-            xscales[held * chunk_scales + (piece * 4 + (sg >> 2)) * (TM * 16) + row] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rxs, o, 0, 0));
-        }
+        store_x<XT>(u.x, lds + held * chunk_bytes + ((piece * 16 + sg) * row_units + row) * UB);
+        if (scaled_steps && (sg & 3) == 0) xscales[held * chunk_scales + (piece * 4 + (sg >> 2)) * (TM * 16) + row] = __builtin_bit_cast(float, u.scale);
     };
 
     struct Piece {
@@ -379,17 +385,23 @@ __global__ __launch_bounds__(NW * 64, TM == 1 && WHOLE ? 4 : 2) void w4_kernel(W
         }
     };
 
+    // Loads arrive in the order of their requests: what is needed first is asked for first
+    auto fill_ring = [&] {
 #pragma unroll
-    for (int d = 0; d < D; ++d) request(ring[d], d);
+        for (int d = 0; d < D; ++d) request(ring[d], d);
+    };
     if constexpr (WHOLE) {
         constexpr int BATCH = XT == X_F32 ? 2 : TM == 1 ? 4 : 8;     // requests of a thread under way
         int piece = piece0, row = row_0;
-        for (int u = tid; u - tid < units; u += BATCH * NW * 64) {
-            XRaw<XT> x[BATCH];
+        auto stage = [&](int u, auto between) {
+            Unit x[BATCH];
             int piece_too = piece, row_too = row;
             each_unit(u, BATCH, piece, row, [&](int k, int q, int r, bool is) { x[k] = request_x(0, q, r, is); });
-            each_unit(u, BATCH, piece_too, row_too, [&](int k, int q, int r, bool is) { store_unit(0, 0, q, r, is, x[k]); });
-        }
+            between();
+            each_unit(u, BATCH, piece_too, row_too, [&](int k, int q, int r, bool is) { store_unit(0, q, r, is, x[k]); });
+        };
+        stage(tid, fill_ring);
+        for (int u = tid + BATCH * NW * 64; u - tid < units; u += BATCH * NW * 64) stage(u, [] {});
         __syncthreads();
         for (int j0 = 0; j0 < my_pieces; j0 += D) {
 #pragma unroll
@@ -401,64 +413,88 @@ __global__ __launch_bounds__(NW * 64, TM == 1 && WHOLE ? 4 : 2) void w4_kernel(W
     } else {
         static_assert(D == 4, "two chunks of two pieces");
         const int chunks = (n_pieces + p.chunk - 1) / p.chunk;
-        XRaw<XT> ahead[MAX_UNITS];
-        auto request_chunk = [&](int chunk) {
+        Unit start[MAX_UNITS], ahead[MAX_UNITS];
+        auto request_chunk = [&](int chunk, Unit *to) {
             int piece = piece0, row = row_0;
-            each_unit(tid, MAX_UNITS, piece, row, [&](int k, int q, int r, bool is) { ahead[k] = request_x(chunk, q, r, is); });
+            each_unit(tid, MAX_UNITS, piece, row, [&](int k, int q, int r, bool is) { to[k] = request_x(chunk, q, r, is); });
         };
-        auto store_chunk = [&](int chunk, int held) {
+        auto store_chunk = [&](int held, const Unit *from) {
             int piece = piece0, row = row_0;
-            each_unit(tid, MAX_UNITS, piece, row, [&](int k, int q, int r, bool is) { store_unit(chunk, held, q, r, is, ahead[k]); });
+            each_unit(tid, MAX_UNITS, piece, row, [&](int k, int q, int r, bool is) { store_unit(held, q, r, is, from[k]); });
         };
-        request_chunk(0);
-        store_chunk(0, 0);
-        request_chunk(1);
+        request_chunk(0, start);
+        request_chunk(1, ahead);
+        fill_ring();
+        store_chunk(0, start);
         __syncthreads();
         for (int c0 = 0; c0 < chunks; c0 += 2) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
+                // the other half has been read before the last barrier; waiting for its X leaves the newest codes under way
+                store_chunk(1 - h, ahead);
+                request_chunk(c0 + h + 2, ahead);
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const int j = 2 * (c0 + h) + t;
                     if (j < my_pieces) use(ring[2 * h + t], h, t * parts + part);
                     request(ring[2 * h + t], j + D);
                 }
-                if (c0 + h + 1 < chunks) {                 // the other half has been read before the barrier in front of this one
-                    store_chunk(c0 + h + 1, 1 - h);
-                    request_chunk(c0 + h + 2);
-                    __syncthreads();
-                }
+                __syncthreads();
             }
         }
     }
 
-    float (*meet)[TM][TN][256] = (float (*)[TM][TN][256])lds;                    // [wavefront][row block][block][r * 64 + lane]
-    __syncthreads();                                       // X has been read
+    // Sums stay in the order of the products' results: a lane has four rows of a column.  Those of a cut reduction go out as they
+    // are, 1 KB a block, and where no other wavefront of the workgroup has a share in them straight from the registers.
+    const int row_blocks = (rows + 15) >> 4;
+    auto plane = [&](int u, int i, int block) {
+        return (f32x4 *)p.planes + ((((int64_t)blockIdx.y * MATS + u) * p.row_blocks + row0 / 16 + i) * p.col_blocks + block) * 64 + lane;
+    };
+    if (__builtin_expect(p.slices > 1 && parts == 1, 0)) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int t = 0; t < TN; ++t)
+                if (i < row_blocks && (SWIGLU ? 0 : t) < left_blocks) *plane(SWIGLU ? t : 0, i, block0 + (SWIGLU ? 0 : t)) = total[i][t];
+        return;
+    }
+    f32x4 (*meet)[TM][TN][64] = (f32x4 (*)[TM][TN][64])lds;                      // [wavefront][row block][block][lane]
+    if constexpr (WHOLE) __syncthreads();                  // X has been read
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int t = 0; t < TN; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) meet[wave][i][t][r * 64 + lane] = total[i][t][r];
+        for (int t = 0; t < TN; ++t) meet[wave][i][t][lane] = total[i][t];
     __syncthreads();
-    // row by row: neighbouring threads have neighbouring columns
-    constexpr int TNO_LOG2 = TNO == 2 ? 1 : 0;
-    const int width_log2 = p.cols_log2 + TNO_LOG2 + 4, width = 1 << width_log2;
-    for (int o = tid; o < rows << width_log2; o += NW * 64) {
-        const int col = o & (width - 1), row = o >> width_log2, n = tile0 * 16 + col;
-        if (n >= p.N) continue;
-        const int m = row & 15, b = col >> 4, slot = (m & 3) * 64 + (m >> 2) * 16 + (col & 15), w0 = b >> TNO_LOG2, t0 = b & (TNO - 1);
+    if (__builtin_expect(p.slices > 1, 0)) {               // blocks over wavefronts
+        for (int job = wave; job < row_blocks * TNO << p.cols_log2; job += NW) {
+            const int c = job & (cols - 1), at = job >> p.cols_log2, t = at & (TNO - 1), i = at / TNO, block = tile0 + c * TNO + t;
+            if (block >= p.col_blocks) continue;
+#pragma unroll
+            for (int u = 0; u < MATS; ++u) {
+                f32x4 v = meet[c][i][t + u][lane];
+                for (int w = 1; w < parts; ++w) {
+                    const f32x4 more = meet[c + (w << p.cols_log2)][i][t + u][lane];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] += more[k];
+                }
+                *plane(u, i, block) = v;
+            }
+        }
+        return;
+    }
+    // every fourth row of a block over wavefronts
+    for (int job = wave; job < row_blocks * TNO * 4 << p.cols_log2; job += NW) {
+        const int r = job & 3, c = job >> 2 & (cols - 1), at = job >> (2 + p.cols_log2), t = at & (TNO - 1), i = at / TNO;
+        const int row = 16 * i + 4 * g + r, n = (tile0 + c * TNO + t) * 16 + l16;
+        if (row >= rows || n >= p.N) continue;
         float v[2] = {0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
             if (w >= parts) break;
-            v[0] += meet[w0 + (w << p.cols_log2)][row >> 4][t0][slot];
-            if (SWIGLU) v[1] += meet[w0 + (w << p.cols_log2)][row >> 4][TN - 1][slot];
-        }
-        if (p.slices > 1) {
 #pragma unroll
-            for (int u = 0; u < MATS; ++u) p.planes[((int64_t)(blockIdx.y * MATS + u) * p.M + row0 + row) * p.N + n] = v[u];
-        } else finish<XT, F32, SWIGLU>(p, v, row0 + row, n);
+            for (int u = 0; u < MATS; ++u) v[u] += ((const float *)&meet[c + (w << p.cols_log2)][i][t + u][lane])[r];
+        }
+        finish<XT, F32, SWIGLU>(p, v, row0 + row, n);
     }
 }
 
@@ -466,14 +502,25 @@ __global__ __launch_bounds__(NW * 64, TM == 1 && WHOLE ? 4 : 2) void w4_kernel(W
 template <int XT, bool F32, bool SWIGLU>
 __global__ __launch_bounds__(256) void w4_finish_kernel(W4Params p) {
     constexpr int MATS = SWIGLU ? 2 : 1;
-    const int64_t size = (int64_t)p.M * p.N;
-    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < size; e += (int64_t)gridDim.x * 256) {
-        float v[2] = {0.f, 0.f};
+    const int64_t plane = (int64_t)p.row_blocks * p.col_blocks * 64;                 // lanes
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < plane; e += (int64_t)gridDim.x * 256) {
+        const int lane = (int)(e & 63), n = (int)((e >> 6) % p.col_blocks) * 16 + (lane & 15);
+        const int row = (int)((e >> 6) / p.col_blocks) * 16 + (lane >> 4) * 4;
+        if (n >= p.N || row >= p.M) continue;
+        f32x4 sum[MATS] = {};
 #pragma unroll 4
         for (int s = 0; s < p.slices; ++s)
 #pragma unroll
-            for (int u = 0; u < MATS; ++u) v[u] += p.planes[(s * MATS + u) * size + e];
-        finish<XT, F32, SWIGLU>(p, v, (int)(e / p.N), (int)(e % p.N));
+            for (int u = 0; u < MATS; ++u) {
+                const f32x4 v = ((const f32x4 *)p.planes)[(s * MATS + u) * plane + e];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sum[u][k] += v[k];
+            }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float v[2] = {sum[0][r], sum[MATS - 1][r]};
+            if (row + r < p.M) finish<XT, F32, SWIGLU>(p, v, row + r, n);
+        }
     }
 }
 
@@ -511,10 +558,11 @@ Cut cut_of(const cascade_w4_weights *w, const cascade_w4_gemm_desc *d) {
             // microseconds: rounds of workgroups, each a start and its pieces at the rate that the resident ones share
             const int64_t groups = tiles * slices * ((d->rows + c.tm * 16 - 1) / (c.tm * 16));
             const int64_t full = groups / (256 * resident), rest = groups - full * 256 * resident;
-            const double piece = c.tn * 1.024 / 20.0 * 8;  // eight wavefronts' pieces at 20 KB a microsecond and CU
-            const double turns = (double)((per + parts - 1) / parts);
-            const double bytes = (full * resident + (rest + 255) / 256) * turns * piece, start = 2.5 * (full + (rest ? 1 : 0));
-            const double planes = slices > 1 ? 3.0 + 2.0 * slices * d->rows * (double)w->n_out * 4 * (swiglu ? 2 : 1) / 4e6 : 0.0;
+            // eight wavefronts' pieces at 20 KB a microsecond and CU, or at their products' pace; X at twice that rate
+            const double turn = std::max(8 * 1.024 * c.tn / 20.0, 0.17 * c.tm * c.tn);
+            const double turns = (double)((per + parts - 1) / parts), x = per * 16.0 * rows * unit / 40e3;
+            const double bytes = (full * resident + (rest + 255) / 256) * (turns * turn + x), start = 2.5 * (full + (rest ? 1 : 0));
+            const double planes = slices > 1 ? 3.0 + 2.0 * slices * d->rows * (double)w->n_out * 4 * (swiglu ? 2 : 1) / 6e6 : 0.0;
             const double cost = bytes + start + planes;
             if (cost < best) {
                 best = cost;
@@ -532,10 +580,10 @@ int32_t launch(const W4Params &p, const Cut &c, hipStream_t s) {
     const void *kernel = (const void *)w4_kernel<XT, F32, TM, TN, SWIGLU, FOLD, WHOLE>;
     CASCADE_HIP_TRY(ensure_dynamic_lds(kernel, (int)LDS_MOST, done));
     const int cols = (SWIGLU ? 1 : TN) << c.cols_log2;
-    const dim3 grid((unsigned)(((p.N + 15) / 16 + cols - 1) / cols), (unsigned)p.slices, (unsigned)((p.M + TM * 16 - 1) / (TM * 16)));
+    const dim3 grid((unsigned)((p.col_blocks + cols - 1) / cols), (unsigned)p.slices, (unsigned)((p.M + TM * 16 - 1) / (TM * 16)));
     hipLaunchKernelGGL((w4_kernel<XT, F32, TM, TN, SWIGLU, FOLD, WHOLE>), grid, dim3(NW * 64), c.lds, s, p);
     if (p.slices > 1)
-        hipLaunchKernelGGL((w4_finish_kernel<XT, F32, SWIGLU>), dim3((unsigned)std::min<int64_t>(((int64_t)p.M * p.N + 255) / 256, 1 << 16)), dim3(256), 0, s, p);
+        hipLaunchKernelGGL((w4_finish_kernel<XT, F32, SWIGLU>), dim3((unsigned)std::min<int64_t>(((int64_t)p.row_blocks * p.col_blocks + 3) / 4, 1 << 16)), dim3(256), 0, s, p);
     CASCADE_HIP_TRY(hipGetLastError());
     return CASCADE_OK;
 }
@@ -614,7 +662,7 @@ int32_t check_weights(const cascade_w4_weights *w) {
     if (w->dtype != CASCADE_F32 && w->dtype != CASCADE_BF16) return CASCADE_EUNSUPPORTED;
     if (w->group != 32 && w->group != 64 && w->group != 128) return CASCADE_EUNSUPPORTED;
     if (w->k % w->group) return CASCADE_ESHAPE;
-    if (w->k > 1 << 20 || w->n_out > INT32_MAX - 64) return CASCADE_EUNSUPPORTED;
+    if (w->k > 1 << 20 || w->n_out > 1 << 26) return CASCADE_EUNSUPPORTED;
     return CASCADE_OK;
 }
 
@@ -623,6 +671,7 @@ int32_t check_gemm(const cascade_w4_weights *w, const cascade_w4_gemm_desc *d) {
     if (st != CASCADE_OK) return st;
     if (!d || d->rows < 0 || d->x_group < 0 || d->x_format < 0 || d->x_format > CASCADE_Q8_E4M3) return CASCADE_EINVAL;
     if (d->x_stride < 0 || d->residual_stride < 0 || d->y_stride < 0) return CASCADE_EINVAL;
+    if (d->rows > 1 << 20) return CASCADE_EUNSUPPORTED;
     const int acts = CASCADE_EPI_GELU_ERF | CASCADE_EPI_GELU_TANH | CASCADE_EPI_SWIGLU;
     if (d->epilogue & ~(acts | CASCADE_EPI_BIAS | CASCADE_EPI_RESIDUAL)) return CASCADE_EUNSUPPORTED;
     if (__builtin_popcount(d->epilogue & acts) > 1) return CASCADE_EUNSUPPORTED;
@@ -661,7 +710,7 @@ extern "C" int32_t cascade_w4_pack(const cascade_w4_weights *w, const void *code
 extern "C" size_t cascade_w4_gemm_workspace_bytes(const cascade_w4_weights *w, const cascade_w4_gemm_desc *d) {
     if (check_gemm(w, d) != CASCADE_OK || d->rows == 0) return 0;
     const Cut c = cut_of(w, d);
-    return c.slices > 1 ? (size_t)c.slices * d->rows * w->n_out * 4 * (d->epilogue & CASCADE_EPI_SWIGLU ? 2 : 1) : 0;
+    return c.slices > 1 ? (size_t)c.slices * ((d->rows + 15) / 16) * ((w->n_out + 15) / 16) * 1024 * (d->epilogue & CASCADE_EPI_SWIGLU ? 2 : 1) : 0;
 }
 
 extern "C" int32_t cascade_w4_gemm(const cascade_w4_weights *w, const cascade_w4_weights *up, const cascade_w4_gemm_desc *d, const void *X,
@@ -697,6 +746,7 @@ extern "C" int32_t cascade_w4_gemm(const cascade_w4_weights *w, const cascade_w4
     }
     p.X = (const char *)X; p.x_scale = x_scale; p.bias = bias; p.residual = residual; p.Y = Y;
     p.blocks = (p.K + BLOCK - 1) / BLOCK; p.groups = p.K / w->group;
+    p.row_blocks = (p.M + 15) / 16; p.col_blocks = (p.N + 15) / 16;
     const int x_group = d->x_format ? d->x_group : 0;
     p.group_shift = __builtin_ctz((unsigned)w->group);
     p.x_group_shift = x_group ? __builtin_ctz((unsigned)x_group) : 31;

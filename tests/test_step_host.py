@@ -76,7 +76,7 @@ def weights(**change):
 BAD_WEIGHTS = [(dict(n_out=0), cas.EINVAL), (dict(k=0), cas.EINVAL), (dict(group=0), cas.EINVAL), (dict(reserved=1), cas.EINVAL),
                (dict(zero_points=2), cas.EINVAL), (dict(dtype=2), cas.EUNSUPPORTED), (dict(group=16), cas.EUNSUPPORTED),
                (dict(group=256), cas.EUNSUPPORTED), (dict(k=288), cas.ESHAPE), (dict(k=(1 << 20) + 64), cas.EUNSUPPORTED),
-               (dict(n_out=(1 << 31) - 1), cas.EUNSUPPORTED), (dict(packed=None), cas.EINVAL), (dict(packed=P + 128), cas.EUNSUPPORTED)]
+               (dict(n_out=(1 << 31) - 1), cas.EUNSUPPORTED), (dict(n_out=(1 << 26) + 1), cas.EUNSUPPORTED), (dict(packed=None), cas.EINVAL), (dict(packed=P + 128), cas.EUNSUPPORTED)]
 
 
 @pytest.mark.parametrize("change,status", BAD_WEIGHTS)
@@ -127,7 +127,7 @@ def gemm(lib, w=None, up=None, X=4 * P, x_scale=None, bias=None, residual=None, 
     (dict(up=weights(group=32), epilogue=cas.EPI_SWIGLU), cas.ESHAPE), (dict(up=weights(zero_points=1), epilogue=cas.EPI_SWIGLU), cas.ESHAPE),
     (dict(up=weights(dtype=cas.F32), epilogue=cas.EPI_SWIGLU), cas.ESHAPE), (dict(up=weights(packed=P + 16), epilogue=cas.EPI_SWIGLU), cas.EUNSUPPORTED),
     (dict(X=4 * P + 8), cas.EUNSUPPORTED), (dict(x_stride=260), cas.EUNSUPPORTED), (dict(x_stride=1 << 23), cas.EUNSUPPORTED),
-    (dict(rows=0), cas.OK), (dict(rows=0, up=weights(), epilogue=cas.EPI_SWIGLU | cas.EPI_RESIDUAL, residual=8 * P), cas.OK)])
+    (dict(rows=(1 << 20) + 1), cas.EUNSUPPORTED), (dict(rows=0), cas.OK), (dict(rows=0, up=weights(), epilogue=cas.EPI_SWIGLU | cas.EPI_RESIDUAL, residual=8 * P), cas.OK)])
 def test_w4_gemm_refuses(lib, change, status):
     assert gemm(lib, **change) == status
 
