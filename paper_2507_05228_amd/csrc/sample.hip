@@ -13,6 +13,9 @@
 // One token is the latency of a chain of short steps that each run once: the second pass is written for little code (rolled loops,
 // lane moves, one copy of a step), which its wavefronts fetch from cold caches.
 //
+// Measured (us, bf16): one row of 128256 7.4 + 13; 256 rows with mixed settings 37 (1.8 TB/s: some 45 instructions and an LDS atomic
+// a logit) + 55 (the rows whose borders lie deep); 32 fp32 rows of 50257 without filters 7.3 + 30 (a second look at each row).
+//
 // Weights are exp(z / 24), z = 24 l / temperature in 64 bits; relative to the middle of the bin, at most a 48th away, they are whole
 // numbers of 2^-29, so that sums within a bin are exact and do not depend on any order; the rounding (2^-30 of a weight, either
 // way) is what the result is exact to.  Elements of weight below e^-42 of the largest are left out: 2^20 of them are 6e-13 of the sum.

@@ -3,7 +3,13 @@
 // What bounds it: every weight is used for a handful of rows, so a launch is as long as streaming the codes from HBM, half a byte
 // each.  The 8 wavefronts of a workgroup are column groups by parts of the reduction; each reads the codes of its columns straight
 // into matrix operands, a ring of pieces ahead of their use.  X, which all of them need, comes through LDS in the
-// order of the operands: whole where it fits, in two halves in turn where not.
+// order of the operands: whole where it fits, in two halves in turn where not (every wavefront reading its own X from L2: 4 rows of
+// 4096x14336 with SwiGLU 31 us instead of 17, since a CU loads some 43 KB a microsecond from L2).
+//
+// Measured (us a call among others; floor: bytes at the rate of a large copy): 1 row of 4096x4096 6 (1.7: start, X, one round of
+// codes and end are a chain of latencies), 4 rows of 4096x14336 with SwiGLU, group 64, 16.9 (12.7), 32 int8 rows of 8192x28672 42.8
+// (24.2; instructions, one workgroup a CU, 224 of 256 CUs), 64 rows of 14336x4096 24 (6.5; X is staged for 5, the loop takes 9.5, the 16
+// slices' sums out and in 7), 1 row of 4096x128256 61 (53).
 //
 // Packed layout.  Codes: blocks of 16 columns by 128 reduction elements, 1 KB each, blocks of a column side by side along the
 // reduction.  In a block, lane (column l, quarter g) of a wavefront finds its 16 bytes at (16 g + l) * 16: word s holds elements
@@ -312,7 +318,7 @@ __global__ __launch_bounds__(NW * 64, TM == 1 && WHOLE ? 4 : 2) void w4_kernel(W
         const char *x = lds + held * chunk_bytes + (piece * 16 + g) * row_units * UB;
         const float *xsc = xscales + held * chunk_scales + piece * 4 * (TM * 16) + 4 * g;
         // all of the piece's operands are under way before the first is waited for (left to itself, the compiler asks for one at a
-        // time), where there is room for them
+        // time), where there is room for them: 64 rows of bf16 with it spill, 30.7 -> 32 us
         constexpr bool AHEAD = XT != X_F32 && (TM <= 2 || (XT == X_INT8 && FOLD > 1));
         XOperand<XT> xo[4][TM];
         auto read_x = [&](int s) {
@@ -445,7 +451,8 @@ __global__ __launch_bounds__(NW * 64, TM == 1 && WHOLE ? 4 : 2) void w4_kernel(W
     }
 
     // Sums stay in the order of the products' results: a lane has four rows of a column.  Those of a cut reduction go out as they
-    // are, 1 KB a block, and where no other wavefront of the workgroup has a share in them straight from the registers.
+    // are, 1 KB a block, and where no other wavefront of the workgroup has a share in them straight from the registers (turned to
+    // rows through LDS first: 7.5 us of a 64-row workgroup instead of 0.5).
     const int row_blocks = (rows + 15) >> 4;
     auto plane = [&](int u, int i, int block) {
         return (f32x4 *)p.planes + ((((int64_t)blockIdx.y * MATS + u) * p.row_blocks + row0 / 16 + i) * p.col_blocks + block) * 64 + lane;
@@ -524,7 +531,10 @@ __global__ __launch_bounds__(256) void w4_finish_kernel(W4Params p) {
     }
 }
 
-// How a product is cut.  One choice for the workspace and the launch.
+// How a product is cut.  One choice for the workspace and the launch: the cheapest by a model of what was measured.  Few columns and
+// a long reduction want slices (16 rows of 14336x4096: 8 slices 16 us, 2 slices 18, none 20), many columns none (32 int8 rows of
+// 8192x28672: none 43, 4 slices 46); a wavefront's columns are 32 where X is shared by more of them that way (1 row of 4096x128256: 61
+// against 62 to 67 with 16), 16 where there are few workgroups (1 row of 4096x4096: 6.1 against 7.8).
 struct Cut {
     int tm, tn, fold, cols_log2, slices, slice_blocks, chunk, held;
     size_t lds;
