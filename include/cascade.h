@@ -648,8 +648,8 @@ CASCADE_API int32_t cascade_pages_copy(const cascade_paged_cache *cache, int32_t
  * delta NULL: s = x.  Any of sum, y and q (with q_scale) may be NULL, one is wanted.  s, its
  * statistics and y are fp32 and each output is rounded once: y does not see the rounding of sum.
  * Of a group with largest magnitude A, q_scale = max(A / 127, 2^-100) and q = y / q_scale rounded
- * to nearest even (E4M3: 448 in the place of 127); a group that holds an infinity or NaN has
- * q_scale = NaN and q = 0.
+ * to nearest even (E4M3: 448 in the place of 127), the quotient as y times 1 / q_scale, 2^-23 of it
+ * off at most; a group that holds an infinity or NaN has q_scale = NaN and q = 0.
  * sum and y may each be x or delta (with the same stride); outputs must not overlap otherwise.  */
 typedef struct cascade_add_norm_desc {
     int32_t dtype;        /* of x, delta, gain, bias, sum and y                       */

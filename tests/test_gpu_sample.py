@@ -219,6 +219,17 @@ def test_strides_and_addresses_off_any_boundary(cas):
             run(cas, logits, u, t=30.0)
 
 
+def test_offsets_beyond_32_bits(cas):
+    import torch
+    V, stride = 50257, (1 << 31) + 64
+    for dtype in (torch.bfloat16, torch.float32):
+        room = torch.empty(2 * stride + V, device="cuda", dtype=dtype)
+        logits = room.as_strided((3, V), (stride, 1))
+        logits.copy_(2.5 * torch.randn((3, V), device="cuda"))
+        run(cas, logits, [0.2, 0.6, 0.9], p=0.9)
+        run(cas, logits, [0.2, 0.6, 0.9], t=[0.0, 1.0, 30.0])
+
+
 def test_many_rows(cas):
     logits, rng = make(3000, 700, "f32", seed=6)
     run(cas, logits, rng.random(3000), t=rng.choice([0.0, 0.7, 1.0], 3000), k=rng.choice([0, 40], 3000), p=rng.choice([0.9, 1.0], 3000))

@@ -156,6 +156,66 @@ def test_strides(cas):
         check(*run(cas, 19, 512, 203, x=x, residual=True, bias=True, strides=True))
 
 
+@pytest.mark.parametrize("seed", range(12))
+def test_drawn_calls(cas, seed):
+    rng = np.random.default_rng(seed)
+
+    def size(most):
+        return int(round(np.exp(rng.uniform(0, np.log(most)))))
+
+    for _ in range(5):
+        dtype, x, act = rng.choice(["bf16", "bf16", "f32"]), rng.choice(["same", "int8", "e4m3"]), rng.choice(["none", "none", "gelu", "swiglu"])
+        group, x_group = int(rng.choice([32, 64, 128])), int(rng.choice([0, 32, 64, 128, 256])) if x != "same" else 0
+        unit = max(group, x_group)
+        call = dict(dtype=dtype, x=x, group=group, x_group=x_group, act=act, zeros=bool(rng.integers(2)), bias=act != "swiglu" and bool(rng.integers(2)),
+                    residual=bool(rng.integers(2)), strides=bool(rng.integers(2)))
+        rows, k, n = size(200), unit * size(8192 // unit), size(3000)
+        print(rows, k, n, call, flush=True)
+        check(*run(cas, rows, k, n, seed=seed, **call), rms=rows * n > 200)
+
+
+def test_longest_reduction(cas):
+    """8192 groups are added one to another: 2^13 roundings of 2^-24 of at most 15 scale |x| an element, 2^-11 * 15 / 62 of the magnitude
+    that `slack` is 2^-15 of: less than four times `slack` on top of it."""
+    for rows, x in ((3, "same"), (20, "int8"), (40, "same")):
+        y, want, slack, half = run(cas, rows, 1 << 20, 16, x=x, zeros=True, seed=11)
+        check(y, want, 5 * slack, half, rms=False)
+
+
+def test_gate_and_up_of_the_same_weights(cas):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(12)
+    codes, scales, _ = make_weights(200, 512, 64, torch.float32, False, g)
+    w = cas.make_w4_weights(codes, scales)
+    x = torch.randn((3, 512), device="cuda", generator=g)
+    y, plain = torch.empty((3, 200), device="cuda"), torch.empty((3, 200), device="cuda")
+    ws = cas.new_workspace(cas.cascade_w4_gemm_workspace_bytes(w, x, w))
+    cas.cascade_w4_gemm(w, x, y, weights_up=w, epilogue=cas.EPI_SWIGLU, workspace=ws)
+    cas.cascade_w4_gemm(w, x, plain, workspace=cas.new_workspace(cas.cascade_w4_gemm_workspace_bytes(w, x)))
+    p = plain.double()
+    # the two may be cut differently: 2^-18 of either factor's largest, and the fast exponential's 2^-20
+    top = p.abs().max()
+    assert ((y.double() - p * p * torch.sigmoid(p)).abs() <= 2.0 ** -16 * (top * top + 1)).all()
+
+
+def test_offsets_beyond_32_bits(cas):
+    """Codes of more than 4 GiB, a scale for 128 of them; the first, some inner and the last columns."""
+    import torch
+    n, k, rows = (1 << 20) + 24, 8320, 2
+    g = torch.Generator(device="cuda").manual_seed(13)
+    codes = torch.randint(0, 16, (n, k), device="cuda", generator=g, dtype=torch.uint8)
+    scales = ((0.5 + torch.rand((n, k // 128), device="cuda", generator=g)) / (4.6 * k ** 0.5)).bfloat16()
+    w = cas.make_w4_weights(codes, scales)
+    assert cas.load_library().cascade_w4_bytes(w) > 1 << 32
+    x = torch.randn((rows, k), device="cuda", generator=g).bfloat16()
+    y = torch.empty((rows, n), device="cuda", dtype=torch.bfloat16)
+    cas.cascade_w4_gemm(w, x, y, workspace=cas.new_workspace(cas.cascade_w4_gemm_workspace_bytes(w, x)))
+    for c in (slice(0, 64), slice(n // 2 - 32, n // 2 + 32), slice(n - 100, n)):
+        want = x.double() @ dense(codes[c], scales[c], None, 128).t()
+        top = 62 * (x.double().abs() @ scales[c].double().repeat_interleave(128, 1).t())
+        check(y[:, c], want, 2.0 ** -15 * top, torch.finfo(torch.bfloat16).eps / 2)
+
+
 def test_residual_in_place(cas):
     import torch
     g = torch.Generator(device="cuda").manual_seed(3)
