@@ -833,7 +833,7 @@ def _device_of(x, where):
     """The current device; x [rows, columns] decides whether there is one."""
     if x.dim() != 2 or not x.is_cuda:
         raise CascadeError(ESHAPE, f"{where}: [rows, columns] on the GPU")
-    return _torch.cuda.current_device()
+    return _torch._C._cuda_getDevice()                     # (a tensor is there, so torch's start-up is over)
 
 
 def _handle(stream, device):
@@ -850,6 +850,12 @@ def _workspace(workspace, device, where):
     if workspace.get_device() != device or not workspace.is_contiguous():
         raise CascadeError(EWORKSPACE, f"{where}: a contiguous workspace on the current device")
     return workspace.data_ptr(), workspace.nbytes
+
+
+def _packed_on(weights, device, where):
+    t = weights.tensors[0]
+    if t is not None and t.get_device() != device:
+        raise CascadeError(EINVAL, f"{where}: weights on device {t.get_device()}, the current device is {device}")
 
 
 def _scale_groups(scale, rows, columns, where):
@@ -927,9 +933,9 @@ def cascade_w4_gemm(weights, x, y, x_scale=None, weights_up=None, bias=None, res
     x_at, sx = _operand(x, (rows, weights.k), x.dtype if fmt else dtype, device, where, "x")
     res_at, sr = _operand(residual, (rows, n), dtype, device, where, "residual")
     y_at, sy = _operand(y, (rows, n), dtype, device, where, "y")
-    for w in (weights, weights_up):
-        if w is not None and w.tensors[0] is not None and w.tensors[0].get_device() != device:
-            raise CascadeError(EINVAL, f"{where}: weights on device {w.tensors[0].get_device()}, the current device is {device}")
+    _packed_on(weights, device, where)
+    if weights_up is not None:
+        _packed_on(weights_up, device, where)
     ws, ws_bytes = _workspace(workspace, device, where)
     desc = W4GemmDesc(rows, fmt, weights.k // groups if groups > 1 else 0, epilogue, sx, sr, sy)
     st = lib.cascade_w4_gemm(C.byref(weights), None if weights_up is None else C.byref(weights_up), C.byref(desc), x_at, scale_at,

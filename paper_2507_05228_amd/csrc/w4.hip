@@ -553,20 +553,22 @@ Cut cut_of(const cascade_w4_weights *w, const cascade_w4_gemm_desc *d) {
     const int x_group = d->x_format ? d->x_group : 0;
     c.fold = w->dtype == CASCADE_F32 ? 1 : std::min(w->group, x_group ? std::min(x_group, BLOCK) : BLOCK) / 32;
     auto lds_of = [&](int chunk, int held) { return (size_t)held * chunk * (16 * (rows | 1) * unit + (d->x_format ? 4 * c.tm * 16 * 4 : 0)); };
+    const int row_tiles = (d->rows + c.tm * 16 - 1) / (c.tm * 16);
     double best = 1e30;
     for (int lg = 0; lg <= 3; ++lg) {
         const int parts = NW >> lg, chunk = 2 * parts;
         const int64_t tiles = (units + (1 << lg) - 1) >> lg;
         for (int slices = 1; slices <= 32; ++slices) {
             const int per = ((blocks + slices - 1) / slices + parts - 1) / parts * parts;
-            if (slices > 1 && ((int64_t)per * (slices - 1) >= blocks || per < 2 * parts)) continue;
+            const int64_t groups = tiles * slices * row_tiles;
+            if (slices > 1 && (per < 2 * parts || groups > 1024)) break;         // no more slices either: the host's time counts, too
+            if (slices > 1 && (int64_t)per * (slices - 1) >= blocks) continue;
             const bool whole = lds_of(std::min(per, blocks), 1) <= LDS_MOST;
             if (!whole && chunk * rows * 16 > MAX_UNITS * NW * 64) continue;
             const size_t lds = std::max(whole ? lds_of(std::min(per, blocks), 1) : lds_of(chunk, 2), (size_t)NW * c.tm * c.tn * 1024);
             if (lds > LDS_MOST) continue;
             const int resident = c.tm == 1 && whole && lds <= LDS_MOST / 2 ? 2 : 1;
             // microseconds: rounds of workgroups, each a start and its pieces at the rate that the resident ones share
-            const int64_t groups = tiles * slices * ((d->rows + c.tm * 16 - 1) / (c.tm * 16));
             const int64_t full = groups / (256 * resident), rest = groups - full * 256 * resident;
             // eight wavefronts' pieces at 20 KB a microsecond and CU, or at their products' pace; X at twice that rate
             const double turn = std::max(8 * 1.024 * c.tn / 20.0, 0.17 * c.tm * c.tn);
@@ -582,6 +584,11 @@ Cut cut_of(const cascade_w4_weights *w, const cascade_w4_gemm_desc *d) {
         }
     }
     return c;
+}
+
+size_t planes_bytes(const Cut &c, const cascade_w4_weights *w, const cascade_w4_gemm_desc *d) {
+    if (c.slices == 1) return 0;
+    return (size_t)c.slices * ((d->rows + 15) / 16) * ((w->n_out + 15) / 16) * 1024 * (d->epilogue & CASCADE_EPI_SWIGLU ? 2 : 1);
 }
 
 template <int XT, bool F32, int TM, int TN, bool SWIGLU, int FOLD, bool WHOLE>
@@ -719,8 +726,7 @@ extern "C" int32_t cascade_w4_pack(const cascade_w4_weights *w, const void *code
 
 extern "C" size_t cascade_w4_gemm_workspace_bytes(const cascade_w4_weights *w, const cascade_w4_gemm_desc *d) {
     if (check_gemm(w, d) != CASCADE_OK || d->rows == 0) return 0;
-    const Cut c = cut_of(w, d);
-    return c.slices > 1 ? (size_t)c.slices * ((d->rows + 15) / 16) * ((w->n_out + 15) / 16) * 1024 * (d->epilogue & CASCADE_EPI_SWIGLU ? 2 : 1) : 0;
+    return planes_bytes(cut_of(w, d), w, d);
 }
 
 extern "C" int32_t cascade_w4_gemm(const cascade_w4_weights *w, const cascade_w4_weights *up, const cascade_w4_gemm_desc *d, const void *X,
@@ -763,7 +769,7 @@ extern "C" int32_t cascade_w4_gemm(const cascade_w4_weights *w, const cascade_w4
     p.x_groups = x_group ? p.K / x_group : 1;
     p.has_zeros = w->zero_points; p.flags = d->epilogue;
     const Cut c = cut_of(w, d);
-    if (c.slices > 1 && (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < cascade_w4_gemm_workspace_bytes(w, d))) return CASCADE_EWORKSPACE;
+    if (c.slices > 1 && (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < planes_bytes(c, w, d))) return CASCADE_EWORKSPACE;
     p.planes = (float *)workspace;
     p.cols_log2 = c.cols_log2; p.slices = c.slices; p.slice_blocks = c.slice_blocks; p.chunk = c.chunk; p.chunks_held = c.held;
     hipStream_t s = (hipStream_t)stream;
