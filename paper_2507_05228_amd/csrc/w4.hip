@@ -215,12 +215,16 @@ __device__ __forceinline__ void finish(const W4Params &p, float (&v)[2], int row
     ((T *)p.Y)[row * p.ldy + n] = (T)y;
 }
 
+// Up to 16 rows that fit whole leave registers for two workgroups on a CU, but not E4M3 rows over 32 columns: held to 128 registers they
+// spill what the ring has requested, and wait for it (8 rows of 8192x28672 51 us; one workgroup, no spills: 41).
+constexpr bool two_resident(bool e4m3, int tm, int tn, bool whole) { return tm == 1 && whole && !(e4m3 && tn == 2); }
+
 // TM: 16-row blocks.  TN: 16-column blocks of a wavefront (SWIGLU: gate and up of the same columns).
 // FOLD: 32-element steps that share all scales, 1, 2 or 4.
 // WHOLE: the slice's X fits into LDS and enters it once; else it comes in chunks of two pieces a wavefront, into halves in turn.
 // F32: scales, bias, residual and Y in fp32, else bf16.
 template <int XT, bool F32, int TM, int TN, bool SWIGLU, int FOLD, bool WHOLE>
-__global__ __launch_bounds__(NW * 64, TM == 1 && WHOLE ? 4 : 2) void w4_kernel(W4Params p) {
+__global__ __launch_bounds__(NW * 64, two_resident(XT == X_E4M3, TM, TN, WHOLE) ? 4 : 2) void w4_kernel(W4Params p) {
     static_assert(!SWIGLU || TN == 2, "gate and up");
     typedef typename std::conditional<F32, float, bf16_t>::type T;
     constexpr bool X8 = XT == X_E4M3 || XT == X_INT8;
@@ -590,7 +594,7 @@ Cut cut_of(const cascade_w4_weights *w, const cascade_w4_gemm_desc *d) {
             if (!whole && chunk * rows * 16 > MAX_UNITS * NW * 64) continue;
             const size_t lds = std::max(whole ? lds_of(std::min(per, blocks), 1) : lds_of(chunk, 2), (size_t)NW * c.tm * c.tn * 1024);
             if (lds > LDS_MOST) continue;
-            const int resident = c.tm == 1 && whole && lds <= LDS_MOST / 2 ? 2 : 1;
+            const int resident = two_resident(d->x_format == CASCADE_Q8_E4M3, c.tm, c.tn, whole) && lds <= LDS_MOST / 2 ? 2 : 1;
             // microseconds: rounds of workgroups, each a start and its pieces at the rate that the resident ones share
             const int64_t full = groups / (256 * resident), rest = groups - full * 256 * resident;
             // eight wavefronts' pieces at 20 KB a microsecond and CU, or at their products' pace; X at twice that rate
