@@ -97,7 +97,6 @@ class PagedAttnDesc(C.Structure):
                 ("q_stride", C.c_int64), ("o_stride", C.c_int64)]
 
 
-
 class AddNormDesc(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("rows", C.c_int32), ("d_model", C.c_int32), ("norm_kind", C.c_int32), ("eps", C.c_float),
                 ("q_format", C.c_int32), ("q_group", C.c_int32), ("x_stride", C.c_int64), ("delta_stride", C.c_int64),
