@@ -857,7 +857,7 @@ __global__ __launch_bounds__(LIST) void sample_row_kernel(SampleParams p) {
         return;
     }
     double mass_kept = left;
-    if (k < all && top_p >= 1.f) mass_kept = search(row, base, sh, steps, true, k, 0.0, false, false).mass;
+    if (left < 0.0) mass_kept = search(row, base, sh, steps, true, k, 0.0, false, false).mass;
     if (top_p < 1.f) {
         const Place q = search(row, base, sh, steps, false, 0, (double)top_p * left, false, false);
         if (q.count < kept) {
