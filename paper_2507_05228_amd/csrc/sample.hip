@@ -849,7 +849,9 @@ __global__ __launch_bounds__(LIST) void sample_row_kernel(SampleParams p) {
         }
         kept = min(kept, max(1u, steps.total(is && z >= least)));
         const double mass_kept = sums[kept - 1];
-        const uint32_t at = min((uint32_t)steps.first_thread(is && upto > uniform * mass_kept), kept - 1);
+        // (1 and more take the last place: sums in a fixed tree are not monotone, an earlier one may be a last bit above the last)
+        const double target = uniform * mass_kept;
+        const uint32_t at = min((uint32_t)steps.first_thread(is && target < mass_kept && upto > target), kept - 1);
         if ((uint32_t)tid == at) {
             p.token[r] = (int32_t)(uint32_t)mine;
             if (p.prob) p.prob[r] = (float)(own / mass_kept);

@@ -1,5 +1,6 @@
-"""Tokens from logits at the ends of the settings: a top_p that is no number behind a top_k that cuts.
+"""Tokens from logits at the ends of the settings: a top_p that is no number behind a top_k that cuts, random numbers of 1 and more.
 Tolerances as in test_gpu_sample."""
+import numpy as np
 import pytest
 
 from test_gpu_sample import make, run
@@ -26,3 +27,21 @@ def test_top_p_that_is_no_number_is_off(cas, dtype, V, spread, k, least):
     token, prob = run(cas, logits, u, k=k, p=float("nan"), least=least)
     off, off_prob = run(cas, logits, u, k=k, p=1.0, least=least)
     assert torch.equal(token, off) and torch.equal(prob, off_prob)
+
+
+@pytest.mark.parametrize("u", [1.0, 1.0 + 2.0 ** -23, 7.0, float("inf")])
+def test_a_random_number_of_one_takes_the_last_place(cas, u):
+    """A few large weights and many below the last bit of their sum: running sums in fixed trees are not monotone there, and the
+    last one is not the largest."""
+    import torch
+    rows, V, tiny = 300, 700, 90
+    g = np.random.default_rng(0)
+    logits = np.full((rows, V), -np.inf, np.float32)
+    for r in range(rows):
+        n = int(g.integers(3, 40))
+        at = g.permutation(V)[:n + tiny]
+        logits[r, at] = np.concatenate([g.normal(size=n), g.uniform(-38.0, -36.2, tiny)])
+    logits = torch.from_numpy(logits).cuda()
+    run(cas, logits, u)
+    run(cas, logits, u, k=60)
+    run(cas, logits, u, least=1e-18)
