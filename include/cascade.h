@@ -716,7 +716,8 @@ CASCADE_API int32_t cascade_w4_gemm(const cascade_w4_weights *weights, const cas
 /* Next tokens from logits by given random numbers, each row with its own settings (device arrays of
  * `rows` values, so that a captured step serves changing requests; NULL: off, temperature 1).
  * Order of a row: logits descending, equal ones by index; NaN counts as -inf.
- *   w_i = exp((l_i - l_max) / temperature); 1 where l_i = l_max, 0 where they are infinitely far apart
+ *   w_i = exp((l_i - l_max) / temperature); 1 where l_i = l_max, 0 where they are infinitely far apart and
+ *   where it would be below about e^-42.6 (3e-19): such tokens are never drawn, and add nothing to any sum
  *   top_k   keeps the first top_k in order                     (<= 0: all)
  *   top_p   of these, the shortest prefix with at least top_p of their mass (NaN or >= 1: all)
  *   min_p   of these, those with w_i >= min_p                  (NaN or <= 0: all)
@@ -724,7 +725,8 @@ CASCADE_API int32_t cascade_w4_gemm(const cascade_w4_weights *weights, const cas
  * the kept w exceeds uniform * W, W their sum (NaN or below 0: the first; too large: the last with w above 0).
  * prob (NULL: not wanted) = w_token / W.  temperature <= 0 or NaN: the first in order, prob 1, the
  * choice of cascade_greedy_token.  A row of -inf and NaN alone: token 0, prob 0.
- * Weights and sums are exact to about 2^-30: a uniform nearer than that to a border between two tokens may fall to either.
+ * Weights and sums are exact to about 2^-30 (or 2^-52 |l| / temperature, where that is more): a uniform nearer than that to a
+ * border between two tokens may fall to either.
  * The same arguments give the same tokens each time, whatever the other rows.       */
 typedef struct cascade_sample_desc {
     int32_t dtype;        /* of the logits                                            */

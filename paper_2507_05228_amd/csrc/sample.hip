@@ -18,7 +18,9 @@
 //
 // Weights are exp(z / 24), z = 24 l / temperature in 64 bits; relative to the middle of the bin, at most a 48th away, they are whole
 // numbers of 2^-29, so that sums within a bin are exact and do not depend on any order; the rounding (2^-30 of a weight, either
-// way) is what the result is exact to.  Elements of weight below e^-42 of the largest are left out: 2^20 of them are 6e-13 of the sum.
+// way) is what the result is exact to, up to |z| = 2^26; z's own rounding, 2^-52 |l| / temperature of a weight, is what counts further
+// out, where neighbouring fp32 numbers are four bins apart or more.  Elements behind the last bin, of weight below e^-42.6 of the largest, count as
+// none: 2^20 of them are 3e-13 of the sum.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>

@@ -1,5 +1,5 @@
-"""Tokens from logits at the ends of the settings: a top_p that is no number behind a top_k that cuts, random numbers of 1 and more.
-Tolerances as in test_gpu_sample."""
+"""Tokens from logits at the ends of the settings: a top_p that is no number behind a top_k that cuts, random numbers of 1 and more,
+weights too small for the bins.  Tolerances as in test_gpu_sample."""
 import numpy as np
 import pytest
 
@@ -45,3 +45,27 @@ def test_a_random_number_of_one_takes_the_last_place(cas, u):
     run(cas, logits, u)
     run(cas, logits, u, k=60)
     run(cas, logits, u, least=1e-18)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [500, 40000])
+@pytest.mark.parametrize("setting", [dict(), dict(k=300), dict(p=0.999), dict(least=1e-25), dict(t=0.25, k=450, least=1e-30)])
+def test_weights_below_the_bins_count_as_none(cas, dtype, V, setting):
+    """Finite logits 50 to 100 temperatures below the largest are as if they were -inf, for random numbers of 1 and more too."""
+    import torch
+    logits, rng = make(8, V, dtype, seed=V, spread=1.0)
+    t = setting.get("t", 1.0)
+    logits = torch.where(logits < 0.5, t * (logits.amax(1, keepdim=True).float() - 75 - 3 * logits.float()), t * logits.float()).to(logits.dtype)
+    most = logits.amax(1, keepdim=True).float()
+    below = (most - logits.float()) / t
+    assert ((below < 20) | (below > 50)).all()             # none near the bins' end
+    cut = torch.where(below > 50, float("-inf"), logits.float()).to(logits.dtype)
+    for u in (0.3, 0.999, 1.0, 3.0, float("inf")):
+        want = run(cas, cut, u, **setting)
+        rows = len(logits)
+        token, prob = torch.empty(rows, device="cuda", dtype=torch.int32), torch.empty(rows, device="cuda")
+        dev = {name: None if key not in setting else torch.full((rows,), setting[key], device="cuda", dtype=torch.int32 if key == "k" else torch.float32)
+               for name, key in (("temperature", "t"), ("top_k", "k"), ("top_p", "p"), ("min_p", "least"))}
+        cas.cascade_sample(logits, torch.full((rows,), u, device="cuda"), token, prob=prob,
+                           workspace=cas.new_workspace(cas.cascade_sample_workspace_bytes(rows, V, logits.dtype)), **dev)
+        assert torch.equal(token, want[0]) and torch.equal(prob, want[1])
