@@ -914,8 +914,9 @@ def make_w4_weights(codes, scales, zeros=None):
 
 def cascade_w4_gemm_workspace_bytes(weights, x, weights_up=None):
     """For x as it will be given; weights_up: with EPI_SWIGLU."""
+    lib = _lib or load_library()                           # (which fills _Q8)
     desc = W4GemmDesc(x.shape[0], _Q8.get(x.dtype, Q8_NONE), 0, EPI_SWIGLU if weights_up is not None else 0, 0, 0, 0)
-    return load_library().cascade_w4_gemm_workspace_bytes(C.byref(weights), C.byref(desc))
+    return lib.cascade_w4_gemm_workspace_bytes(C.byref(weights), C.byref(desc))
 
 
 def cascade_w4_gemm(weights, x, y, x_scale=None, weights_up=None, bias=None, residual=None, epilogue=0, workspace=None, stream=None):

@@ -1,0 +1,30 @@
+"""Workspaces of a token's step on the host: the binding gives the same size whether or not the library was loaded before."""
+import os
+import subprocess
+import sys
+
+import pytest
+
+import paper_2507_05228_amd as cas
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(cas.LIB_PATH):
+        import __graft_entry__
+        __graft_entry__.build()
+    return cas.load_library()
+
+
+def test_the_first_question_for_a_workspace_has_the_same_answer(lib):
+    code = ("import torch, paper_2507_05228_amd as cas\n"
+            "for dtype, n, k in ((cas.BF16, 4096, 14336), (cas.F32, 4096, 14336), (cas.F32, 8192, 8192)):\n"
+            "    w = cas.W4Weights(dtype, n, k, 128, 0, 0, None)\n"
+            "    for x in (torch.empty((rows, k), dtype=t) for rows in (32, 64) for t in (torch.int8, torch.float8_e4m3fn)):\n"
+            "        cas._lib, cas._Q8 = None, {}\n"
+            "        print(*(cas.cascade_w4_gemm_workspace_bytes(w, x) for _ in range(2)))\n")
+    out = subprocess.run([sys.executable, "-c", code], cwd=ROOT, check=True, capture_output=True, text=True, timeout=600).stdout
+    pairs = [line.split() for line in out.splitlines() if line[:1].isdigit()]
+    assert len(pairs) == 12 and all(a == b for a, b in pairs), out
