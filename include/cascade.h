@@ -736,7 +736,7 @@ typedef struct cascade_sample_desc {
 } cascade_sample_desc;
 
 /* uniform [rows] in [0, 1); token [rows] int32.  workspace: 16-byte aligned; calls that may overlap in time need one each, its contents
- * need not be kept between calls.
+ * need not be kept between calls; the size for a number of rows is enough for fewer, too.
  * Errors: EINVAL, ESHAPE (stride), EUNSUPPORTED (dtype, rows, vocab), EWORKSPACE, EHIP.   */
 CASCADE_API size_t cascade_sample_workspace_bytes(const cascade_sample_desc *desc);
 CASCADE_API int32_t cascade_sample(const cascade_sample_desc *desc, const void *logits, const float *temperature, const int32_t *top_k,

@@ -896,7 +896,9 @@ __global__ __launch_bounds__(LIST) void sample_row_kernel(SampleParams p) {
 // Threads of a workgroup of the first pass: small chunks while they are few (latency), larger ones where the bins they write would
 // otherwise weigh as much as the logits
 int bins_threads(int32_t rows, int32_t vocab) { return (int64_t)rows * ((vocab + 8191) / 8192) <= 1024 ? 256 : 512; }
+int32_t most_rows_of_small_chunks(int32_t vocab) { return 1024 / ((vocab + 8191) / 8192); }
 int chunks_of(int threads, int32_t vocab) { return (vocab + chunk_of(threads) - 1) / chunk_of(threads); }
+size_t chunk_bytes(int32_t rows, int32_t vocab) { return (size_t)rows * chunks_of(bins_threads(rows, vocab), vocab) * CHUNK_WORDS * 8; }
 
 int32_t check(const cascade_sample_desc *d) {
     if (!d || d->rows < 0 || d->vocab <= 0 || d->stride < 0 || d->reserved) return CASCADE_EINVAL;
@@ -918,10 +920,10 @@ int32_t launch(const SampleParams &p, int32_t rows, int threads, hipStream_t s) 
 
 }  // namespace
 
+// Enough for fewer rows too: the last ones that take small chunks need more than those after them
 extern "C" size_t cascade_sample_workspace_bytes(const cascade_sample_desc *d) {
     if (check(d) != CASCADE_OK) return 0;
-    const int threads = bins_threads(d->rows, d->vocab);
-    return (size_t)d->rows * chunks_of(threads, d->vocab) * CHUNK_WORDS * 8;
+    return std::max(chunk_bytes(d->rows, d->vocab), chunk_bytes(std::min(d->rows, most_rows_of_small_chunks(d->vocab)), d->vocab));
 }
 
 extern "C" int32_t cascade_sample(const cascade_sample_desc *d, const void *logits, const float *temperature, const int32_t *top_k,
@@ -931,7 +933,7 @@ extern "C" int32_t cascade_sample(const cascade_sample_desc *d, const void *logi
     if (st != CASCADE_OK) return st;
     if (d->rows == 0) return CASCADE_OK;
     if (!logits || !uniform || !token) return CASCADE_EINVAL;
-    if (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < cascade_sample_workspace_bytes(d)) return CASCADE_EWORKSPACE;
+    if (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < chunk_bytes(d->rows, d->vocab)) return CASCADE_EWORKSPACE;
     SampleParams p;
     p.logits = logits; p.temperature = temperature; p.top_k = top_k; p.top_p = top_p; p.min_p = min_p; p.uniform = uniform;
     p.token = token; p.prob = prob; p.chunks = (uint64_t *)workspace;

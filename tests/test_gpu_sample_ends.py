@@ -69,3 +69,16 @@ def test_weights_below_the_bins_count_as_none(cas, dtype, V, setting):
         cas.cascade_sample(logits, torch.full((rows,), u, device="cuda"), token, prob=prob,
                            workspace=cas.new_workspace(cas.cascade_sample_workspace_bytes(rows, V, logits.dtype)), **dev)
         assert torch.equal(token, want[0]) and torch.equal(prob, want[1])
+
+
+@pytest.mark.parametrize("most,few,V", [(65, 64, 128256), (200, 146, 50257), (300, 1, 32000)])
+def test_a_workspace_for_many_rows_serves_fewer(cas, most, few, V):
+    import torch
+    logits, rng = make(few, V, "bf16", seed=V)
+    u, t = torch.from_numpy(rng.random(few)).float().cuda(), torch.full((few,), 0.7, device="cuda")
+    results = []
+    for rows in (most, few):
+        token, prob = torch.empty(few, device="cuda", dtype=torch.int32), torch.empty(few, device="cuda")
+        cas.cascade_sample(logits, u, token, temperature=t, prob=prob, workspace=cas.new_workspace(cas.cascade_sample_workspace_bytes(rows, V, logits.dtype)))
+        results.append((token, prob))
+    assert torch.equal(results[0][0], results[1][0]) and torch.equal(results[0][1], results[1][1])

@@ -1,4 +1,6 @@
-"""Workspaces of a token's step on the host: the binding gives the same size whether or not the library was loaded before."""
+"""Workspaces of a token's step on the host: one that serves a number of rows serves any smaller one,
+and the binding gives the same size whether or not the library was loaded before."""
+import ctypes as C
 import os
 import subprocess
 import sys
@@ -16,6 +18,14 @@ def lib():
         import __graft_entry__
         __graft_entry__.build()
     return cas.load_library()
+
+
+@pytest.mark.parametrize("vocab", [1, 700, 8192, 8193, 32000, 50257, 128256, 1 << 20])
+@pytest.mark.parametrize("dtype", [cas.BF16, cas.F32])
+def test_a_workspace_of_tokens_serves_fewer_rows(lib, vocab, dtype):
+    sizes = [lib.cascade_sample_workspace_bytes(C.byref(cas.SampleDesc(dtype, r, vocab, 0, 0))) for r in [*range(1, 1200), 4096, 65535, 65536]]
+    assert sizes[0] > 0 and sizes == sorted(sizes)
+    assert sizes[-1] <= 65536 * -(-vocab // 8192) * 9300   # (no more than the bins of every chunk)
 
 
 def test_the_first_question_for_a_workspace_has_the_same_answer(lib):
