@@ -696,7 +696,7 @@ CASCADE_API int32_t cascade_w4_pack(const cascade_w4_weights *weights, const voi
  * An infinity or NaN in a row of X reaches that row's outputs as in the formula, others' not.
  * X and its stride: multiples of 16 bytes.  Y may be residual (with the same stride) and must not
  * overlap X.  Calls that may overlap in time need a workspace each (16-byte aligned; contents need
- * not be kept between calls).  A call with the same arguments gives the same bits each time; those of a row may depend on the
+ * not be kept between calls; the size for a number of rows is enough for fewer, too).  A call with the same arguments gives the same bits each time; those of a row may depend on the
  * number of rows.
  * Errors: EINVAL, ESHAPE (strides, W_up), EUNSUPPORTED (dtype, group, sizes, alignment, an
  * epilogue other than these, BIAS with SWIGLU), EWORKSPACE, EHIP.                   */

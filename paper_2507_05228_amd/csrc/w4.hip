@@ -751,9 +751,17 @@ extern "C" int32_t cascade_w4_pack(const cascade_w4_weights *w, const void *code
     return CASCADE_OK;
 }
 
+// Enough for fewer rows too: more of them are cut into fewer slices, so the largest of all counts up to this one.  Up to 64 rows each
+// count has a cut of its own.  Behind them the slices only become fewer as the sums' share of the cost grows, from one 16 rows to
+// the next as many blocks of sums: the first of each 16 has the most.  Reductions are cut up to 1024 workgroups, no more.
 extern "C" size_t cascade_w4_gemm_workspace_bytes(const cascade_w4_weights *w, const cascade_w4_gemm_desc *d) {
-    if (check_gemm(w, d) != CASCADE_OK || d->rows == 0) return 0;
-    return planes_bytes(cut_of(w, d), w, d);
+    if (check_gemm(w, d) != CASCADE_OK) return 0;
+    const int columns = 16 * 8 * (d->epilogue & CASCADE_EPI_SWIGLU ? 1 : 2), tiles = (int)(((int64_t)w->n_out + columns - 1) / columns);      // at least
+    const int last = std::min(d->rows, 512 / std::min(tiles, 513) * 64);
+    cascade_w4_gemm_desc fewer = *d;
+    size_t most = 0;
+    for (fewer.rows = 1; fewer.rows <= last; fewer.rows += fewer.rows < 65 ? 1 : 16) most = std::max(most, planes_bytes(cut_of(w, &fewer), w, &fewer));
+    return most;
 }
 
 extern "C" int32_t cascade_w4_gemm(const cascade_w4_weights *w, const cascade_w4_weights *up, const cascade_w4_gemm_desc *d, const void *X,

@@ -28,6 +28,17 @@ def test_a_workspace_of_tokens_serves_fewer_rows(lib, vocab, dtype):
     assert sizes[-1] <= 65536 * -(-vocab // 8192) * 9300   # (no more than the bins of every chunk)
 
 
+@pytest.mark.parametrize("n,k,group", [(4096, 14336, 128), (14336, 4096, 64), (48, 1 << 17, 32), (17, 96, 32), (8192, 8192, 128), (100000, 512, 128)])
+@pytest.mark.parametrize("dtype", [cas.BF16, cas.F32])
+@pytest.mark.parametrize("x_format", [cas.Q8_NONE, cas.Q8_INT8, cas.Q8_E4M3])
+@pytest.mark.parametrize("epilogue", [0, cas.EPI_SWIGLU])
+def test_a_workspace_of_products_serves_fewer_rows(lib, n, k, group, dtype, x_format, epilogue):
+    w = cas.W4Weights(dtype, n, k, group, 0, 0, None)
+    sizes = [lib.cascade_w4_gemm_workspace_bytes(C.byref(w), C.byref(cas.W4GemmDesc(r, x_format, 0, epilogue, 0, 0, 0)))
+             for r in [*range(1, 300), 1000, 5000, 40000, 1 << 20]]
+    assert sizes == sorted(sizes)
+
+
 def test_the_first_question_for_a_workspace_has_the_same_answer(lib):
     code = ("import torch, paper_2507_05228_amd as cas\n"
             "for dtype, n, k in ((cas.BF16, 4096, 14336), (cas.F32, 4096, 14336), (cas.F32, 8192, 8192)):\n"
