@@ -693,7 +693,8 @@ CASCADE_API int32_t cascade_w4_pack(const cascade_w4_weights *weights, const voi
  * X [rows, k] in the weights' dtype, or in 8 bits with x_scale [rows, k / x_group] (dense).  W_up:
  * EPI_SWIGLU only, of the same sizes, dtype, group and zero_points.  Codes, zeros and 8-bit X enter
  * the products exactly, sums are fp32 (of INT8 X: whole numbers within a group, then fp32).
- * An infinity or NaN in a row of X reaches that row's outputs as in the formula, others' not.
+ * An infinity or NaN in a row of X reaches that row's outputs as in the formula, others' not; such
+ * rows are formed again term by term, which makes a call several times as long.
  * X and its stride: multiples of 16 bytes.  Y may be residual (with the same stride) and must not
  * overlap X.  Calls that may overlap in time need a workspace each (16-byte aligned; contents need
  * not be kept between calls; the size for a number of rows is enough for fewer, too).  A call with the same arguments gives the same bits each time; those of a row may depend on the

@@ -169,44 +169,82 @@ __device__ __forceinline__ Sum<XT> product(const XOperand<XT> *x, const WOperand
     return acc;
 }
 
-// One output from the formula, term by term.  The products above give NaN where a row holds an infinity (16 + code and
-// 16 + zero meet it with opposite signs; in fp32 its further parts are none), and fp32 values next to the largest leave the range of
-// the first of their parts.
+// A row's outputs of 16 columns from the formula, term by term, in 64 bits: column l16 in every quarter's lanes.  The products above give
+// NaN where a row holds an infinity (16 + code and 16 + zero meet it with opposite signs; in fp32 its further parts are none), and fp32
+// values next to the largest leave the range of the first of their parts.  The whole wavefront walks along the reduction, a block of
+// codes a step: one such row among 32 of 28672x8192 makes a call 0.25 ms instead of 0.04 (a lane for each output alone: 4.2 ms).  With the
+// next step's requests under way 0.22, but then kernels that have no use for it spill.
 template <int XT, bool F32>
-__device__ __forceinline__ float plain_output(const W4Params &p, int which, int m, int n) {
-    float sum = 0.f;
-    for (int grp = 0; grp < p.groups; ++grp) {
-        const int64_t at = ((int64_t)(n >> 4) * p.groups + grp) * 16 + (n & 15);
-        const float scale = F32 ? ((const float *)p.scales[which])[at] : (float)((const bf16_t *)p.scales[which])[at];
-        const float zero = p.has_zeros ? (float)(((const uint8_t *)p.zeros[which])[at]) : 8.f;
-        for (int k = grp << p.group_shift; k < (grp + 1) << p.group_shift; ++k) {
-            const int j = k & 7;
-            const uint32_t *word = (const uint32_t *)(p.codes[which] + ((int64_t)(n >> 4) * p.blocks + k / BLOCK) * 1024 +
-                                                      ((k >> 3 & 3) * 16 + (n & 15)) * 16) + (k >> 5 & 3);
-            const float code = (float)((*word >> (4 * ((j >> 1) + 4 * (j & 1)))) & 15u);
-            const int64_t e = m * p.ldx + k;
-            float x;
-            if constexpr (XT == X_BF16) x = (float)((const bf16_t *)p.X)[e];
-            else if constexpr (XT == X_F32) x = ((const float *)p.X)[e];
-            else if constexpr (XT == X_E4M3) x = __builtin_amdgcn_cvt_f32_fp8(((const uint8_t *)p.X)[e], 0);
-            else x = (float)((const int8_t *)p.X)[e];
-            if constexpr (XT == X_E4M3 || XT == X_INT8) x *= p.x_scale[(int64_t)m * p.x_groups + (k >> p.x_group_shift)];
-            sum = fmaf(x, scale * (code - zero), sum);
+__device__ __forceinline__ float plain_outputs(const W4Params &p, int which, int m, int block) {
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
+    const char *x_row = p.X + m * p.ldx * x_bytes<XT>();
+    struct Step {
+        u32x4 words;
+        XRaw<XT> x[4];
+        float scale[4], x_scale[4];
+        int zero[4];
+    };
+    auto request = [&](int b) {                            // of the last block's columns behind K the last ones
+        Step c;
+        c.words = *(const u32x4 *)(p.codes[which] + ((int64_t)block * p.blocks + b) * 1024 + lane * 16);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const int k = min(b * BLOCK + 32 * s, p.K - 32) + 8 * g;
+            const int64_t at = ((int64_t)block * p.groups + (k >> p.group_shift)) * 16 + l16;
+            c.scale[s] = F32 ? ((const float *)p.scales[which])[at] : (float)((const bf16_t *)p.scales[which])[at];
+            c.zero[s] = p.has_zeros ? ((const uint8_t *)p.zeros[which])[at] : 8;
+            c.x[s].v = *(const decltype(c.x[s].v) *)(x_row + k * x_bytes<XT>());
+            if constexpr (XT == X_F32) c.x[s].w = *(const u32x4 *)(x_row + k * 4 + 16);
+            if constexpr (XT == X_E4M3 || XT == X_INT8) c.x_scale[s] = p.x_scale[(int64_t)m * p.x_groups + (k >> p.x_group_shift)];
         }
-        if (sum != sum) break;                             // stays NaN
+        return c;
+    };
+    double sum = 0.0;
+    for (int b = 0; b < p.blocks; ++b) {
+        const Step c = request(b);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            if (b * BLOCK + 32 * s >= p.K) break;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                double x;
+                if constexpr (XT == X_BF16) x = __builtin_bit_cast(float, j & 1 ? c.x[s].v[j >> 1] & 0xffff0000u : c.x[s].v[j >> 1] << 16);
+                else if constexpr (XT == X_F32) x = __builtin_bit_cast(float, j < 4 ? c.x[s].v[j] : c.x[s].w[j - 4]);
+                else if constexpr (XT == X_E4M3) x = __builtin_amdgcn_cvt_f32_fp8(c.x[s].v[j >> 2] >> (8 * (j & 3)), 0) * (double)c.x_scale[s];
+                else x = (double)(int8_t)(c.x[s].v[j >> 2] >> (8 * (j & 3))) * c.x_scale[s];
+                const int code = (int)(c.words[s] >> (4 * ((j >> 1) + 4 * (j & 1))) & 15u);
+                sum = fma(x, (double)c.scale[s] * (code - c.zero[s]), sum);
+            }
+        }
+        // where every column has met a NaN, they stay
+        uint64_t none = __ballot(sum != sum);
+        none |= none >> 32;
+        if (((none | none >> 16) & 0xffff) == 0xffff) break;
     }
-    return sum;
+    sum += __shfl_xor(sum, 16, WAVE);
+    return (float)(sum + __shfl_xor(sum, 32, WAVE));
 }
 
-// Behind the sums: scales of whole rows, the formula where a sum is no number, bias, activation, residual
+// Behind the sums: scales of whole rows, the formula where a sum is no number, bias, activation, residual.  For whole wavefronts whose
+// quarters have a row each, of the same 16 columns; is: whether the lane's output exists.
 template <int XT, bool F32, bool SWIGLU>
-__device__ __forceinline__ void finish(const W4Params &p, float (&v)[2], int row, int n) {
+__device__ __forceinline__ void finish(const W4Params &p, float (&v)[2], int row, int n, bool is) {
     typedef typename std::conditional<F32, float, bf16_t>::type T;
 #pragma unroll
     for (int u = 0; u < (SWIGLU ? 2 : 1); ++u) {
-        if ((XT == X_E4M3 || XT == X_INT8) && p.x_groups == 1) v[u] *= p.x_scale[row];
-        if (!(fabsf(v[u]) < __builtin_inff())) v[u] = plain_output<XT, F32>(p, u, row, n);
+        if ((XT == X_E4M3 || XT == X_INT8) && p.x_groups == 1 && is) v[u] *= p.x_scale[row];
+        const bool mend = is && !(fabsf(v[u]) < __builtin_inff());
+        const uint64_t rows = __ballot(mend);
+        if (__builtin_expect(rows != 0, 0)) {
+#pragma unroll 1
+            for (int q = 0; q < 4; ++q) {
+                if (!(rows >> (16 * q) & 0xffff)) continue;
+                const float formed = plain_outputs<XT, F32>(p, u, __builtin_amdgcn_readlane(row, 16 * q), __builtin_amdgcn_readfirstlane(n) >> 4);
+                if (mend && (threadIdx.x >> 4 & 3) == q) v[u] = formed;
+            }
+        }
     }
+    if (!is) return;
     float y = v[0];
     if (p.flags & CASCADE_EPI_BIAS) y += (float)((const T *)p.bias)[n];
     if (SWIGLU) y = silu_f(y) * v[1];
@@ -516,11 +554,11 @@ __global__ __launch_bounds__(NW * 64, two_resident(XT == X_E4M3, TM, TN, WHOLE) 
         }
         return;
     }
-    // every fourth row of a block over wavefronts
-    for (int job = wave; job < row_blocks * TNO * 4 << p.cols_log2; job += NW) {
-        const int r = job & 3, c = job >> 2 & (cols - 1), at = job >> (2 + p.cols_log2), t = at & (TNO - 1), i = at / TNO;
+    // every fourth row of a block over wavefronts, a row's blocks over different ones (they share what a row with an infinity costs)
+    const int jobs_log2 = p.cols_log2 + TNO - 1;           // of a row
+    for (int job = wave; job < row_blocks * 4 << jobs_log2; job += NW) {
+        const int c = job & (cols - 1), t = job >> p.cols_log2 & (TNO - 1), r = job >> jobs_log2 & 3, i = job >> (jobs_log2 + 2);
         const int row = 16 * i + 4 * g + r, n = (tile0 + c * TNO + t) * 16 + l16;
-        if (row >= rows || n >= p.N) continue;
         float v[2] = {0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
@@ -528,7 +566,7 @@ __global__ __launch_bounds__(NW * 64, two_resident(XT == X_E4M3, TM, TN, WHOLE) 
 #pragma unroll
             for (int u = 0; u < MATS; ++u) v[u] += ((const float *)&meet[c + (w << p.cols_log2)][i][t + u][lane])[r];
         }
-        finish<XT, F32, SWIGLU>(p, v, row0 + row, n);
+        finish<XT, F32, SWIGLU>(p, v, row0 + row, n, row < rows && n < p.N);
     }
 }
 
@@ -540,7 +578,6 @@ __global__ __launch_bounds__(256) void w4_finish_kernel(W4Params p) {
     for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < plane; e += (int64_t)gridDim.x * 256) {
         const int lane = (int)(e & 63), n = (int)((e >> 6) % p.col_blocks) * 16 + (lane & 15);
         const int row = (int)((e >> 6) / p.col_blocks) * 16 + (lane >> 4) * 4;
-        if (n >= p.N || row >= p.M) continue;
         f32x4 sum[MATS] = {};
 #pragma unroll 4
         for (int s = 0; s < p.slices; ++s)
@@ -553,7 +590,7 @@ __global__ __launch_bounds__(256) void w4_finish_kernel(W4Params p) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             float v[2] = {sum[0][r], sum[MATS - 1][r]};
-            if (row + r < p.M) finish<XT, F32, SWIGLU>(p, v, row + r, n);
+            finish<XT, F32, SWIGLU>(p, v, row + r, n, n < p.N && row + r < p.M);
         }
     }
 }
