@@ -689,7 +689,8 @@ CASCADE_API int32_t cascade_w4_pack(const cascade_w4_weights *weights, const voi
                         void *stream);
 
 /* Y = epilogue(X W^T), the few-row counterpart of cascade_shard_gemm: every weight is read once for
- * up to 64 rows (more rows: once for every 64 of them; prompts are better served by weights in bf16).
+ * up to 64 rows (fp32 X: 32; more rows: once for every 64, or 32, of them; prompts are better served
+ * by weights in bf16).
  * X [rows, k] in the weights' dtype, or in 8 bits with x_scale [rows, k / x_group] (dense).  W_up:
  * EPI_SWIGLU only, of the same sizes, dtype, group and zero_points.  Codes, zeros and 8-bit X enter
  * the products exactly, sums are fp32 (of INT8 X: whole numbers within a group, then fp32).
