@@ -230,7 +230,7 @@ __device__ __forceinline__ float plain_outputs(const W4Params &p, int which, int
 template <int XT, bool F32, bool SWIGLU>
 __device__ __forceinline__ void finish(const W4Params &p, float (&v)[2], int row, int n, bool is) {
     typedef typename std::conditional<F32, float, bf16_t>::type T;
-#pragma unroll
+#pragma unroll 1                                            // (one copy of what is formed again: registers)
     for (int u = 0; u < (SWIGLU ? 2 : 1); ++u) {
         if ((XT == X_E4M3 || XT == X_INT8) && p.x_groups == 1 && is) v[u] *= p.x_scale[row];
         const bool mend = is && !(fabsf(v[u]) < __builtin_inff());
