@@ -646,7 +646,8 @@ CASCADE_API int32_t cascade_pages_copy(const cascade_paged_cache *cache, int32_t
 /* The residual's addition and the norm behind it:
  *   s = x + delta;  sum = s;  y = norm(s) * gain (+ bias);  q * q_scale = y in 8 bits
  * delta NULL: s = x.  Any of sum, y and q (with q_scale) may be NULL, one is wanted.  s, its
- * statistics and y are fp32 and each output is rounded once: y does not see the rounding of sum.
+ * statistics and y are fp32 (a row's sum of squares has to stay in its range: |s| up to 1e17) and
+ * each output is rounded once: y does not see the rounding of sum.
  * Of a group with largest magnitude A, q_scale = max(A / 127, 2^-100) and q = y / q_scale rounded
  * to nearest even (E4M3: 448 in the place of 127), the quotient as y times 1 / q_scale, 2^-23 of it
  * off at most; a group that holds an infinity or NaN has q_scale = NaN and q = 0.
@@ -689,8 +690,8 @@ CASCADE_API int32_t cascade_w4_pack(const cascade_w4_weights *weights, const voi
                         void *stream);
 
 /* Y = epilogue(X W^T), the few-row counterpart of cascade_shard_gemm: every weight is read once for
- * up to 64 rows (fp32 X: 32; more rows: once for every 64, or 32, of them; prompts are better served
- * by weights in bf16).
+ * up to 64 rows (fp32 X: 32; more rows: once for every 64, or 32, of them; from some 200 rows on
+ * weights in bf16 serve better).
  * X [rows, k] in the weights' dtype, or in 8 bits with x_scale [rows, k / x_group] (dense).  W_up:
  * EPI_SWIGLU only, of the same sizes, dtype, group and zero_points.  Codes, zeros and 8-bit X enter
  * the products exactly, sums are fp32 (of INT8 X: whole numbers within a group, then fp32).

@@ -14,7 +14,9 @@
 // lane moves, one copy of a step), which its wavefronts fetch from cold caches.
 //
 // Measured (us, bf16): one row of 128256 7.4 + 13; 256 rows with mixed settings 37 (1.8 TB/s: some 45 instructions and an LDS atomic
-// a logit) + 55 (the rows whose borders lie deep); 32 fp32 rows of 50257 without filters 7.3 + 30 (a second look at each row).
+// a logit) + 55 to 65 (the rows whose borders lie deep, by their settings); 32 fp32 rows of 50257 without filters 7.3 + 30 (a second
+// look at each row).  The second pass spills: 1024 threads leave 128 registers, eight pieces under way and what lives across the
+// look at a row want more (bf16 340 bytes of scratch memory a lane, fp32 176).
 //
 // Weights are exp(z / 24), z = 24 l / temperature in 64 bits; relative to the middle of the bin, at most a 48th away, they are whole
 // numbers of 2^-29, so that sums within a bin are exact and do not depend on any order; the rounding (2^-30 of a weight, either
